@@ -155,16 +155,15 @@ def _signed(v):
     return v - (1 << 64) if v >> 63 else v
 
 
-def _kept(rows, cols, drop, seed, site):
-    """Element (r, c) goes by 16 bits of output number 1 + site 2^40 + r ceil(cols / 4) + c / 4 of SplitMix64."""
-    q = (cols + 3) // 4
-    count = torch.arange(1, rows * q + 1, dtype=torch.int64, device="cuda") + (site << 40)
+def _kept(n, drop, seed, site):
+    """Element e goes by 16 bits, the (e mod 4)-th, of output number 1 + site 2^40 + e / 4 of SplitMix64."""
+    count = torch.arange(1, (n + 3) // 4 + 1, dtype=torch.int64, device="cuda") + (site << 40)
     z = count * _signed(0x9E3779B97F4A7C15) + _signed(seed)
     z = (z ^ _shifted(z, 30)) * _signed(0xBF58476D1CE4E5B9)
     z = (z ^ _shifted(z, 27)) * _signed(0x94D049BB133111EB)
     z = z ^ _shifted(z, 31)
-    bits = (z.view(rows, q, 1) >> torch.arange(0, 64, 16, device="cuda")) & 0xFFFF
-    return bits.view(rows, 4 * q)[:, :cols] >= int(drop * 65536 + 0.5)
+    bits = (z[:, None] >> torch.arange(0, 64, 16, device="cuda")) & 0xFFFF
+    return bits.view(-1)[:n] >= int(drop * 65536 + 0.5)
 
 
 def _scale(drop):
@@ -174,8 +173,7 @@ def _scale(drop):
 
 def _dropped(x, drop, seed, site):
     """fp32 x with its dropped elements zero and the others scaled."""
-    kept = _kept(x.numel() // x.shape[-1], x.shape[-1], drop, seed, site).view(x.shape)
-    return torch.where(kept, x * _scale(drop), 0.0)
+    return torch.where(_kept(x.numel(), drop, seed, site).view(x.shape), x * _scale(drop), 0.0)
 
 
 def _plain_drop(s):
@@ -267,10 +265,9 @@ def work(case):
 
 # ---- the definition in 64 bits -----------------------------------------------------------------------------------
 
-def _keep_factors(first_row, rows, cols, drop, seed, site):
-    """0 or the scale for every element of some rows, from numpy's unsigned words and their 16-bit quarters."""
-    q = -(-cols // 4)
-    c = np.arange(first_row * q, (first_row + rows) * q, dtype=np.uint64) + np.uint64((site << 40) + 1)
+def _keep_factors(first, n, drop, seed, site):
+    """0 or the scale for n elements from the first-th on, from numpy's unsigned words and their 16-bit quarters."""
+    c = np.arange(first // 4, (first + n - 1) // 4 + 1, dtype=np.uint64) + np.uint64((site << 40) + 1)
     with np.errstate(over="ignore"):
         z = np.uint64(seed) + c * np.uint64(0x9E3779B97F4A7C15)
         for shift, factor in ((30, 0xBF58476D1CE4E5B9), (27, 0x94D049BB133111EB)):
@@ -278,7 +275,7 @@ def _keep_factors(first_row, rows, cols, drop, seed, site):
             z *= np.uint64(factor)
         z ^= z >> np.uint64(31)
     gone = math.floor(drop * 65536 + 0.5)
-    quarters = z.astype("<u8").view("<u2").reshape(rows, 4 * q)[:, :cols]
+    quarters = z.astype("<u8").view("<u2")[first % 4:first % 4 + n]
     return torch.from_numpy(quarters >= gone).cuda().double() * (65536.0 / (65536 - gone))
 
 
@@ -306,7 +303,7 @@ def _exact_norm(s):
             z = w[j, :, None] * xh + b[j, :, None]
             factor = torch.ones((), dtype=torch.float64, device="cuda")
             if s["drop"]:
-                factor = _keep_factors((j * I + i) * S, k * S, C, s["drop"], s["seed"], s["site"])
+                factor = _keep_factors((j * I + i) * S * C, k * S * C, s["drop"], s["seed"], s["site"])
                 factor = factor.view(k, S, C).permute(0, 2, 1)
             if not s["backward"]:
                 a = {"none": lambda t: t, "relu": torch.relu, "silu": lambda t: t * torch.sigmoid(t)}[s["act"]](z)
@@ -340,5 +337,6 @@ def exact(case, seed):
     step = max(1, (1 << 24) // cols)
     for r in range(0, rows, step):
         k = min(step, rows - r)
-        y[r:r + k] = s["x"][r:r + k].double() * _keep_factors(r, k, cols, case["drop"], s["seed"], s["site"])
+        factors = _keep_factors(r * cols, k * cols, case["drop"], s["seed"], s["site"])
+        y[r:r + k] = s["x"][r:r + k].double() * factors.view(k, cols)
     return y + s["residual_x"].double() if case["residual"] else y
