@@ -324,6 +324,76 @@ int kavg_meta_update_flat(float* w_tilde_dev, float* v_dev, float* replicas_dev,
                           size_t replica_stride, uint16_t* shadow_dev, size_t shadow_stride,
                           int P, size_t n, float mu, void* hip_stream);
 
+/* ---- Layers of a learner: normalisation and regularisation --------------------------------------------------------
+ * Stateless calls on caller arrays for learners whose local steps the caller writes (F is any model, the meta step is
+ * kavg_meta_update_flat's).  The activations of all learners are one tensor, channels last, and every learner has its
+ * own parameters, which may lie inside its replica.  dtype is that of the activations (KAVG_FP32 or KAVG_BF16);
+ * parameters, statistics, every sum and their gradients are fp32, and a result is rounded once (bf16: nearest, ties to
+ * even).  All calls are asynchronous on hip_stream (NULL = the default stream), work on the current device, hold nothing
+ * between calls, and may be recorded into a graph.
+ * Errors: KAVG_EINVAL for what a call says it wants and does not get (checked before any device call), KAVG_ENOMEM
+ * (workspace too small), KAVG_EDEVICE (a launch failed). */
+#define KAVG_ACT_NONE 0
+#define KAVG_ACT_RELU 1
+#define KAVG_ACT_SILU 2                  /* z / (1 + exp(-z)) */
+
+/* Images of all learners: element (j, i, s, c) at data[j*set_stride + i*image_stride + s*row_stride + c], in elements.
+ * Strides of inputs may be anything from 0 on; rows, images and sets of an output may not overlap. */
+typedef struct {
+    void* data;                          /* dev */
+    int64_t set_stride, image_stride, row_stride;
+} kavg_images;
+
+/* Group norm of images [sets][images][positions][channels]: the channels of an image are cut into `groups` equal runs,
+ *   m, v = mean and variance (divided by the count) of a run's positions * channels/groups values,
+ *   z = weight_c (x - m) / sqrt(v + eps) + bias_c,   y = activation(z),
+ * and where drop > 0, y is then dropped as by kavg_dropout (element numbers of the whole [sets][images][positions]
+ * [channels] tensor).  sets: learners, each with its own weight and bias.  Any size may be 0 but channels and groups.
+ * Limits: fewer than 2^42 elements, eps > 0, 0 <= drop <= 1, site < 2^24. */
+typedef struct {
+    int dtype, activation;
+    int64_t sets, images, positions;
+    int channels, groups;
+    float eps;
+    int reserved;                        /* 0 */
+    double drop;
+    uint64_t seed, site;
+} kavg_norm;
+
+/* Bytes of device workspace a call wants (may be 0). */
+int kavg_group_norm_workspace(const kavg_norm* norm, int backward, size_t* bytes);
+
+/* weight, bias: learner j's [channels] at weight + j*weight_stride; NULL = ones / zeros.  mean, rstd: [sets][images]
+ * [groups], m and 1/sqrt(v + eps), both NULL if not wanted.  y may be x (same strides). */
+int kavg_group_norm(const kavg_norm* norm, const kavg_images* x, const float* weight, int64_t weight_stride,
+                    const float* bias, int64_t bias_stride, const kavg_images* y, float* mean, float* rstd,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* From dy, the gradient of y, and what the forward call read and left (x, mean, rstd, weight, bias and the same `norm`):
+ * dx, and dweight, dbias (learner j's [channels] at dweight + j*dweight_stride; either may be NULL), which are written,
+ * not added to, and summed over a learner's images and positions in a fixed order.  ReLU's derivative at 0 is 0.
+ * dx may be dy (same strides). */
+int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const kavg_images* x, const float* mean,
+                             const float* rstd, const float* weight, int64_t weight_stride, const float* bias,
+                             int64_t bias_stride, const kavg_images* dx, float* dweight, int64_t dweight_stride,
+                             float* dbias, int64_t dbias_stride, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* Dropout of [rows][cols] (strides in elements): y = keep ? x / (1 - p) : 0, plus the residual where there is one
+ * (residual NULL: none).  The mask is never stored: element number e = row*cols + col is kept if the 16 bits at
+ * 16*(e mod 4) of SplitMix64 output number 1 + site*2^40 + floor(e/4), seeded with `seed`, are at least
+ * T = floor(65536*drop + 1/2); so p = T/65536 (at most 2^-17 from drop), and 1/(1-p) is that of the p in force, so that
+ * the expectation of y is x.  A dropped element gives zero whatever x holds, infinities and NaN among it.
+ * site: the place in the model and the step (a number of the caller's, < 2^24), so that one seed serves them all.
+ * The backward call with the same drop, seed and site applies the same mask to dy (the residual's gradient is dy itself).
+ * y may be x or residual, dx may be dy (same strides).
+ * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, drop outside [0, 1], site >= 2^24, unknown dtype, null pointers,
+ * an output whose rows overlap. */
+int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
+                 int64_t rows, int64_t cols, int dtype, double drop, uint64_t seed, uint64_t site, void* hip_stream);
+int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int64_t rows, int64_t cols,
+                          int dtype, double drop, uint64_t seed, uint64_t site, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,6 +1,7 @@
 // Minibatch index stream, label / index validation, and the fused
 // softmax-cross-entropy + gradient kernel of the learner step.
 #include "kavg_internal.h"
+#include "counter_stream.h"
 #include "loss_mean.h"
 
 namespace kavg {
@@ -13,12 +14,6 @@ namespace kavg {
 // with `seed`: because that generator's state is seed + i*gamma after i
 // steps, any draw is computed directly from its counter.  Integer only.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint64_t splitmix64_mix(uint64_t z) {
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    return z ^ (z >> 31);
-}
-
 __global__ void index_stream_kernel(int32_t* __restrict__ idx, int P, int K, int B,
                                     uint64_t seed, uint32_t t0, uint32_t N) {
     size_t e = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -28,7 +23,7 @@ __global__ void index_stream_kernel(int32_t* __restrict__ idx, int P, int K, int
     uint32_t k = (uint32_t)((e / B) % K);
     uint64_t j = e / ((size_t)B * K);
     uint64_t c = (j << 40) | ((uint64_t)(t0 + k) << 16) | s;
-    uint64_t z = splitmix64_mix(seed + (c + 1) * 0x9E3779B97F4A7C15ull);
+    uint64_t z = splitmix64_mix(seed + (c + 1) * SPLITMIX_GAMMA);
     idx[e] = (int32_t)(z % (uint64_t)N);
 }
 

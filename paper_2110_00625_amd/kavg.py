@@ -5,6 +5,7 @@ if the library is missing or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -13,6 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libkavg.so")
 
 KAVG_OK, KAVG_EINVAL, KAVG_ENOMEM, KAVG_EDEVICE, KAVG_ESTATE = 0, 1, 2, 3, 4
 KAVG_FP32, KAVG_BF16 = 0, 1
+KAVG_ACT_NONE, KAVG_ACT_RELU, KAVG_ACT_SILU = 0, 1, 2
 _CODES = {1: "KAVG_EINVAL", 2: "KAVG_ENOMEM", 3: "KAVG_EDEVICE", 4: "KAVG_ESTATE"}
 
 EXPORTS = [
@@ -22,6 +24,7 @@ EXPORTS = [
     "kavg_destroy", "kavg_meta_update_flat", "kavg_profile", "kavg_profile_read",
     "kavg_velocity_bytes", "kavg_set_learner_momentum", "kavg_velocity", "kavg_graph", "kavg_init_static", "kavg_probe", "kavg_refresh_bytes", "kavg_set_refresh",
     "kavg_num_params_conv", "kavg_workspace_bytes_conv", "kavg_init_conv", "kavg_fused", "kavg_set_fused", "kavg_set_wait_limit",
+    "kavg_group_norm_workspace", "kavg_group_norm", "kavg_group_norm_backward", "kavg_dropout", "kavg_dropout_backward",
 ]
 STATIC_WORKSPACE_BYTES = 32 << 20
 CLASS_NAMES = ["index", "forward", "loss", "backward", "update", "meta", "head", "correction"]
@@ -49,7 +52,7 @@ def load_library():
         raise FileNotFoundError(
             "%s not found: build it with `python -m paper_2110_00625_amd.build`" % LIB_PATH)
     lib = ctypes.CDLL(LIB_PATH)
-    c_int, c_f, c_sz, c_vp = ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
+    c_int, c_f, c_sz, c_vp, c_i64 = ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int64
     ip = ctypes.POINTER(ctypes.c_int)
     lib.kavg_num_params.restype = c_sz
     lib.kavg_num_params.argtypes = [c_int, ip]
@@ -94,6 +97,14 @@ def load_library():
         "kavg_graph": [c_vp, c_int],
         "kavg_set_refresh": [c_vp, c_int, c_vp, c_sz],
         "kavg_meta_update_flat": [c_vp, c_vp, c_vp, c_sz, c_vp, c_sz, c_int, c_sz, c_f, c_vp],
+        "kavg_group_norm_workspace": [ctypes.c_char_p, c_int, ctypes.POINTER(c_sz)],
+        "kavg_group_norm": [ctypes.c_char_p, ctypes.c_char_p, c_vp, c_i64, c_vp, c_i64, ctypes.c_char_p, c_vp, c_vp, c_vp, c_sz, c_vp],
+        "kavg_group_norm_backward": [ctypes.c_char_p] * 3 + [c_vp, c_vp, c_vp, c_i64, c_vp, c_i64, ctypes.c_char_p,
+                                                             c_vp, c_i64, c_vp, c_i64, c_vp, c_sz, c_vp],
+        "kavg_dropout": [c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_int, ctypes.c_double, ctypes.c_uint64,
+                         ctypes.c_uint64, c_vp],
+        "kavg_dropout_backward": [c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_int, ctypes.c_double, ctypes.c_uint64,
+                                  ctypes.c_uint64, c_vp],
         "kavg_probe": [c_int, c_vp, c_vp, c_sz, c_int, c_vp, c_vp, ctypes.POINTER(ctypes.c_double)],
     }.items():
         fn = getattr(lib, name)
@@ -158,6 +169,222 @@ def kavg_probe(kind, a=None, b=None, iters=1, sink=None, stream=None):
     if rc != KAVG_OK:
         raise KavgError(rc, "kavg_probe rejected its arguments" if rc == KAVG_EINVAL else "HIP launch failed")
     return work.value
+
+
+# -- layers of a learner: calls on caller tensors, on the current stream of their device -------------------------------
+
+_NORM = struct.Struct("=iiqqqiifidQQ")        # kavg_norm
+_IMAGES = struct.Struct("=Qqqq")              # kavg_images
+
+
+def _bad(text):
+    raise KavgError(KAVG_EINVAL, text)
+
+
+def _activations(x, name, dims):
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        _bad("%s is no device tensor" % name)
+    if x.dtype is not torch.float32 and x.dtype is not torch.bfloat16:
+        _bad("%s is %s: float32 or bfloat16 is wanted" % (name, x.dtype))
+    if x.dim() not in dims:
+        _bad("%s has %d dimensions" % (name, x.dim()))
+    return x
+
+
+def _like(t, x, name):
+    if t.dtype is not x.dtype or t.shape != x.shape or t.device != x.device:
+        _bad("%s is not of x's type, shape and device" % name)
+    return t
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        load_library()
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
+def _images(x, name):
+    """kavg_images of [sets][images][positions][channels] or [images][positions][channels]."""
+    st = x.stride()
+    if st[-1] != 1 and x.shape[-1] > 1:
+        _bad("%s is not channels last (its last stride is %d)" % (name, st[-1]))
+    return _IMAGES.pack(x.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+
+
+def _params(p, x, sets, name):
+    """(pointer, learner stride) of a fp32 [sets][channels] (or [channels]) tensor, None: (None, 0)."""
+    if p is None:
+        return None, 0
+    if p.dtype is not _torch_module.float32 or p.device != x.device or tuple(p.shape) != ((sets, x.shape[-1]) if x.dim() == 4 else (x.shape[-1],)):
+        _bad("%s is not a float32 tensor of [%schannels] on x's device" % (name, "sets, " if x.dim() == 4 else ""))
+    if p.stride(-1) != 1 and p.shape[-1] > 1:
+        _bad("%s has a last stride of %d" % (name, p.stride(-1)))
+    return p.data_ptr(), p.stride(0) if p.dim() == 2 else 0
+
+
+def _norm(x, groups, eps, activation, drop, seed, site):
+    shape = x.shape
+    try:
+        return _NORM.pack(1 if x.dtype is _torch_module.bfloat16 else 0, activation, shape[0] if len(shape) == 4 else 1, shape[-3],
+                          shape[-2], shape[-1], groups, eps, 0, drop, seed, site)
+    except struct.error as e:
+        _bad(str(e))
+
+
+class _OnDevice:
+    """The current device is x's while a call is made; its current stream."""
+
+    def __init__(self, x):
+        cuda = _torch_module.cuda
+        self.stream = cuda.current_stream(x.device).cuda_stream
+        self.guard = None if x.device.index == cuda.current_device() else cuda.device(x.device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *args):
+        if self.guard is not None:
+            self.guard.__exit__(*args)
+
+
+def _workspace(lib, norm, backward, x):
+    n = ctypes.c_size_t(0)
+    if lib.kavg_group_norm_workspace(norm, backward, ctypes.byref(n)) != KAVG_OK:
+        _bad("kavg_group_norm rejected its sizes or options")
+    if not n.value:
+        return None, None, 0
+    block = _torch_module.empty(n.value, dtype=_torch_module.uint8, device=x.device)
+    return block, block.data_ptr(), n.value
+
+
+def _done(rc, name):
+    if rc != KAVG_OK:
+        raise KavgError(rc, "%s rejected its arguments" % name if rc == KAVG_EINVAL else "HIP launch failed")
+
+
+def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE, drop=0.0, seed=0, site=0, stats=False, out=None):
+    """Group norm of channels-last images, an activation, and dropout (where drop > 0) behind it.
+    x [sets, images, positions, channels] with weight, bias [sets, channels] (float32; None: ones, zeros), or
+    [images, positions, channels] with [channels]; float32 or bfloat16, any strides but a last one of 1.
+    Returns y (out, if given: x itself among others), or with stats=True (y, mean, rstd), the latter [sets, images, groups]
+    or [images, groups] in float32, which kavg_group_norm_backward wants."""
+    torch = _torch()
+    _activations(x, "x", (3, 4))
+    norm = _norm(x, groups, eps, activation, drop, seed, site)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
+    w, ws = _params(weight, x, x.shape[0], "weight")
+    b, bs = _params(bias, x, x.shape[0], "bias")
+    lib = _lib
+    block, at, nbytes = _workspace(lib, norm, 0, x)
+    mean = rstd = None
+    if stats:
+        mean, rstd = torch.empty((2,) + tuple(x.shape[:-2]) + (groups,), dtype=torch.float32, device=x.device)
+    with _OnDevice(x) as st:
+        rc = lib.kavg_group_norm(norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), mean.data_ptr() if stats else None,
+                                 rstd.data_ptr() if stats else None, at, nbytes, st)
+    _done(rc, "kavg_group_norm")
+    return (y, mean, rstd) if stats else y
+
+
+def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation=KAVG_ACT_NONE, drop=0.0, seed=0, site=0,
+                             out=None, dweight=None, dbias=None):
+    """Gradients of kavg_group_norm (same options; mean, rstd as it returned them): dx (out, if given: dy itself among
+    others), dweight, dbias (float32, [sets, channels] or [channels]; written into the tensors given, which may lie in a
+    learner's gradient vector; None where weight, bias are None)."""
+    torch = _torch()
+    _activations(x, "x", (3, 4))
+    _like(dy, x, "dy")
+    norm = _norm(x, groups, 1.0, activation, drop, seed, site)       # (eps went into rstd)
+    lib = _lib
+    block, at, nbytes = _workspace(lib, norm, 1, x)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
+    sets = x.shape[0]
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous() or tuple(t.shape) != tuple(x.shape[:-2]) + (groups,):
+            _bad("%s is not what kavg_group_norm returned" % name)
+    w, ws = _params(weight, x, sets, "weight")
+    b, bs = _params(bias, x, sets, "bias")
+    if dweight is None and weight is not None:
+        dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
+    if dbias is None and bias is not None:
+        dbias = torch.empty(bias.shape, dtype=torch.float32, device=x.device)
+    gw, gws = _params(dweight, x, sets, "dweight")
+    gb, gbs = _params(dbias, x, sets, "dbias")
+    with _OnDevice(x) as st:
+        rc = lib.kavg_group_norm_backward(norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(), rstd.data_ptr(), w, ws, b, bs,
+                                          _images(dx, "out"), gw, gws, gb, gbs, at, nbytes, st)
+    _done(rc, "kavg_group_norm_backward")
+    return dx, dweight, dbias
+
+
+def _rows(x, name):
+    """(rows, columns, row stride) of a tensor whose last dimension lies together and whose others are evenly spaced rows."""
+    shape, st = x.shape, x.stride()
+    if x.dim() == 0:
+        return 1, 1, 1
+    cols, rows = shape[-1], 1
+    if x.is_contiguous():
+        return (x.numel() // cols if cols else 0), max(cols, 1), max(cols, 1)
+    if cols == 0 or x.numel() == 0:
+        return 0, max(cols, 1), max(cols, 1)
+    if st[-1] != 1 and cols > 1:
+        _bad("%s has a last stride of %d" % (name, st[-1]))
+    stride = None
+    for d in range(x.dim() - 2, -1, -1):
+        if shape[d] == 1:
+            continue
+        if stride is None:
+            stride = st[d]
+        elif st[d] != stride * rows:
+            _bad("%s does not lie in evenly spaced rows" % name)
+        rows *= shape[d]
+    return rows, cols, cols if stride is None else stride
+
+
+def _dropout(name, x, drop, seed, site, residual, out):
+    torch = _torch()
+    _activations(x, "dy" if residual is _NO_RESIDUAL else "x", range(0, 65))
+    if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 24:
+        _bad("seed %d, site %d" % (seed, site))
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
+    rows, cols, xs = _rows(x, "x")
+    ys = _rows(y, "out")[2]
+    dtype = 1 if x.dtype is torch.bfloat16 else 0
+    try:
+        with _OnDevice(x) as st:
+            if residual is _NO_RESIDUAL:
+                rc = _lib.kavg_dropout_backward(x.data_ptr(), xs, y.data_ptr(), ys, rows, cols, dtype, drop, seed, site, st)
+            else:
+                at, rs = (None, 0) if residual is None else (_like(residual, x, "residual").data_ptr(), _rows(residual, "residual")[2])
+                rc = _lib.kavg_dropout(x.data_ptr(), xs, at, rs, y.data_ptr(), ys, rows, cols, dtype, drop, seed, site, st)
+    except ctypes.ArgumentError as e:
+        _bad(str(e))
+    _done(rc, name)
+    return y
+
+
+_NO_RESIDUAL = object()
+
+
+def kavg_dropout(x, drop, seed, site=0, residual=None, out=None):
+    """Dropout of a float32 or bfloat16 tensor in evenly spaced rows (contiguous, or slices of the last dimension), plus a
+    residual of the same shape.  The mask is that of (drop, seed, site) and of an element's number in row-major order; it is
+    not stored.  out: x or the residual among others."""
+    return _dropout("kavg_dropout", x, drop, seed, site, residual, out)
+
+
+def kavg_dropout_backward(dy, drop, seed, site=0, out=None):
+    """Gradient of kavg_dropout with respect to x (that with respect to the residual is dy)."""
+    return _dropout("kavg_dropout_backward", dy, drop, seed, site, _NO_RESIDUAL, out)
 
 
 class MAvg:
