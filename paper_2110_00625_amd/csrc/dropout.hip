@@ -2,6 +2,7 @@
 // (counter_stream.h), so the backward pass draws it again and nothing is stored.  Bound by memory: an element is read and written once,
 // and a draw of 64 bits serves four of them.
 #include "layers.h"
+#include "fastdiv.h"
 #include <cmath>
 
 namespace kavg {
@@ -13,27 +14,114 @@ DropRule drop_rule(double drop, uint64_t seed, uint64_t site) {
 
 namespace {
 
-template <class E>
-__global__ void __launch_bounds__(256) dropout_kernel(DropCall c) {
-    const uint64_t n = (uint64_t)c.rows * c.cols;
-    for (uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (uint64_t)gridDim.x * 256) {
-        const uint64_t r = e / c.cols, k = e % c.cols;
-        float v = drop_keeps(c.drop, e) ? to_float(((const E*)c.x)[r * c.x_stride + k]) * c.drop.scale : 0.f;
-        if (c.residual) v += to_float(((const E*)c.residual)[r * c.residual_stride + k]);
-        ((E*)c.y)[r * c.y_stride + k] = from_float<E>(v);
+constexpr int T = 256;
+
+// U packs of V elements (16 bytes) per lane, T packs apart; pack i of the tensor lies in row i / per_row.  A row's last pack, if V does
+// not divide its length, is the last V elements, of which the pack before has had `skip`: they are read for nothing and not written
+// (in place they may have changed by then).  No load stands behind a branch: a lane with nothing to do reads the last pack.
+template <class E, int U, bool ROWS, bool ALIGNED, bool RESIDUAL>
+__device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first, uint64_t per_row, uint32_t div_m, int div_s) {
+    constexpr int V = 16 / sizeof(E);
+    typedef typename Pack<E, V>::type pack;
+    const uint64_t total = per_row * c.rows;
+    // (ROWS: per_row < 2^28, so that what is divided stays below 2^30)
+    const uint64_t row0 = ROWS ? first / per_row : 0;
+    const uint32_t pack0 = (uint32_t)(first - row0 * per_row);
+    uint64_t row[U], col[U];
+    int skip[U];                                            // V: nothing to do
+    pack xv[U], rv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t i = u * T + threadIdx.x;
+        const bool none = first + i >= total;
+        if (none) i = (uint32_t)(total - 1 - first);
+        row[u] = 0;
+        if (ROWS) {
+            const uint32_t r = fastdiv(pack0 + i, div_m, div_s);
+            row[u] = row0 + r;
+            col[u] = (uint64_t)(pack0 + i - r * (uint32_t)per_row) * V;
+        } else col[u] = (first + i) * V;
+        skip[u] = 0;
+        if (!ALIGNED || ROWS) {
+            const int64_t over = (int64_t)col[u] + V - c.cols;
+            if (over > 0) { col[u] -= over; skip[u] = (int)over; }
+        }
+        if (none) skip[u] = V;
+        xv[u] = pack_load<E, V>((const E*)c.x + row[u] * c.x_stride + col[u]);
+        if (RESIDUAL) rv[u] = pack_load<E, V>((const E*)c.residual + row[u] * c.residual_stride + col[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = to_float(xv[u][i]);
+        if (c.drop.threshold) drop_apply<V, ALIGNED>(c.drop, row[u] * c.cols + col[u], v);
+        pack o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = from_float<E>(RESIDUAL ? v[i] + to_float(rv[u][i]) : v[i]);
+        E* y = (E*)c.y + row[u] * c.y_stride + col[u];
+        if (skip[u] == 0) pack_store<E, V>(y, o);
+        else {
+#pragma unroll
+            for (int i = 1; i < V; ++i) if (i >= skip[u]) y[i] = o[i];
+        }
+    }
+}
+
+template <class E, int U, bool ROWS, bool ALIGNED, bool RESIDUAL>
+__global__ void __launch_bounds__(T) dropout_kernel(DropCall c, uint64_t per_row, uint32_t div_m, int div_s) {
+    constexpr int V = 16 / sizeof(E);
+    const uint64_t first = (uint64_t)blockIdx.x * (U * T);
+    if (ROWS) packs_of_lane<E, U, true, ALIGNED, RESIDUAL>(c, first, per_row, div_m, div_s);
+    else if (first + U * T <= (uint64_t)c.cols / V) packs_of_lane<E, U, false, true, RESIDUAL>(c, first, per_row, 0, 0);
+    else packs_of_lane<E, U, false, false, RESIDUAL>(c, first, per_row, 0, 0);     // the end of the tensor
+}
+
+// rows of fewer than V elements: an element per lane
+template <class E>
+__global__ void __launch_bounds__(T) dropout_short_kernel(DropCall c) {
+    const uint64_t e = (uint64_t)blockIdx.x * T + threadIdx.x;
+    if (e >= (uint64_t)c.rows * c.cols) return;
+    const uint64_t r = e / c.cols, k = e - r * c.cols;
+    float v = to_float(((const E*)c.x)[r * c.x_stride + k]);
+    if (c.drop.threshold) v = drop_keeps(c.drop, e) ? v * c.drop.scale : 0.f;
+    if (c.residual) v += to_float(((const E*)c.residual)[r * c.residual_stride + k]);
+    ((E*)c.y)[r * c.y_stride + k] = from_float<E>(v);
+}
+
+template <class E, int U, bool ROWS, bool ALIGNED>
+void start(const DropCall& c, uint64_t per_row, hipStream_t st) {
+    uint32_t m = 0;
+    int s = 0;
+    if (ROWS) fastdiv_make((uint32_t)per_row, &m, &s);
+    const dim3 grid((unsigned)((per_row * c.rows + U * T - 1) / (U * T)));
+    if (c.residual) dropout_kernel<E, U, ROWS, ALIGNED, true><<<grid, dim3(T), 0, st>>>(c, per_row, m, s);
+    else dropout_kernel<E, U, ROWS, ALIGNED, false><<<grid, dim3(T), 0, st>>>(c, per_row, m, s);
+}
+
+template <class E>
+hipError_t launch(const DropCall& call, hipStream_t st) {
+    constexpr int V = 16 / sizeof(E);
+    DropCall c = call;
+    if (c.x_stride == c.cols && c.y_stride == c.cols && (!c.residual || c.residual_stride == c.cols)) {
+        c.cols *= c.rows;                                   // one row
+        c.rows = 1;
+    }
+    const uint64_t per_row = (c.cols + V - 1) / V;
+    if (c.cols < V) dropout_short_kernel<E><<<dim3((unsigned)((c.rows * c.cols + T - 1) / T)), dim3(T), 0, st>>>(c);
+    else if (c.rows > 1) {
+        if (c.cols % 4 == 0) start<E, 1, true, true>(c, per_row, st);
+        else start<E, 1, true, false>(c, per_row, st);
+    } else if (per_row >= 4 * T * 1024) start<E, 4, false, true>(c, per_row, st);
+    else start<E, 1, false, true>(c, per_row, st);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_dropout(const DropCall& c, hipStream_t st) {
-    const uint64_t n = (uint64_t)c.rows * c.cols;
-    if (!n) return hipSuccess;
-    const uint64_t blocks = (n + 255) / 256;
-    const dim3 grid((unsigned)(blocks < (1u << 20) ? blocks : (1u << 20)));
-    if (c.dtype == KAVG_BF16) dropout_kernel<__bf16><<<grid, dim3(256), 0, st>>>(c);
-    else dropout_kernel<float><<<grid, dim3(256), 0, st>>>(c);
-    return hipGetLastError();
+    if (!c.rows) return hipSuccess;
+    return c.dtype == KAVG_BF16 ? launch<__bf16>(c, st) : launch<float>(c, st);
 }
 
 }  // namespace kavg

@@ -52,6 +52,39 @@ __device__ __forceinline__ bool drop_keeps(const DropRule& d, uint64_t e) {
     return (uint32_t)(drop_bits(d, e >> 2) >> (16 * (e & 3)) & 0xFFFF) >= d.threshold;
 }
 
+// V consecutive elements in registers and in memory, at any multiple of an element's size (the hardware takes 16-byte accesses at any
+// address; one that straddles a line costs a second one)
+template <class E, int V> struct Pack {
+    typedef E type __attribute__((ext_vector_type(V)));
+    typedef type loose __attribute__((aligned(sizeof(E))));
+};
+template <class E, int V> __device__ __forceinline__ typename Pack<E, V>::type pack_load(const E* p) { return *(const typename Pack<E, V>::loose*)p; }
+template <class E, int V> __device__ __forceinline__ void pack_store(E* p, typename Pack<E, V>::type v) { *(typename Pack<E, V>::loose*)p = v; }
+
+// v[i] = keep ? v[i] * scale : 0 for elements e .. e+V-1.  V a multiple of 4: a draw serves four of them; where e is no multiple of 4
+// (ALIGNED false) they straddle one draw more.  A field is compared in the upper half of a word, with the bits below it left where they
+// are: field >= T if the word exceeds (T - 1) 2^16 + 65535 (threshold 1..65536).
+template <int V, bool ALIGNED> __device__ __forceinline__ void drop_apply(const DropRule& d, uint64_t e, float (&v)[V]) {
+    const uint32_t below = ((d.threshold - 1) << 16) | 0xFFFF;
+    uint64_t state = d.base + (e >> 2) * SPLITMIX_GAMMA;
+    uint64_t word = splitmix64_mix(state);
+    const int shift = 16 * (int)(e & 3);
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+        uint64_t fields = word;
+        if (!ALIGNED || i + 4 < V) {
+            state += SPLITMIX_GAMMA;
+            word = splitmix64_mix(state);
+            if (!ALIGNED && shift) fields = (fields >> shift) | (word << (64 - shift));
+        }
+        const uint32_t lo = (uint32_t)fields, hi = (uint32_t)(fields >> 32);
+        v[i] = lo << 16 > below ? v[i] * d.scale : 0.f;
+        v[i + 1] = lo > below ? v[i + 1] * d.scale : 0.f;
+        v[i + 2] = hi << 16 > below ? v[i + 2] * d.scale : 0.f;
+        v[i + 3] = hi > below ? v[i + 3] * d.scale : 0.f;
+    }
+}
+
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__bf16 v) { return (float)v; }
 template <class E> __device__ __forceinline__ E from_float(float v) { return (E)v; }     // bf16: nearest, ties to even

@@ -131,6 +131,8 @@ int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
         const int64_t most = ((int64_t)1 << 46) / rows;
         if (x_stride < 0 || x_stride > most || (residual && (residual_stride < 0 || residual_stride > most)) || y_stride < cols || y_stride > most)
             return KAVG_EINVAL;
+        const bool apart = x_stride != cols || y_stride != cols || (residual && residual_stride != cols);
+        if (apart && cols >= (int64_t)1 << 30) return KAVG_EINVAL;
     }
     const bool one = rows < 2;                              // (its strides say nothing)
     DropCall c = {dtype, x, one ? cols : x_stride, residual, one ? cols : residual_stride, y, one ? cols : y_stride, rows, cols, drop_rule(drop, seed, site)};
