@@ -360,7 +360,7 @@ typedef struct {
     uint64_t seed, site;
 } kavg_norm;
 
-/* Bytes of device workspace a call wants (may be 0). */
+/* Bytes of device workspace a call wants (may be 0); 16-byte aligned. */
 int kavg_group_norm_workspace(const kavg_norm* norm, int backward, size_t* bytes);
 
 /* weight, bias: learner j's [channels] at weight + j*weight_stride; NULL = ones / zeros.  mean, rstd: [sets][images]

@@ -5,7 +5,7 @@
 //     dbias_c = sum dz,  dweight_c = sum dz xh  (over a learner's images and positions),
 //     dx = r (h - mean h - xh mean(h xh))       (means over the group).
 // Statistics and sums are fp32; the variance is taken about the mean, in a second sum.
-#include "layers.h"
+#include "norm_forward.h"
 #include "wave_sum.h"
 
 namespace kavg {
@@ -31,7 +31,7 @@ __device__ __forceinline__ Group group_of_block(const NormCall& c) {
 
 // one workgroup per group
 template <class E, int ACT>
-__global__ void __launch_bounds__(T) norm_forward_kernel(NormCall c) {
+__global__ void __launch_bounds__(T) norm_wide_forward_kernel(NormCall c) {
     __shared__ float lds[4];
     const Group at = group_of_block(c);
     const int D = c.channels / c.groups, c0 = at.group * D;
@@ -129,23 +129,26 @@ hipError_t backward(const NormCall& c, hipStream_t st) {
     return e;
 }
 
-template <class E, int ACT>
-hipError_t forward(const NormCall& c, hipStream_t st) {
+template <class E>
+hipError_t forward(const NormCall& c, void* workspace, hipStream_t st) {
     const int64_t groups = c.sets * c.images * c.groups;
     if (!groups) return hipSuccess;
-    norm_forward_kernel<E, ACT><<<dim3((unsigned)groups), dim3(T), 0, st>>>(c);
+    Tile t;
+    const bool contiguous = c.xs.row == c.channels && c.outs.row == c.channels;
+    if (c.positions && norm_tile(c, contiguous, false, &t)) return tiled_forward<E>(c, t, workspace, st);
+    const dim3 grid((unsigned)groups);
+    switch (c.activation) {
+        case KAVG_ACT_RELU: norm_wide_forward_kernel<E, KAVG_ACT_RELU><<<grid, dim3(T), 0, st>>>(c); break;
+        case KAVG_ACT_SILU: norm_wide_forward_kernel<E, KAVG_ACT_SILU><<<grid, dim3(T), 0, st>>>(c); break;
+        default: norm_wide_forward_kernel<E, KAVG_ACT_NONE><<<grid, dim3(T), 0, st>>>(c);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_group_norm(const NormCall& c, hipStream_t st) {
-    const bool b = c.dtype == KAVG_BF16;
-    switch (c.activation) {
-        case KAVG_ACT_RELU: return b ? forward<__bf16, KAVG_ACT_RELU>(c, st) : forward<float, KAVG_ACT_RELU>(c, st);
-        case KAVG_ACT_SILU: return b ? forward<__bf16, KAVG_ACT_SILU>(c, st) : forward<float, KAVG_ACT_SILU>(c, st);
-        default: return b ? forward<__bf16, KAVG_ACT_NONE>(c, st) : forward<float, KAVG_ACT_NONE>(c, st);
-    }
+hipError_t launch_group_norm(const NormCall& c, void* workspace, hipStream_t st) {
+    return c.dtype == KAVG_BF16 ? forward<__bf16>(c, workspace, st) : forward<float>(c, workspace, st);
 }
 
 hipError_t launch_group_norm_backward(const NormCall& c, hipStream_t st) {

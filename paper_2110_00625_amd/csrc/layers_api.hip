@@ -71,6 +71,12 @@ NormCall call_of(const kavg_norm* n) {
     return c;
 }
 
+int workspace_ok(const kavg_norm* n, const NormCall& c, bool backward, const void* workspace, size_t bytes) {
+    const size_t want = empty(n) ? 0 : norm_workspace(c, backward);
+    if (want > bytes) return KAVG_ENOMEM;
+    return want && (!workspace || ((uintptr_t)workspace & 15)) ? KAVG_EINVAL : KAVG_OK;
+}
+
 int status(hipError_t e) { return e == hipSuccess ? KAVG_OK : KAVG_EDEVICE; }
 
 }  // namespace
@@ -79,8 +85,7 @@ extern "C" {
 
 int kavg_group_norm_workspace(const kavg_norm* norm, int backward, size_t* bytes) {
     if (!norm_ok(norm) || !bytes) return KAVG_EINVAL;
-    (void)backward;
-    *bytes = 0;
+    *bytes = empty(norm) ? 0 : norm_workspace(call_of(norm), backward != 0);
     return KAVG_OK;
 }
 
@@ -89,14 +94,14 @@ int kavg_group_norm(const kavg_norm* norm, const kavg_images* x, const float* we
                     void* hip_stream) {
     if (!norm_ok(norm) || !images_ok(norm, x, false) || !images_ok(norm, y, true) || !mean != !rstd) return KAVG_EINVAL;
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
-    (void)workspace; (void)workspace_bytes;
     NormCall c = call_of(norm);
+    if (const int rc = workspace_ok(norm, c, false, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.out = y->data; c.outs = strides_of(norm, y);
     c.weight = weight; c.weight_stride = weight_stride;
     c.bias = bias; c.bias_stride = bias_stride;
     c.mean = mean; c.rstd = rstd;
-    return status(launch_group_norm(c, (hipStream_t)hip_stream));
+    return status(launch_group_norm(c, workspace, (hipStream_t)hip_stream));
 }
 
 int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const kavg_images* x, const float* mean, const float* rstd,
@@ -107,8 +112,8 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
     if ((!mean || !rstd) && !empty(norm)) return KAVG_EINVAL;
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
     if (!params_ok(norm, dweight, dweight_stride, true) || !params_ok(norm, dbias, dbias_stride, true)) return KAVG_EINVAL;
-    (void)workspace; (void)workspace_bytes;
     NormCall c = call_of(norm);
+    if (const int rc = workspace_ok(norm, c, true, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.dy = dy->data; c.dys = strides_of(norm, dy);
     c.out = dx->data; c.outs = strides_of(norm, dx);

@@ -1,0 +1,173 @@
+// Group norm in tiles that stay in registers: what the forward and the backward kernels share.
+//
+// A tile is some channels (whole groups) of a run of an image's positions.  A lane owns packs of V elements (16 bytes; one element
+// where no pack fits), NV of them: always the same V channels, at positions `lane_rows` apart, so that parameters and sums of a channel
+// stay in the lane's registers, and a wavefront reads and writes whole segments of rows.
+//
+//   rows   V divides the channels: a row is a position, a pack never leaves it.
+//   flat   V does not, but the positions of an image lie end to end: the image is one run of elements, cut into rows of `cols` packs.
+//          cols * V is a multiple of the channels, so a lane's packs still hold the same channels (going round after the last one).
+//   V = 1  neither.
+//
+// An image that one workgroup cannot hold is cut into chunks of NV * lane_rows rows; small images share a workgroup (units).
+#pragma once
+#include "layers.h"
+#include "fastdiv.h"
+
+namespace kavg {
+
+struct Tile {
+    int nv, vec;             // packs per lane, elements per pack
+    bool flat, whole_pack;   // whole_pack: a pack lies in one group
+    int threads, units;      // lanes of a workgroup, images of a workgroup
+    int cols, lane_rows;     // packs per row, rows that the lanes of a unit cover together
+    int channels, groups;    // of a tile
+    int blocks, chunks;      // tiles of an image: along its channels, along its rows
+    int rows;                // of an image
+    uint32_t unit_m, col_m, d_m; int unit_s, col_s, d_s;     // divisions by lanes per unit, cols, channels per group
+    size_t lds;
+};
+
+constexpr int FLAT_PACKS = 8;    // the most packs per lane of a flat tile (its sums are per channel, and its last pack needs care: more spill)
+enum { TILE_WHOLE = 0, TILE_SUMS = 1, TILE_APPLY = 2 };      // sums and results; sums alone (chunks); results from finished sums
+
+// false: no tile fits (groups too wide for a workgroup)
+bool norm_tile(const NormCall& c, bool contiguous, bool backward, Tile* t);
+
+#if defined(__HIPCC__)
+
+// Workgroup -> tile: workgroup g runs on XCD g mod 8, and tiles next to each other share lines of memory and parameters, so each
+// XCD takes a contiguous range of them.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t g, uint32_t n) {
+    const uint32_t per = n / 8, extra = n % 8, x = g % 8;
+    return x * per + (x < extra ? x : extra) + g / 8;
+}
+
+// where a lane works
+template <int V, bool FLAT> struct Lane {
+    uint32_t chunk, block, image, unit, row, col;   // image: of all learners'; row, col: in the unit
+    uint32_t set, image_in_set;
+    int first_channel;                              // of the lane's pack (flat: within the image's channels)
+    bool on;
+    int64_t run;                                    // flat: elements of an image
+
+    __device__ __forceinline__ Lane(const NormCall& c, const Tile& t) {
+        const uint32_t b = xcd_order(blockIdx.x, gridDim.x), per_unit = t.cols * t.lane_rows;
+        const uint32_t rest = b / (uint32_t)t.chunks;
+        chunk = b - rest * t.chunks;
+        const uint32_t first = rest / (uint32_t)t.blocks;
+        block = rest - first * t.blocks;
+        unit = fastdiv(threadIdx.x, t.unit_m, t.unit_s);
+        uint32_t at = threadIdx.x - unit * per_unit;
+        image = first * t.units + unit;
+        on = unit < (uint32_t)t.units && image < (uint32_t)(c.sets * c.images);
+        if (!on) { at = 0; image = first * t.units; unit = 0; }
+        row = FLAT ? 0 : fastdiv(at, t.col_m, t.col_s);
+        col = at - row * t.cols;
+        run = (int64_t)c.positions * c.channels;
+        if (FLAT) first_channel = (int)(col * V % (uint32_t)c.channels);
+        else {
+            first_channel = block * t.channels + col * V;
+            if (first_channel >= c.channels) { on = false; first_channel = 0; }
+        }
+        set = image / (uint32_t)c.images;
+        image_in_set = image - set * (uint32_t)c.images;
+    }
+    __device__ __forceinline__ int channel(const NormCall& c, int i) const {
+        const int ch = first_channel + i;
+        return FLAT && ch >= c.channels ? FLAT && V > c.channels ? ch % c.channels : ch - c.channels : ch;
+    }
+    // row of the image of the lane's pack k
+    __device__ __forceinline__ int image_row(const Tile& t, int k) const { return (int)(chunk * t.nv + k) * t.lane_rows + (int)row; }
+    // elements of pack k that are the image's
+    __device__ __forceinline__ int valid(const Tile& t, int k) const {
+        const int r = image_row(t, k);
+        if (!FLAT) return on && r < t.rows ? V : 0;
+        const int64_t left = run - ((int64_t)r * t.cols + col) * V;
+        return !on || left <= 0 ? 0 : left < V ? (int)left : V;
+    }
+    // is k the last row of an image that is not made of whole rows (flat)?
+    __device__ __forceinline__ bool ragged(const Tile& t, int k) const { return FLAT && (int)(chunk * t.nv + k) == t.rows - 1; }
+    // number of pack 0's first element in the whole tensor; what a pack more adds
+    __device__ __forceinline__ uint64_t number(const NormCall& c, const Tile& t) const {
+        const uint64_t before = (uint64_t)image * run;
+        return before + (FLAT ? ((uint64_t)image_row(t, 0) * t.cols + col) * V : (uint64_t)image_row(t, 0) * c.channels + first_channel);
+    }
+    __device__ __forceinline__ uint64_t number_step(const NormCall& c, const Tile& t) const {
+        return FLAT ? (uint64_t)t.cols * V : (uint64_t)t.lane_rows * c.channels;
+    }
+};
+
+// A lane's packs in a tensor: from `first` on, `step` apart.
+template <int V, bool FLAT> struct Place {
+    int64_t first, step;
+    __device__ __forceinline__ Place(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Strides& s) {
+        first = l.set * s.set + l.image_in_set * s.image;
+        if (FLAT) { first += ((int64_t)l.image_row(t, 0) * t.cols + l.col) * V; step = (int64_t)t.cols * V; }
+        else { first += l.image_row(t, 0) * s.row + l.first_channel; step = t.lane_rows * s.row; }
+        // (a lane without a pack 0 reads the image's first row)
+        if (!l.valid(t, 0)) first = l.set * s.set + l.image_in_set * s.image + (FLAT ? 0 : l.first_channel);
+    }
+};
+
+// Pack k of a tensor; pack 0 once more where the image has no such pack.  One at a flat image's end may reach past it, into the next image,
+// which does no harm, but not past the tensor (extent): there it is put together from single elements.  No load but those stands behind
+// a branch.
+template <class E, int V, bool FLAT>
+__device__ __forceinline__ typename Pack<E, V>::type tile_load(const Tile& t, const Lane<V, FLAT>& l, const E* p, const Place<V, FLAT>& at0, int64_t extent, int k) {
+    const int64_t at = at0.first + (l.valid(t, k) ? k * at0.step : 0);
+    if (!FLAT) return pack_load<E, V>(p + at);
+    typename Pack<E, V>::type v = pack_load<E, V>(p + (at + V <= extent ? at : extent - V));
+    if (l.ragged(t, k) && at + V > extent) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = at + i < extent ? p[at + i] : (E)0.f;
+    }
+    return v;
+}
+
+template <class E, int V, bool FLAT>
+__device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l, E* p, const Place<V, FLAT>& at0, int k, const float (&v)[V]) {
+    const int n = l.valid(t, k);
+    if (!n) return;
+    p += at0.first + k * at0.step;
+    typename Pack<E, V>::type o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = from_float<E>(v[i]);
+    if (!FLAT || n == V) pack_store<E, V>(p, o);
+    else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) if (i < n) p[i] = o[i];
+    }
+}
+
+// Packs stay packed between their uses (the compiler would keep a bf16 pack's floats, twice the registers).
+template <class P> __device__ __forceinline__ void keep_packed(P& v) {
+    if constexpr (sizeof(P) == 16) {
+        typedef int words __attribute__((ext_vector_type(4)));
+        words w = __builtin_bit_cast(words, v);
+        asm volatile("" : "+v"(w));
+        v = __builtin_bit_cast(P, w);
+    }
+}
+
+// v = elements from number e on, dropped.  (Rows: V = 4, 8 divides the channels, so e is a multiple of 4; flat: images of a multiple of 4 elements)
+template <int V, bool FLAT> __device__ __forceinline__ void tile_drop(const DropRule& d, int64_t run, uint64_t e, float (&v)[V]) {
+    if constexpr (V == 1) v[0] = drop_keeps(d, e) ? v[0] * d.scale : 0.f;
+    else if (!FLAT || run % 4 == 0) drop_apply<V, true>(d, e, v);
+    else drop_apply<V, false>(d, e, v);
+}
+
+__device__ __forceinline__ float team_sum(float v, int team) {
+    for (int m = team / 2; m; m /= 2) v += __shfl_xor(v, m);
+    return v;
+}
+// lanes that add up `terms` terms each of `sums` sums together: a power of two, at most a wavefront
+__device__ __forceinline__ int team_of(int threads, int sums, int terms) {
+    int team = 64;
+    while (team > 1 && (team / 2 >= terms || threads / team < sums)) team /= 2;
+    return team;
+}
+
+#endif
+
+}  // namespace kavg

@@ -175,21 +175,34 @@ def kavg_probe(kind, a=None, b=None, iters=1, sink=None, stream=None):
 
 _NORM = struct.Struct("=iiqqqiifidQQ")        # kavg_norm
 _IMAGES = struct.Struct("=Qqqq")              # kavg_images
+_torch_module = _stream_of = None
+_DTYPES = {}
+
+
+def _torch():
+    """The library and torch, loaded at the first call."""
+    global _torch_module, _stream_of
+    if _torch_module is None:
+        load_library()
+        import torch
+        _DTYPES.update({torch.float32: KAVG_FP32, torch.bfloat16: KAVG_BF16})
+        # (the public way to the current stream builds an object, which takes two microseconds)
+        _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _torch_module = torch
+    return _torch_module
 
 
 def _bad(text):
     raise KavgError(KAVG_EINVAL, text)
 
 
-def _activations(x, name, dims):
-    torch = _torch()
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+def _dtype(x, name):
+    if not isinstance(x, _torch_module.Tensor) or not x.is_cuda:
         _bad("%s is no device tensor" % name)
-    if x.dtype is not torch.float32 and x.dtype is not torch.bfloat16:
+    code = _DTYPES.get(x.dtype)
+    if code is None:
         _bad("%s is %s: float32 or bfloat16 is wanted" % (name, x.dtype))
-    if x.dim() not in dims:
-        _bad("%s has %d dimensions" % (name, x.dim()))
-    return x
+    return code
 
 
 def _like(t, x, name):
@@ -198,16 +211,26 @@ def _like(t, x, name):
     return t
 
 
-_torch_module = None
+def _output(x, out):
+    """out, or a contiguous tensor like x."""
+    if out is not None:
+        return _like(out, x, "out")
+    return _torch_module.empty_like(x) if x.is_contiguous() else _torch_module.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
-def _torch():
-    global _torch_module
-    if _torch_module is None:
-        load_library()
-        import torch
-        _torch_module = torch
-    return _torch_module
+def _call(name, x, fn, *args):
+    """fn on x's device and its current stream."""
+    index = x.device.index
+    try:
+        if index == _torch_module.cuda.current_device():
+            rc = fn(*args, _stream_of(index))
+        else:
+            with _torch_module.cuda.device(index):
+                rc = fn(*args, _stream_of(index))
+    except ctypes.ArgumentError as e:
+        _bad(str(e))
+    if rc != KAVG_OK:
+        raise KavgError(rc, "%s rejected its arguments" % name if rc == KAVG_EINVAL else "HIP launch failed")
 
 
 def _images(x, name):
@@ -218,57 +241,37 @@ def _images(x, name):
     return _IMAGES.pack(x.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-def _params(p, x, sets, name):
+def _params(p, x, name):
     """(pointer, learner stride) of a fp32 [sets][channels] (or [channels]) tensor, None: (None, 0)."""
     if p is None:
         return None, 0
-    if p.dtype is not _torch_module.float32 or p.device != x.device or tuple(p.shape) != ((sets, x.shape[-1]) if x.dim() == 4 else (x.shape[-1],)):
-        _bad("%s is not a float32 tensor of [%schannels] on x's device" % (name, "sets, " if x.dim() == 4 else ""))
-    if p.stride(-1) != 1 and p.shape[-1] > 1:
-        _bad("%s has a last stride of %d" % (name, p.stride(-1)))
-    return p.data_ptr(), p.stride(0) if p.dim() == 2 else 0
+    shape = x.shape
+    if p.dtype is not _torch_module.float32 or p.device != x.device or p.shape != (shape[-1:] if len(shape) == 3 else shape[::3]):
+        _bad("%s is not a float32 tensor of [%schannels] on x's device" % (name, "sets, " if len(shape) == 4 else ""))
+    st = p.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        _bad("%s has a last stride of %d" % (name, st[-1]))
+    return p.data_ptr(), st[0] if len(st) == 2 else 0
 
 
 def _norm(x, groups, eps, activation, drop, seed, site):
-    shape = x.shape
+    code, shape = _dtype(x, "x"), x.shape
+    if len(shape) != 3 and len(shape) != 4:
+        _bad("x has %d dimensions: [sets, images, positions, channels] or [images, positions, channels] is wanted" % len(shape))
     try:
-        return _NORM.pack(1 if x.dtype is _torch_module.bfloat16 else 0, activation, shape[0] if len(shape) == 4 else 1, shape[-3],
-                          shape[-2], shape[-1], groups, eps, 0, drop, seed, site)
+        return _NORM.pack(code, activation, shape[0] if len(shape) == 4 else 1, shape[-3], shape[-2], shape[-1], groups, eps, 0, drop, seed, site)
     except struct.error as e:
         _bad(str(e))
 
 
-class _OnDevice:
-    """The current device is x's while a call is made; its current stream."""
-
-    def __init__(self, x):
-        cuda = _torch_module.cuda
-        self.stream = cuda.current_stream(x.device).cuda_stream
-        self.guard = None if x.device.index == cuda.current_device() else cuda.device(x.device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *args):
-        if self.guard is not None:
-            self.guard.__exit__(*args)
-
-
-def _workspace(lib, norm, backward, x):
+def _workspace(norm, backward, x):
     n = ctypes.c_size_t(0)
-    if lib.kavg_group_norm_workspace(norm, backward, ctypes.byref(n)) != KAVG_OK:
+    if _lib.kavg_group_norm_workspace(norm, backward, ctypes.byref(n)) != KAVG_OK:
         _bad("kavg_group_norm rejected its sizes or options")
     if not n.value:
         return None, None, 0
     block = _torch_module.empty(n.value, dtype=_torch_module.uint8, device=x.device)
     return block, block.data_ptr(), n.value
-
-
-def _done(rc, name):
-    if rc != KAVG_OK:
-        raise KavgError(rc, "%s rejected its arguments" % name if rc == KAVG_EINVAL else "HIP launch failed")
 
 
 def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE, drop=0.0, seed=0, site=0, stats=False, out=None):
@@ -277,21 +280,17 @@ def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE,
     [images, positions, channels] with [channels]; float32 or bfloat16, any strides but a last one of 1.
     Returns y (out, if given: x itself among others), or with stats=True (y, mean, rstd), the latter [sets, images, groups]
     or [images, groups] in float32, which kavg_group_norm_backward wants."""
-    torch = _torch()
-    _activations(x, "x", (3, 4))
+    torch = _torch_module or _torch()
     norm = _norm(x, groups, eps, activation, drop, seed, site)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
-    w, ws = _params(weight, x, x.shape[0], "weight")
-    b, bs = _params(bias, x, x.shape[0], "bias")
-    lib = _lib
-    block, at, nbytes = _workspace(lib, norm, 0, x)
-    mean = rstd = None
+    block, at, nbytes = _workspace(norm, 0, x)
+    y = _output(x, out)
+    w, ws = _params(weight, x, "weight")
+    b, bs = _params(bias, x, "bias")
+    mean = rstd = m = r = None
     if stats:
-        mean, rstd = torch.empty((2,) + tuple(x.shape[:-2]) + (groups,), dtype=torch.float32, device=x.device)
-    with _OnDevice(x) as st:
-        rc = lib.kavg_group_norm(norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), mean.data_ptr() if stats else None,
-                                 rstd.data_ptr() if stats else None, at, nbytes, st)
-    _done(rc, "kavg_group_norm")
+        mean, rstd = torch.empty((2,) + x.shape[:-2] + (groups,), dtype=torch.float32, device=x.device)
+        m, r = mean.data_ptr(), rstd.data_ptr()
+    _call("kavg_group_norm", x, _lib.kavg_group_norm, norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), m, r, at, nbytes)
     return (y, mean, rstd) if stats else y
 
 
@@ -300,45 +299,38 @@ def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation
     """Gradients of kavg_group_norm (same options; mean, rstd as it returned them): dx (out, if given: dy itself among
     others), dweight, dbias (float32, [sets, channels] or [channels]; written into the tensors given, which may lie in a
     learner's gradient vector; None where weight, bias are None)."""
-    torch = _torch()
-    _activations(x, "x", (3, 4))
-    _like(dy, x, "dy")
+    torch = _torch_module or _torch()
     norm = _norm(x, groups, 1.0, activation, drop, seed, site)       # (eps went into rstd)
-    lib = _lib
-    block, at, nbytes = _workspace(lib, norm, 1, x)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
-    sets = x.shape[0]
+    block, at, nbytes = _workspace(norm, 1, x)
+    _like(dy, x, "dy")
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous() or tuple(t.shape) != tuple(x.shape[:-2]) + (groups,):
+        if t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous() or t.shape != x.shape[:-2] + (groups,):
             _bad("%s is not what kavg_group_norm returned" % name)
-    w, ws = _params(weight, x, sets, "weight")
-    b, bs = _params(bias, x, sets, "bias")
+    dx = _output(x, out)
+    w, ws = _params(weight, x, "weight")
+    b, bs = _params(bias, x, "bias")
     if dweight is None and weight is not None:
         dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
     if dbias is None and bias is not None:
         dbias = torch.empty(bias.shape, dtype=torch.float32, device=x.device)
-    gw, gws = _params(dweight, x, sets, "dweight")
-    gb, gbs = _params(dbias, x, sets, "dbias")
-    with _OnDevice(x) as st:
-        rc = lib.kavg_group_norm_backward(norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(), rstd.data_ptr(), w, ws, b, bs,
-                                          _images(dx, "out"), gw, gws, gb, gbs, at, nbytes, st)
-    _done(rc, "kavg_group_norm_backward")
+    gw, gws = _params(dweight, x, "dweight")
+    gb, gbs = _params(dbias, x, "dbias")
+    _call("kavg_group_norm_backward", x, _lib.kavg_group_norm_backward, norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(),
+          rstd.data_ptr(), w, ws, b, bs, _images(dx, "out"), gw, gws, gb, gbs, at, nbytes)
     return dx, dweight, dbias
 
 
 def _rows(x, name):
     """(rows, columns, row stride) of a tensor whose last dimension lies together and whose others are evenly spaced rows."""
     shape, st = x.shape, x.stride()
-    if x.dim() == 0:
-        return 1, 1, 1
-    cols, rows = shape[-1], 1
+    cols = shape[-1] if shape else 1
+    if x.numel() == 0:
+        return 0, 1, 1
     if x.is_contiguous():
-        return (x.numel() // cols if cols else 0), max(cols, 1), max(cols, 1)
-    if cols == 0 or x.numel() == 0:
-        return 0, max(cols, 1), max(cols, 1)
+        return x.numel() // cols, cols, cols
     if st[-1] != 1 and cols > 1:
         _bad("%s has a last stride of %d" % (name, st[-1]))
-    stride = None
+    rows, stride = 1, None
     for d in range(x.dim() - 2, -1, -1):
         if shape[d] == 1:
             continue
@@ -350,41 +342,38 @@ def _rows(x, name):
     return rows, cols, cols if stride is None else stride
 
 
-def _dropout(name, x, drop, seed, site, residual, out):
-    torch = _torch()
-    _activations(x, "dy" if residual is _NO_RESIDUAL else "x", range(0, 65))
-    if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 24:
+def _counters_ok(seed, site):
+    if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 24:           # (ctypes would wrap them)
         _bad("seed %d, site %d" % (seed, site))
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, x, "out")
-    rows, cols, xs = _rows(x, "x")
-    ys = _rows(y, "out")[2]
-    dtype = 1 if x.dtype is torch.bfloat16 else 0
-    try:
-        with _OnDevice(x) as st:
-            if residual is _NO_RESIDUAL:
-                rc = _lib.kavg_dropout_backward(x.data_ptr(), xs, y.data_ptr(), ys, rows, cols, dtype, drop, seed, site, st)
-            else:
-                at, rs = (None, 0) if residual is None else (_like(residual, x, "residual").data_ptr(), _rows(residual, "residual")[2])
-                rc = _lib.kavg_dropout(x.data_ptr(), xs, at, rs, y.data_ptr(), ys, rows, cols, dtype, drop, seed, site, st)
-    except ctypes.ArgumentError as e:
-        _bad(str(e))
-    _done(rc, name)
-    return y
-
-
-_NO_RESIDUAL = object()
 
 
 def kavg_dropout(x, drop, seed, site=0, residual=None, out=None):
     """Dropout of a float32 or bfloat16 tensor in evenly spaced rows (contiguous, or slices of the last dimension), plus a
     residual of the same shape.  The mask is that of (drop, seed, site) and of an element's number in row-major order; it is
     not stored.  out: x or the residual among others."""
-    return _dropout("kavg_dropout", x, drop, seed, site, residual, out)
+    _torch_module or _torch()
+    dtype = _dtype(x, "x")
+    _counters_ok(seed, site)
+    y = _output(x, out)
+    rows, cols, xs = _rows(x, "x")
+    at = rs = None
+    if residual is not None:
+        at, rs = _like(residual, x, "residual").data_ptr(), _rows(residual, "residual")[2]
+    _call("kavg_dropout", x, _lib.kavg_dropout, x.data_ptr(), xs, at, rs or 0, y.data_ptr(), _rows(y, "out")[2], rows, cols, dtype, drop, seed,
+          site)
+    return y
 
 
 def kavg_dropout_backward(dy, drop, seed, site=0, out=None):
     """Gradient of kavg_dropout with respect to x (that with respect to the residual is dy)."""
-    return _dropout("kavg_dropout_backward", dy, drop, seed, site, _NO_RESIDUAL, out)
+    _torch_module or _torch()
+    dtype = _dtype(dy, "dy")
+    _counters_ok(seed, site)
+    dx = _output(dy, out)
+    rows, cols, stride = _rows(dy, "dy")
+    _call("kavg_dropout_backward", dy, _lib.kavg_dropout_backward, dy.data_ptr(), stride, dx.data_ptr(), _rows(dx, "out")[2], rows, cols, dtype,
+          drop, seed, site)
+    return dx
 
 
 class MAvg:
