@@ -5,6 +5,7 @@
 //     dbias_c = sum dz,  dweight_c = sum dz xh  (over a learner's images and positions),
 //     dx = r (h - mean h - xh mean(h xh))       (means over the group).
 // Statistics and sums are fp32; the variance is taken about the mean, in a second sum.
+#include "norm_backward.h"
 #include "norm_forward.h"
 #include "wave_sum.h"
 
@@ -65,7 +66,7 @@ __device__ __forceinline__ float grad_z(const NormCall& c, float dy, float z, ui
 
 // dx: one workgroup per group
 template <class E, int ACT>
-__global__ void __launch_bounds__(T) norm_backward_kernel(NormCall c) {
+__global__ void __launch_bounds__(T) norm_wide_backward_kernel(NormCall c) {
     __shared__ float lds[4];
     const Group at = group_of_block(c);
     const int D = c.channels / c.groups, c0 = at.group * D;
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(T) norm_backward_kernel(NormCall c) {
 
 // dweight, dbias: one workgroup per learner and channel
 template <class E, int ACT>
-__global__ void __launch_bounds__(T) norm_param_kernel(NormCall c) {
+__global__ void __launch_bounds__(T) norm_wide_param_kernel(NormCall c) {
     __shared__ float lds[4];
     const int64_t j = blockIdx.x / c.channels;
     const int ch = (int)(blockIdx.x % c.channels), g = ch / (c.channels / c.groups);
@@ -118,15 +119,28 @@ __global__ void __launch_bounds__(T) norm_param_kernel(NormCall c) {
 }
 
 template <class E, int ACT>
-hipError_t backward(const NormCall& c, hipStream_t st) {
+hipError_t wide_backward(const NormCall& c, hipStream_t st) {
     const int64_t params = c.sets * c.channels, groups = c.sets * c.images * c.groups;
-    if (params && (c.dweight || c.dbias)) norm_param_kernel<E, ACT><<<dim3((unsigned)params), dim3(T), 0, st>>>(c);   // (before dx, which may be dy)
+    if (c.dweight || c.dbias) norm_wide_param_kernel<E, ACT><<<dim3((unsigned)params), dim3(T), 0, st>>>(c);   // (before dx, which may be dy)
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && groups && c.positions) {
-        norm_backward_kernel<E, ACT><<<dim3((unsigned)groups), dim3(T), 0, st>>>(c);
+        norm_wide_backward_kernel<E, ACT><<<dim3((unsigned)groups), dim3(T), 0, st>>>(c);
         e = hipGetLastError();
     }
     return e;
+}
+
+template <class E>
+hipError_t backward(const NormCall& c, void* workspace, hipStream_t st) {
+    if (!c.sets) return hipSuccess;
+    Tile t;
+    const bool contiguous = c.xs.row == c.channels && c.dys.row == c.channels && c.outs.row == c.channels;
+    if (c.images && c.positions && norm_tile(c, contiguous, true, &t)) return tiled_backward<E>(c, t, workspace, st);
+    switch (c.activation) {
+        case KAVG_ACT_RELU: return wide_backward<E, KAVG_ACT_RELU>(c, st);
+        case KAVG_ACT_SILU: return wide_backward<E, KAVG_ACT_SILU>(c, st);
+        default: return wide_backward<E, KAVG_ACT_NONE>(c, st);
+    }
 }
 
 template <class E>
@@ -151,13 +165,8 @@ hipError_t launch_group_norm(const NormCall& c, void* workspace, hipStream_t st)
     return c.dtype == KAVG_BF16 ? forward<__bf16>(c, workspace, st) : forward<float>(c, workspace, st);
 }
 
-hipError_t launch_group_norm_backward(const NormCall& c, hipStream_t st) {
-    const bool b = c.dtype == KAVG_BF16;
-    switch (c.activation) {
-        case KAVG_ACT_RELU: return b ? backward<__bf16, KAVG_ACT_RELU>(c, st) : backward<float, KAVG_ACT_RELU>(c, st);
-        case KAVG_ACT_SILU: return b ? backward<__bf16, KAVG_ACT_SILU>(c, st) : backward<float, KAVG_ACT_SILU>(c, st);
-        default: return b ? backward<__bf16, KAVG_ACT_NONE>(c, st) : backward<float, KAVG_ACT_NONE>(c, st);
-    }
+hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, hipStream_t st) {
+    return c.dtype == KAVG_BF16 ? backward<__bf16>(c, workspace, st) : backward<float>(c, workspace, st);
 }
 
 }  // namespace kavg

@@ -34,7 +34,7 @@ struct NormCall {
 
 size_t norm_workspace(const NormCall& c, bool backward);
 hipError_t launch_group_norm(const NormCall& c, void* workspace, hipStream_t st);
-hipError_t launch_group_norm_backward(const NormCall& c, hipStream_t st);
+hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, hipStream_t st);
 
 struct DropCall {
     int dtype;

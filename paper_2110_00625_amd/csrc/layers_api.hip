@@ -122,7 +122,7 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
     c.mean = const_cast<float*>(mean); c.rstd = const_cast<float*>(rstd);
     c.dweight = dweight; c.dweight_stride = dweight_stride;
     c.dbias = dbias; c.dbias_stride = dbias_stride;
-    return status(launch_group_norm_backward(c, (hipStream_t)hip_stream));
+    return status(launch_group_norm_backward(c, workspace, (hipStream_t)hip_stream));
 }
 
 int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride, int64_t rows,

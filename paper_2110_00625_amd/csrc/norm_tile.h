@@ -29,6 +29,7 @@ struct Tile {
 };
 
 constexpr int FLAT_PACKS = 8;    // the most packs per lane of a flat tile (its sums are per channel, and its last pack needs care: more spill)
+constexpr int BACKWARD_PACKS = 4;   // of the backward pass, which holds x and dz (in fp32) of each
 enum { TILE_WHOLE = 0, TILE_SUMS = 1, TILE_APPLY = 2 };      // sums and results; sums alone (chunks); results from finished sums
 
 // false: no tile fits (groups too wide for a workgroup)

@@ -104,13 +104,13 @@ bool flat_tile(const NormCall& c, int vec, int most, bool backward, Tile* t) {
 size_t bytes_of(const NormCall& c, const Tile& t, bool backward) {
     const size_t images = (size_t)(c.sets * c.images), groups = images * c.groups;
     if (!backward) return t.chunks == 1 ? 0 : (2 * groups * t.chunks + 2 * groups) * sizeof(float);
-    return 0;
+    return (images * t.chunks * 2 * c.channels + (t.chunks == 1 ? 0 : 2 * groups)) * sizeof(float);
 }
 
 }  // namespace
 
 bool norm_tile(const NormCall& c, bool contiguous, bool backward, Tile* t) {
-    const int elem = c.dtype == KAVG_BF16 ? 2 : 4, vec = 16 / elem, most = backward ? 4 : 16;
+    const int elem = c.dtype == KAVG_BF16 ? 2 : 4, vec = 16 / elem, most = backward ? BACKWARD_PACKS : 16;
     if (c.channels % vec == 0) return rows_tile(c, vec, elem, most, backward, t);
     if (contiguous && flat_tile(c, vec, std::min(most, FLAT_PACKS), backward, t)) return true;
     return rows_tile(c, 1, elem, most, backward, t);
