@@ -54,8 +54,8 @@ __device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first,
     for (int u = 0; u < U; ++u) {
         float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = to_float(xv[u][i]);
-        if (c.drop.threshold) drop_apply<V, ALIGNED>(c.drop, row[u] * c.cols + col[u], v);
+        for (int i = 0; i < V; ++i) v[i] = to_float(xv[u][i]) * c.drop.scale;
+        if (c.drop.threshold) drop_mask<V, ALIGNED>(c.drop, row[u] * c.cols + col[u], v);
         pack o;
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = from_float<E>(RESIDUAL ? v[i] + to_float(rv[u][i]) : v[i]);

@@ -62,11 +62,12 @@ template <class E, int V> struct Pack {
 template <class E, int V> __device__ __forceinline__ typename Pack<E, V>::type pack_load(const E* p) { return *(const typename Pack<E, V>::loose*)p; }
 template <class E, int V> __device__ __forceinline__ void pack_store(E* p, typename Pack<E, V>::type v) { *(typename Pack<E, V>::loose*)p = v; }
 
-// v[i] = keep ? v[i] * scale : 0 for elements e .. e+V-1.  V a multiple of 4: a draw serves four of them; where e is no multiple of 4
-// (ALIGNED false) they straddle one draw more.  A field is compared in the upper half of a word, with the bits below it left where they
-// are: field >= T if the word exceeds (T - 1) 2^16 + 65535 (threshold 1..65536).
-template <int V, bool ALIGNED> __device__ __forceinline__ void drop_apply(const DropRule& d, uint64_t e, float (&v)[V]) {
-    const uint32_t below = ((d.threshold - 1) << 16) | 0xFFFF;
+// v[i] = keep ? v[i] : 0 for elements e .. e+V-1.  V a multiple of 4: a draw serves four of them; where e is no multiple of 4
+// (ALIGNED false) they straddle one draw more.  field >= T is field > T - 1 (threshold 1..65536): 16-bit comparisons for the lower
+// halves of a draw's words, for the upper ones the word against (T - 1) 2^16 + 65535, so that no field is moved.
+template <int V, bool ALIGNED> __device__ __forceinline__ void drop_mask(const DropRule& d, uint64_t e, float (&v)[V]) {
+    const uint16_t low = (uint16_t)(d.threshold - 1);
+    const uint32_t high = ((d.threshold - 1) << 16) | 0xFFFF;
     uint64_t state = d.base + (e >> 2) * SPLITMIX_GAMMA;
     uint64_t word = splitmix64_mix(state);
     const int shift = 16 * (int)(e & 3);
@@ -79,10 +80,10 @@ template <int V, bool ALIGNED> __device__ __forceinline__ void drop_apply(const 
             if (!ALIGNED && shift) fields = (fields >> shift) | (word << (64 - shift));
         }
         const uint32_t lo = (uint32_t)fields, hi = (uint32_t)(fields >> 32);
-        v[i] = lo << 16 > below ? v[i] * d.scale : 0.f;
-        v[i + 1] = lo > below ? v[i + 1] * d.scale : 0.f;
-        v[i + 2] = hi << 16 > below ? v[i + 2] * d.scale : 0.f;
-        v[i + 3] = hi > below ? v[i + 3] * d.scale : 0.f;
+        v[i] = (uint16_t)lo > low ? v[i] : 0.f;
+        v[i + 1] = lo > high ? v[i + 1] : 0.f;
+        v[i + 2] = (uint16_t)hi > low ? v[i + 2] : 0.f;
+        v[i + 3] = hi > high ? v[i + 3] : 0.f;
     }
 }
 
@@ -95,7 +96,7 @@ template <class E> __device__ __forceinline__ E from_float(float v) { return (E)
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
 template <int ACT> __device__ __forceinline__ float activate(float z) {
-    if (ACT == KAVG_ACT_RELU) return z < 0.f ? 0.f : z;             // (NaN stays)
+    if (ACT == KAVG_ACT_RELU) return __builtin_elementwise_maximum(z, 0.f);      // (NaN stays)
     if (ACT == KAVG_ACT_SILU) return z * sigmoid(z);
     return z;
 }

@@ -1,6 +1,7 @@
 // Backward pass of the group norm on tiles in registers (norm_tile.h).  With da = drop(dy), dz = da act'(z), z = weight_c xh + bias_c:
 //     dbias_c = sum dz,  dweight_c = sum dz xh  over a learner's images and positions,
 //     dx = r (weight_c dz - A - xh B),  A = mean weight_c dz,  B = mean weight_c dz xh  over the group.
+// Everything is linear in dz: drop's scale and r (xh = (x - m) r) are applied to sums and parameters, not to elements.
 // Both pairs come from the same sums, of dz and dz xh per channel of an image: they are taken once, the group's are the sum over its
 // channels times their weights, and the parameters' the sum over images, by a kernel of its own (norm_param_kernel), in a fixed order.
 // x and dz stay in registers between the sums and dx, so that x and dy are read once.  An image that one workgroup cannot hold is read
@@ -45,14 +46,8 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
             gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
         }
     }
-    float w[V], b[V], mean[A], rstd[A];
+    float w[V], b[V], mean[A], rstd[A];              // (w: weight_c r)
     int group[A];                                    // in the tile
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int ch = l.channel(c, i);
-        w[i] = c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f;
-        b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
-    }
     // (a lane without work, whose group may not exist, looks at the first one)
     const int64_t first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
 #pragma unroll
@@ -61,18 +56,24 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
         mean[a] = c.mean[first_group + group[a]];
         rstd[a] = c.rstd[first_group + group[a]];
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int ch = l.channel(c, i);
+        w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[WHOLE_PACK ? 0 : i];
+        b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
+    }
     const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
-    // dz of pack k, and of its elements xh
-    const auto gradient = [&](int k, float (&xh)[V], float (&d)[V]) {
+    // of pack k: x - m, and dz without drop's scale
+    const auto gradient = [&](int k, float (&d)[V], float (&g)[V]) {
         float z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            xh[i] = (to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]) * rstd[WHOLE_PACK ? 0 : i];
-            z[i] = xh[i] * w[i] + b[i];
-            d[i] = to_float(gv[k][i]);
+            d[i] = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i];
+            z[i] = d[i] * w[i] + b[i];
+            g[i] = to_float(gv[k][i]);
         }
-        if (c.drop.threshold) tile_drop<V, FLAT>(c.drop, l.run, number + k * number_step, d);
-        slopes<V>(c.activation, z, d);
+        if (c.drop.threshold) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, g);
+        slopes<V>(c.activation, z, g);
     };
 
     float dz[MODE == TILE_WHOLE ? NV : 1][V];
@@ -83,15 +84,15 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
         for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float xh[V], (&d)[V] = dz[MODE == TILE_WHOLE ? k : 0];
-            gradient(k, xh, d);
+            float d[V], (&g)[V] = dz[MODE == TILE_WHOLE ? k : 0];
+            gradient(k, d, g);
             const int n = l.valid(t, k);
             if (n == V) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) { s0[i] += d[i]; s1[i] += d[i] * xh[i]; }
+                for (int i = 0; i < V; ++i) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
             } else if (FLAT && n) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) if (i < n) { s0[i] += d[i]; s1[i] += d[i] * xh[i]; }
+                for (int i = 0; i < V; ++i) if (i < n) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
             }
             keep_packed(xv[k]);
         }
@@ -106,7 +107,10 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
         float* g0 = c1 + sums;                       // [unit][group]
         float* g1 = g0 + t.units * t.groups;
 #pragma unroll
-        for (int i = 0; i < V; ++i) { p0[threadIdx.x * V + i] = l.on ? s0[i] : 0.f; p1[threadIdx.x * V + i] = l.on ? s1[i] : 0.f; }
+        for (int i = 0; i < V; ++i) {
+            p0[threadIdx.x * V + i] = l.on ? s0[i] * c.drop.scale : 0.f;
+            p1[threadIdx.x * V + i] = l.on ? s1[i] * (c.drop.scale * rstd[WHOLE_PACK ? 0 : i]) : 0.f;
+        }
         __syncthreads();
         const int shares = sums >= threads ? 1 : places < threads / sums ? places : threads / sums;
         for (int s = threadIdx.x; s < sums * shares; s += threads) {
@@ -168,14 +172,16 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     }
     const Place<V, FLAT> to(c, t, l, c.outs);
 #pragma unroll
+    for (int a = 0; a < A; ++a) gB[a] *= rstd[a];
+#pragma unroll
     for (int k = 0; k < NV; ++k) {
-        float v[V], xh[V];
-        if (MODE == TILE_APPLY) gradient(k, xh, v);
+        float v[V], d[V];
+        if (MODE == TILE_APPLY) gradient(k, d, v);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int a = WHOLE_PACK ? 0 : i;
-            if (MODE == TILE_WHOLE) { v[i] = dz[k][i]; xh[i] = (to_float(xv[k][i]) - mean[a]) * rstd[a]; }
-            v[i] = v[i] * (w[i] * rstd[a]) - gA[a] - xh[i] * gB[a];
+            if (MODE == TILE_WHOLE) { v[i] = dz[k][i]; d[i] = to_float(xv[k][i]) - mean[a]; }
+            v[i] = v[i] * (w[i] * c.drop.scale) - gA[a] - d[i] * gB[a];
         }
         tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
     }

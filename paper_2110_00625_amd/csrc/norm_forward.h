@@ -58,7 +58,8 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int n = l.valid(t, k);
-            if (n == V) {
+            if (WHOLE_PACK) { if (n) sum[0] = pack_sum<V>(xv[k], sum[0]); }
+            else if (n == V) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += to_float(xv[k][i]);
             } else if (FLAT && n) {
@@ -144,6 +145,11 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] *= rstd[WHOLE_PACK ? 0 : i];
+    // drop's scale commutes with ReLU
+    if (c.activation != KAVG_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { w[i] *= c.drop.scale; b[i] *= c.drop.scale; }
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         float v[V];
@@ -151,12 +157,12 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
         for (int i = 0; i < V; ++i) v[i] = (to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]) * w[i] + b[i];
         if (c.activation == KAVG_ACT_SILU) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activate<KAVG_ACT_SILU>(v[i]);
+            for (int i = 0; i < V; ++i) v[i] = activate<KAVG_ACT_SILU>(v[i]) * c.drop.scale;
         } else if (c.activation == KAVG_ACT_RELU) {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = activate<KAVG_ACT_RELU>(v[i]);
         }
-        if (c.drop.threshold) tile_drop<V, FLAT>(c.drop, l.run, number + k * number_step, v);
+        if (c.drop.threshold) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, v);
         tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
     }
 }

@@ -151,11 +151,29 @@ template <class P> __device__ __forceinline__ void keep_packed(P& v) {
     }
 }
 
-// v = elements from number e on, dropped.  (Rows: V = 4, 8 divides the channels, so e is a multiple of 4; flat: images of a multiple of 4 elements)
-template <int V, bool FLAT> __device__ __forceinline__ void tile_drop(const DropRule& d, int64_t run, uint64_t e, float (&v)[V]) {
-    if constexpr (V == 1) v[0] = drop_keeps(d, e) ? v[0] * d.scale : 0.f;
-    else if (!FLAT || run % 4 == 0) drop_apply<V, true>(d, e, v);
-    else drop_apply<V, false>(d, e, v);
+// v = elements from number e on, 0 where they are dropped.  (Rows: V = 4, 8 divides the channels, so e is a multiple of 4; flat: images of a
+// multiple of 4 elements)
+template <int V, bool FLAT> __device__ __forceinline__ void tile_mask(const DropRule& d, int64_t run, uint64_t e, float (&v)[V]) {
+    if constexpr (V == 1) v[0] = drop_keeps(d, e) ? v[0] : 0.f;
+    else if (!FLAT || run % 4 == 0) drop_mask<V, true>(d, e, v);
+    else drop_mask<V, false>(d, e, v);
+}
+
+// sum + the elements of a pack, in bf16 two at a time (exact products with one, fp32 sums)
+template <int V> __device__ __forceinline__ float pack_sum(typename Pack<float, V>::type v, float sum) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum += v[i];
+    return sum;
+}
+template <int V> __device__ __forceinline__ float pack_sum(typename Pack<__bf16, V>::type v, float sum) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    if constexpr (V == 1) return sum + (float)v[0];
+    else {
+        const pair ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+        for (int i = 0; i < V; i += 2) { const pair p = {v[i], v[i + 1]}; sum = __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false); }
+        return sum;
+    }
 }
 
 __device__ __forceinline__ float team_sum(float v, int team) {

@@ -26,13 +26,13 @@ bool finish(Tile* t, const NormCall& c, bool backward) {
     return t->lds <= 160 * 1024;
 }
 
-// packs per lane: the most of 1, 2, 4, .. `most` that leave lanes enough to fill the device, but at least what brings an image (lanes_of
-// packs) into a workgroup; 0: it does not fit
-template <class LanesOf> int packs_per_lane(int most, int64_t tiles, LanesOf lanes_of) {
+// Packs per lane: the fewest of 1, 2, 4, .. `most` that bring an image (lanes_of packs) into a workgroup of at most `lanes`, 0 if none does;
+// more of them where workgroups are plenty even so.
+template <class LanesOf> int packs_per_lane(int most, int lanes, int64_t tiles, LanesOf lanes_of) {
     int nv = 1;
-    while (nv <= most && lanes_of(nv) > MOST_LANES) nv *= 2;
+    while (nv <= most && lanes_of(nv) > lanes) nv *= 2;
     if (nv > most) return 0;
-    while (nv < most && nv < 8 && tiles * lanes_of(2 * nv) >= FULL) nv *= 2;
+    while (nv < most && tiles * lanes_of(2 * nv) >= FULL) nv *= 2;
     return nv;
 }
 
@@ -45,32 +45,30 @@ bool rows_tile(const NormCall& c, int vec, int elem, int most, bool backward, Ti
     t->vec = vec;
     t->whole_pack = D % vec == 0;
     t->rows = (int)c.positions;
-    // segments of 128 bytes of a row, or of 64 where only these bring an image into a workgroup
-    for (int64_t segment = 128; ; segment /= 2) {
-        int64_t blocks = up(pieces, std::max<int64_t>(1, segment / (elem * least)));
-        const int64_t per = up(pieces, blocks);
-        blocks = up(pieces, per);
+    // tiles of rows' segments of so many bytes, or of a piece if that is more
+    const auto cut = [&](int64_t segment) {
+        const int64_t blocks = up(pieces, std::max<int64_t>(1, segment / (elem * least))), per = up(pieces, blocks);
         t->channels = (int)(per * least);
         t->cols = t->channels / vec;
         t->groups = t->channels / D;
-        t->blocks = (int)blocks;
-        if (t->cols > MOST_LANES / 2) { if (segment < 32) return false; continue; }
-        t->nv = packs_per_lane(most, images * blocks, [&](int nv) { return t->cols * up(c.positions, nv); });
-        if (t->nv || segment < 64 || per == 1) break;
+        t->blocks = (int)up(pieces, per);
+    };
+    t->nv = 0;
+    for (const int lanes : {MOST_LANES / 2, MOST_LANES}) {
+        for (int64_t segment = 128; segment >= 32 && !t->nv; segment /= 2) {
+            cut(segment);
+            t->nv = packs_per_lane(most, lanes, images * t->blocks, [&](int nv) { return t->cols * up(c.positions, nv); });
+        }
+        if (t->nv) break;
     }
     if (t->nv) {
         t->lane_rows = (int)up(c.positions, t->nv);
         t->chunks = 1;
         t->units = (int)std::max<int64_t>(1, std::min<int64_t>(images, 256 / (t->cols * t->lane_rows)));
     } else {
-        // cut along the positions, 512 lanes to a workgroup; whole lines again
-        const int64_t blocks = up(pieces, std::max<int64_t>(1, 128 / (elem * least))), per = up(pieces, blocks);
-        t->channels = (int)(per * least);
-        t->cols = t->channels / vec;
-        t->groups = t->channels / D;
-        t->blocks = (int)up(pieces, per);
+        cut(128);
         t->nv = most;
-        t->lane_rows = std::max(1, 512 / t->cols);
+        t->lane_rows = std::max(1, MOST_LANES / 2 / t->cols);
         t->chunks = (int)up(c.positions, (int64_t)t->nv * t->lane_rows);
         t->units = 1;
     }
@@ -90,8 +88,9 @@ bool flat_tile(const NormCall& c, int vec, int most, bool backward, Tile* t) {
     t->blocks = 1;
     t->lane_rows = 1;
     const auto lanes = [&](int nv) { return up(up(packs, nv), period) * period; };
-    t->nv = packs_per_lane(most, images, lanes);
-    t->cols = (int)(t->nv ? lanes(t->nv) : std::max(1, 512 / period) * period);
+    t->nv = packs_per_lane(most, MOST_LANES / 2, images, lanes);
+    if (!t->nv) t->nv = packs_per_lane(most, MOST_LANES, images, lanes);
+    t->cols = (int)(t->nv ? lanes(t->nv) : std::max(1, MOST_LANES / 2 / period) * period);
     if (!t->nv) t->nv = most;
     const int64_t rows = up(packs, t->cols);
     if (rows > (int64_t)1 << 30) return false;
