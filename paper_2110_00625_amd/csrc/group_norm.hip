@@ -5,8 +5,7 @@
 //     dbias_c = sum dz,  dweight_c = sum dz xh  (over a learner's images and positions),
 //     dx = r (h - mean h - xh mean(h xh))       (means over the group).
 // Statistics and sums are fp32; the variance is taken about the mean, in a second sum.
-#include "norm_backward.h"
-#include "norm_forward.h"
+#include "norm_tile.h"
 #include "wave_sum.h"
 
 namespace kavg {
@@ -31,7 +30,7 @@ __device__ __forceinline__ Group group_of_block(const NormCall& c) {
 }
 
 // one workgroup per group
-template <class E, int ACT>
+template <class E, bool SILU>
 __global__ void __launch_bounds__(T) norm_wide_forward_kernel(NormCall c) {
     __shared__ float lds[4];
     const Group at = group_of_block(c);
@@ -52,20 +51,20 @@ __global__ void __launch_bounds__(T) norm_wide_forward_kernel(NormCall c) {
         const int d = (int)(i % D), ch = c0 + d;
         const float xh = (to_float(x[s * c.xs.row + d]) - mean) * rstd;
         const float z = xh * (c.weight ? c.weight[at.set * c.weight_stride + ch] : 1.f) + (c.bias ? c.bias[at.set * c.bias_stride + ch] : 0.f);
-        float a = activate<ACT>(z);
+        float a = activate<SILU>(z, c.floor);
         if (c.drop.threshold) a = drop_keeps(c.drop, first + (uint64_t)s * c.channels + d) ? a * c.drop.scale : 0.f;
         y[s * c.outs.row + d] = from_float<E>(a);
     }
 }
 
-template <class E, int ACT>
+template <class E, bool SILU>
 __device__ __forceinline__ float grad_z(const NormCall& c, float dy, float z, uint64_t e) {
     if (c.drop.threshold) dy = drop_keeps(c.drop, e) ? dy * c.drop.scale : 0.f;
-    return dy * activate_slope<ACT>(z);
+    return through_slope<SILU>(dy, z, c.floor);
 }
 
 // dx: one workgroup per group
-template <class E, int ACT>
+template <class E, bool SILU>
 __global__ void __launch_bounds__(T) norm_wide_backward_kernel(NormCall c) {
     __shared__ float lds[4];
     const Group at = group_of_block(c);
@@ -84,7 +83,7 @@ __global__ void __launch_bounds__(T) norm_wide_backward_kernel(NormCall c) {
             const float w = c.weight ? c.weight[at.set * c.weight_stride + ch] : 1.f;
             const float xh = (to_float(x[s * c.xs.row + d]) - mean) * rstd;
             const float z = xh * w + (c.bias ? c.bias[at.set * c.bias_stride + ch] : 0.f);
-            const float h = w * grad_z<E, ACT>(c, to_float(dy[s * c.dys.row + d]), z, first + (uint64_t)s * c.channels + d);
+            const float h = w * grad_z<E, SILU>(c, to_float(dy[s * c.dys.row + d]), z, first + (uint64_t)s * c.channels + d);
             if (pass == 0) { sh += h; shx += h * xh; }
             else dx[s * c.outs.row + d] = from_float<E>(rstd * (h - sh - xh * shx));
         }
@@ -93,7 +92,7 @@ __global__ void __launch_bounds__(T) norm_wide_backward_kernel(NormCall c) {
 }
 
 // dweight, dbias: one workgroup per learner and channel
-template <class E, int ACT>
+template <class E, bool SILU>
 __global__ void __launch_bounds__(T) norm_wide_param_kernel(NormCall c) {
     __shared__ float lds[4];
     const int64_t j = blockIdx.x / c.channels;
@@ -106,7 +105,7 @@ __global__ void __launch_bounds__(T) norm_wide_param_kernel(NormCall c) {
         const int64_t i = r / c.positions, s = r % c.positions, stat = (j * c.images + i) * c.groups + g;
         const float xh = (to_float(x[i * c.xs.image + s * c.xs.row]) - c.mean[stat]) * c.rstd[stat];
         const uint64_t e = (uint64_t)((j * c.images + i) * c.positions + s) * c.channels + ch;
-        const float dz = grad_z<E, ACT>(c, to_float(dy[i * c.dys.image + s * c.dys.row]), xh * w + b, e);
+        const float dz = grad_z<E, SILU>(c, to_float(dy[i * c.dys.image + s * c.dys.row]), xh * w + b, e);
         sz += dz;
         szx += dz * xh;
     }
@@ -118,13 +117,13 @@ __global__ void __launch_bounds__(T) norm_wide_param_kernel(NormCall c) {
     }
 }
 
-template <class E, int ACT>
+template <class E, bool SILU>
 hipError_t wide_backward(const NormCall& c, hipStream_t st) {
     const int64_t params = c.sets * c.channels, groups = c.sets * c.images * c.groups;
-    if (c.dweight || c.dbias) norm_wide_param_kernel<E, ACT><<<dim3((unsigned)params), dim3(T), 0, st>>>(c);   // (before dx, which may be dy)
+    if (c.dweight || c.dbias) norm_wide_param_kernel<E, SILU><<<dim3((unsigned)params), dim3(T), 0, st>>>(c);   // (before dx, which may be dy)
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && groups && c.positions) {
-        norm_wide_backward_kernel<E, ACT><<<dim3((unsigned)groups), dim3(T), 0, st>>>(c);
+        norm_wide_backward_kernel<E, SILU><<<dim3((unsigned)groups), dim3(T), 0, st>>>(c);
         e = hipGetLastError();
     }
     return e;
@@ -133,29 +132,22 @@ hipError_t wide_backward(const NormCall& c, hipStream_t st) {
 template <class E>
 hipError_t backward(const NormCall& c, void* workspace, hipStream_t st) {
     if (!c.sets) return hipSuccess;
-    Tile t;
+    NormTiles t;
     const bool contiguous = c.xs.row == c.channels && c.dys.row == c.channels && c.outs.row == c.channels;
-    if (c.images && c.positions && norm_tile(c, contiguous, true, &t)) return tiled_backward<E>(c, t, workspace, st);
-    switch (c.activation) {
-        case KAVG_ACT_RELU: return wide_backward<E, KAVG_ACT_RELU>(c, st);
-        case KAVG_ACT_SILU: return wide_backward<E, KAVG_ACT_SILU>(c, st);
-        default: return wide_backward<E, KAVG_ACT_NONE>(c, st);
-    }
+    if (c.images && c.positions && norm_tiles(c, contiguous, true, &t)) return tiled_backward<E>(c, t, workspace, st);
+    return c.silu ? wide_backward<E, true>(c, st) : wide_backward<E, false>(c, st);
 }
 
 template <class E>
 hipError_t forward(const NormCall& c, void* workspace, hipStream_t st) {
     const int64_t groups = c.sets * c.images * c.groups;
     if (!groups) return hipSuccess;
-    Tile t;
+    NormTiles t;
     const bool contiguous = c.xs.row == c.channels && c.outs.row == c.channels;
-    if (c.positions && norm_tile(c, contiguous, false, &t)) return tiled_forward<E>(c, t, workspace, st);
+    if (c.positions && norm_tiles(c, contiguous, false, &t)) return tiled_forward<E>(c, t, workspace, st);
     const dim3 grid((unsigned)groups);
-    switch (c.activation) {
-        case KAVG_ACT_RELU: norm_wide_forward_kernel<E, KAVG_ACT_RELU><<<grid, dim3(T), 0, st>>>(c); break;
-        case KAVG_ACT_SILU: norm_wide_forward_kernel<E, KAVG_ACT_SILU><<<grid, dim3(T), 0, st>>>(c); break;
-        default: norm_wide_forward_kernel<E, KAVG_ACT_NONE><<<grid, dim3(T), 0, st>>>(c);
-    }
+    if (c.silu) norm_wide_forward_kernel<E, true><<<grid, dim3(T), 0, st>>>(c);
+    else norm_wide_forward_kernel<E, false><<<grid, dim3(T), 0, st>>>(c);
     return hipGetLastError();
 }
 

@@ -17,7 +17,9 @@ DropRule drop_rule(double drop, uint64_t seed, uint64_t site);
 struct Strides { int64_t set, image, row; };
 
 struct NormCall {
-    int dtype, activation;
+    int dtype;
+    bool silu;                              // else ReLU above `floor` (see activate)
+    float floor;
     int64_t sets, images, positions;
     int channels, groups;
     float eps;
@@ -95,15 +97,14 @@ template <class E> __device__ __forceinline__ E from_float(float v) { return (E)
 // before the exponential, so up to |z| 2^-24 more)
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
-template <int ACT> __device__ __forceinline__ float activate(float z) {
-    if (ACT == KAVG_ACT_RELU) return __builtin_elementwise_maximum(z, 0.f);      // (NaN stays)
-    if (ACT == KAVG_ACT_SILU) return z * sigmoid(z);
-    return z;
+// Activation and slope: SiLU, or ReLU with the floor below which it cuts; none is a floor that nothing is below (forward: -inf, which leaves
+// NaN and -inf what they are; backward: NaN, which compares as false).
+template <bool SILU> __device__ __forceinline__ float activate(float z, float floor) {
+    return SILU ? z * sigmoid(z) : __builtin_elementwise_maximum(z, floor);
 }
-template <int ACT> __device__ __forceinline__ float activate_slope(float z) {
-    if (ACT == KAVG_ACT_RELU) return z <= 0.f ? 0.f : 1.f;
-    if (ACT == KAVG_ACT_SILU) { const float s = sigmoid(z); return s * (1.f + z * (1.f - s)); }
-    return 1.f;
+template <bool SILU> __device__ __forceinline__ float through_slope(float g, float z, float floor) {
+    if (SILU) { const float s = sigmoid(z); return g * (s + z * s * (1.f - s)); }
+    return z <= floor ? 0.f : g;
 }
 #endif
 

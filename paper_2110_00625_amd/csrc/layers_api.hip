@@ -57,10 +57,11 @@ Strides strides_of(const kavg_norm* n, const kavg_images* x) {
     return {n->sets > 1 ? x->set_stride : 0, n->images > 1 ? x->image_stride : 0, n->positions > 1 ? x->row_stride : n->channels};
 }
 
-NormCall call_of(const kavg_norm* n) {
+NormCall call_of(const kavg_norm* n, bool backward) {
     NormCall c = {};
     c.dtype = n->dtype;
-    c.activation = n->activation;
+    c.silu = n->activation == KAVG_ACT_SILU;
+    c.floor = n->activation == KAVG_ACT_RELU ? 0.f : backward ? NAN : -INFINITY;
     c.sets = n->sets;
     c.images = n->images;
     c.positions = n->positions;
@@ -85,7 +86,7 @@ extern "C" {
 
 int kavg_group_norm_workspace(const kavg_norm* norm, int backward, size_t* bytes) {
     if (!norm_ok(norm) || !bytes) return KAVG_EINVAL;
-    *bytes = empty(norm) ? 0 : norm_workspace(call_of(norm), backward != 0);
+    *bytes = empty(norm) ? 0 : norm_workspace(call_of(norm, backward != 0), backward != 0);
     return KAVG_OK;
 }
 
@@ -94,7 +95,7 @@ int kavg_group_norm(const kavg_norm* norm, const kavg_images* x, const float* we
                     void* hip_stream) {
     if (!norm_ok(norm) || !images_ok(norm, x, false) || !images_ok(norm, y, true) || !mean != !rstd) return KAVG_EINVAL;
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
-    NormCall c = call_of(norm);
+    NormCall c = call_of(norm, false);
     if (const int rc = workspace_ok(norm, c, false, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.out = y->data; c.outs = strides_of(norm, y);
@@ -112,7 +113,7 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
     if ((!mean || !rstd) && !empty(norm)) return KAVG_EINVAL;
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
     if (!params_ok(norm, dweight, dweight_stride, true) || !params_ok(norm, dbias, dbias_stride, true)) return KAVG_EINVAL;
-    NormCall c = call_of(norm);
+    NormCall c = call_of(norm, true);
     if (const int rc = workspace_ok(norm, c, true, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.dy = dy->data; c.dys = strides_of(norm, dy);

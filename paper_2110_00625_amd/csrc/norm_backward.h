@@ -16,27 +16,178 @@ struct BackwardCall {
     Tile t;
     int64_t x_extent, dy_extent;
     float* parts;                  // [image][chunk] of (sum dz [channels], sum dz xh [channels])
-    const float* group_sums;       // [image][group] of (A, B): results from finished sums
+    const float* group_sums;       // [image][group] of (A, B): results from finished sums, or null: from the parts of `chunks` chunks
+    int chunks;
+    uint32_t tiles;                // workgroups that write results; those behind them add up the parameters' gradients
+    int param_wide, param_blocks;
 };
 
-template <int V> __device__ __forceinline__ void slopes(int activation, const float (&z)[V], float (&d)[V]) {
-    if (activation == KAVG_ACT_SILU) {
+// What a lane keeps of its channels: m, r, weight_c r, bias_c.
+template <int V, bool FLAT, bool WHOLE_PACK> struct Channels {
+    static constexpr int A = WHOLE_PACK ? 1 : V;
+    float w[V], b[V], mean[A], rstd[A];
+    int group[A];                                    // in the tile
+    int64_t first_group;                             // of the tile (of a lane without work, whose groups may not exist: the first of all)
+    uint64_t number, number_step;
+
+    __device__ __forceinline__ Channels(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) {
+        first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) d[i] *= activate_slope<KAVG_ACT_SILU>(z[i]);
-    } else if (activation == KAVG_ACT_RELU) {
+        for (int a = 0; a < A; ++a) {
+            group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s) : 0;
+            mean[a] = c.mean[first_group + group[a]];
+            rstd[a] = c.rstd[first_group + group[a]];
+        }
 #pragma unroll
-        for (int i = 0; i < V; ++i) d[i] *= activate_slope<KAVG_ACT_RELU>(z[i]);
+        for (int i = 0; i < V; ++i) {
+            const int ch = l.channel(c, i);
+            w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[WHOLE_PACK ? 0 : i];
+            b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
+        }
+        number = l.number(c, t);
+        number_step = l.number_step(c, t);
+    }
+    // of pack k: x - m, and dz without drop's scale
+    template <bool SILU, bool DROP, class P>
+    __device__ __forceinline__ void gradient(const NormCall& c, const Lane<V, FLAT>& l, int k, const P& x, const P& dy, float (&d)[V], float (&g)[V]) const {
+        float z[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            d[i] = to_float(x[i]) - mean[WHOLE_PACK ? 0 : i];
+            z[i] = d[i] * w[i] + b[i];
+            g[i] = to_float(dy[i]);
+        }
+        if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = through_slope<SILU>(g[i], z[i], c.floor);
+    }
+};
+
+// s0 += g, s1 += g d of a pack, n of its elements valid
+template <int V, bool FLAT>
+__device__ __forceinline__ void add_pack(int n, const float (&d)[V], const float (&g)[V], float (&s0)[V], float (&s1)[V]) {
+    if (n == V) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
+    } else if (FLAT && n) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) if (i < n) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
     }
 }
 
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, int MODE>
+// `shares` lanes for each of `sums` sums
+__device__ __forceinline__ int shares_of(int threads, int sums, int terms) { return sums >= threads ? 1 : terms < threads / sums ? terms : threads / sums; }
+
+// LDS of the sums
+struct SumSpace {
+    float *p0, *p1;          // [lane][V]: [unit][place][channel]
+    float *q0, *q1;          // [share][unit][channel]
+    float *c0, *c1;          // [unit][channel]: sums of dz, dz xh
+    float* g0;               // [unit][group]: A, then B
+    __device__ __forceinline__ SumSpace(float* lds, int packs, int sums, int threads) {
+        p0 = lds;
+        p1 = p0 + packs;
+        q0 = p1 + packs;
+        q1 = q0 + threads;
+        c0 = q1 + threads;
+        c1 = c0 + sums;
+        g0 = c1 + sums;
+    }
+};
+
+// sums per channel from `terms` terms each, term(sum, j, &a0, &a1) adding the j-th: into c0, c1 and to done(sum, a0, a1)
+template <class Term, class Done>
+__device__ __forceinline__ void add_up(const SumSpace& s, int sums, int terms, Term term, Done done) {
+    const int threads = blockDim.x, shares = shares_of(threads, sums, terms);
+    if (shares > 1) {
+        for (int i = threadIdx.x; i < sums * shares; i += threads) {
+            const int share = (int)((uint32_t)i / (uint32_t)sums), sum = i - share * sums;
+            float a0 = 0.f, a1 = 0.f;
+            for (int j = share; j < terms; j += shares) term(sum, j, a0, a1);
+            s.q0[i] = a0;
+            s.q1[i] = a1;
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < sums; i += threads) {
+        float a0 = 0.f, a1 = 0.f;
+        if (shares > 1) for (int j = 0; j < shares; ++j) { a0 += s.q0[j * sums + i]; a1 += s.q1[j * sums + i]; }
+        else for (int j = 0; j < terms; ++j) term(i, j, a0, a1);
+        s.c0[i] = a0;
+        s.c1[i] = a1;
+        done(i, a0, a1);
+    }
+}
+
+// the lanes' sums per channel: into LDS and, where wanted, to the parts
+template <int V, bool FLAT, bool WHOLE_PACK>
+__device__ __forceinline__ void channel_sums(const BackwardCall& f, const Lane<V, FLAT>& l, const Channels<V, FLAT, WHOLE_PACK>& h, const SumSpace& s,
+                                             const float (&s0)[V], const float (&s1)[V]) {
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        s.p0[threadIdx.x * V + i] = l.on ? s0[i] * c.drop.scale : 0.f;
+        s.p1[threadIdx.x * V + i] = l.on ? s1[i] * (c.drop.scale * h.rstd[WHOLE_PACK ? 0 : i]) : 0.f;
+    }
+    __syncthreads();
+    const int tc = t.channels, sums = t.units * tc, places = FLAT ? t.cols * V / tc : t.lane_rows, per_unit = t.cols * t.lane_rows * V;
+    const uint32_t image0 = l.image - l.unit, images = (uint32_t)(c.sets * c.images);
+    add_up(s, sums, places,
+           [&](int sum, int j, float& a0, float& a1) {
+               const int unit = t.units > 1 ? sum / tc : 0, at = unit * per_unit + sum - unit * tc + j * tc;
+               a0 += s.p0[at];
+               a1 += s.p1[at];
+           },
+           [&](int sum, float a0, float a1) {
+               const int unit = t.units > 1 ? sum / tc : 0, ch = (int)l.block * tc + sum - unit * tc;
+               if (!f.parts || image0 + unit >= images || ch >= c.channels) return;
+               float* to = f.parts + ((int64_t)(image0 + unit) * t.chunks + l.chunk) * 2 * c.channels + ch;
+               to[0] = a0;
+               to[c.channels] = a1;
+           });
+}
+
+// A and B of the tile's groups from the channels' sums
+template <int V, bool FLAT> __device__ __forceinline__ void group_means(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const SumSpace& s) {
+    const int D = c.channels / c.groups, threads = blockDim.x, groups = t.units * t.groups, team = team_of(threads, groups, D), lane = threadIdx.x % team;
+    const float n = (float)c.positions * (float)D;
+    const uint32_t image0 = l.image - l.unit, images = (uint32_t)(c.sets * c.images);
+    for (int g = threadIdx.x / team; g < groups; g += threads / team) {
+        const int unit = t.units > 1 ? g / t.groups : 0, in = (g - unit * t.groups) * D, ch0 = (int)l.block * t.channels + in;
+        const uint32_t image = image0 + unit;
+        float a0 = 0.f, a1 = 0.f;
+        if (image < images && ch0 < c.channels) {
+            const float* weight = c.weight ? c.weight + (t.units > 1 ? image / (uint32_t)c.images : l.set) * c.weight_stride + ch0 : nullptr;
+            for (int i = lane; i < D; i += team) {
+                const float wi = weight ? weight[i] : 1.f;
+                a0 += wi * s.c0[unit * t.channels + in + i];
+                a1 += wi * s.c1[unit * t.channels + in + i];
+            }
+        }
+        a0 = team_sum(a0, team);
+        a1 = team_sum(a1, team);
+        if (lane == 0) { s.g0[g] = a0 / n; s.g0[groups + g] = a1 / n; }
+    }
+}
+
+// dx of pack k from dz (without scale) and x - m
+template <class E, int V, bool FLAT, bool WHOLE_PACK>
+__device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Channels<V, FLAT, WHOLE_PACK>& h, const Place<V, FLAT>& to, int k,
+                                         const float (&d)[V], float (&g)[V], const float (&rA)[WHOLE_PACK ? 1 : V], const float (&rrB)[WHOLE_PACK ? 1 : V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = g[i] * (h.w[i] * c.drop.scale) - rA[WHOLE_PACK ? 0 : i] - d[i] * rrB[WHOLE_PACK ? 0 : i];
+    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, g);
+}
+
+// images that a workgroup holds
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
 __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     constexpr int A = WHOLE_PACK ? 1 : V;
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t);
-    const int D = c.channels / c.groups, threads = blockDim.x;
     typename Pack<E, V>::type xv[NV], gv[NV];
     {
         const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
@@ -46,147 +197,273 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
             gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
         }
     }
-    float w[V], b[V], mean[A], rstd[A];              // (w: weight_c r)
-    int group[A];                                    // in the tile
-    // (a lane without work, whose group may not exist, looks at the first one)
-    const int64_t first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
+    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    float dz[NV][V], s0[V], s1[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float d[V];
+        h.template gradient<SILU, DROP>(c, l, k, xv[k], gv[k], d, dz[k]);
+        add_pack<V, FLAT>(l.valid(t, k), d, dz[k], s0, s1);
+        keep_packed(xv[k]);
+        __builtin_amdgcn_sched_barrier(0);           // (a pack's registers at a time)
+    }
+    const SumSpace s(lds, blockDim.x * V, t.units * t.channels, blockDim.x);
+    channel_sums(f, l, h, s, s0, s1);
+    __syncthreads();
+    group_means(c, t, l, s);
+    __syncthreads();
+    float rA[A], rrB[A];
 #pragma unroll
     for (int a = 0; a < A; ++a) {
-        group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s) : 0;
-        mean[a] = c.mean[first_group + group[a]];
-        rstd[a] = c.rstd[first_group + group[a]];
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int ch = l.channel(c, i);
-        w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[WHOLE_PACK ? 0 : i];
-        b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
-    }
-    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
-    // of pack k: x - m, and dz without drop's scale
-    const auto gradient = [&](int k, float (&d)[V], float (&g)[V]) {
-        float z[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            d[i] = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i];
-            z[i] = d[i] * w[i] + b[i];
-            g[i] = to_float(gv[k][i]);
-        }
-        if (c.drop.threshold) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, g);
-        slopes<V>(c.activation, z, g);
-    };
-
-    float dz[MODE == TILE_WHOLE ? NV : 1][V];
-    float gA[A], gB[A];                              // r A, r B
-    if (MODE != TILE_APPLY) {
-        float s0[V], s1[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float d[V], (&g)[V] = dz[MODE == TILE_WHOLE ? k : 0];
-            gradient(k, d, g);
-            const int n = l.valid(t, k);
-            if (n == V) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
-            } else if (FLAT && n) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) if (i < n) { s0[i] += g[i]; s1[i] += g[i] * d[i]; }
-            }
-            keep_packed(xv[k]);
-        }
-        // over the tile's places, per channel: `shares` lanes a channel, then those
-        const int tc = FLAT ? c.channels : t.channels, sums = t.units * tc, places = FLAT ? t.cols * V / c.channels : t.lane_rows;
-        float* p0 = lds;                             // [lane][V]: [unit][place][channel]
-        float* p1 = p0 + threads * V;
-        float* q0 = p1 + threads * V;                // [share][unit][channel]
-        float* q1 = q0 + threads;
-        float* c0 = q1 + threads;                    // [unit][channel]
-        float* c1 = c0 + sums;
-        float* g0 = c1 + sums;                       // [unit][group]
-        float* g1 = g0 + t.units * t.groups;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            p0[threadIdx.x * V + i] = l.on ? s0[i] * c.drop.scale : 0.f;
-            p1[threadIdx.x * V + i] = l.on ? s1[i] * (c.drop.scale * rstd[WHOLE_PACK ? 0 : i]) : 0.f;
-        }
-        __syncthreads();
-        const int shares = sums >= threads ? 1 : places < threads / sums ? places : threads / sums;
-        for (int s = threadIdx.x; s < sums * shares; s += threads) {
-            const int share = s / sums, ch = s - share * sums, unit = ch / tc, base = unit * t.cols * t.lane_rows * V + ch - unit * tc;
-            float a0 = 0.f, a1 = 0.f;
-            for (int r = share; r < places; r += shares) { a0 += p0[base + r * tc]; a1 += p1[base + r * tc]; }
-            (shares > 1 ? q0 : c0)[s] = a0;
-            (shares > 1 ? q1 : c1)[s] = a1;
-        }
-        __syncthreads();
-        const int64_t image0 = (int64_t)l.image - l.unit, images = c.sets * c.images;
-        for (int ch = threadIdx.x; ch < sums; ch += threads) {
-            float a0 = c0[ch], a1 = c1[ch];
-            if (shares > 1) {
-                a0 = a1 = 0.f;
-                for (int s = 0; s < shares; ++s) { a0 += q0[s * sums + ch]; a1 += q1[s * sums + ch]; }
-                c0[ch] = a0;
-                c1[ch] = a1;
-            }
-            const int unit = ch / tc, in = (int)l.block * t.channels + ch - unit * tc;
-            if (f.parts && image0 + unit < images && in < c.channels) {
-                float* to = f.parts + ((image0 + unit) * t.chunks + l.chunk) * 2 * c.channels + in;
-                to[0] = a0;
-                to[c.channels] = a1;
-            }
-        }
-        if (MODE == TILE_SUMS) return;
-        __syncthreads();
-        const int groups = t.units * t.groups, team = team_of(threads, groups, D), lane = threadIdx.x % team;
-        const float n = (float)c.positions * (float)D;
-        for (int g = threadIdx.x / team; g < groups; g += threads / team) {
-            const int unit = g / t.groups, in = (g - unit * t.groups) * D, ch0 = (int)l.block * t.channels + in;
-            const int64_t image = image0 + unit;
-            float a0 = 0.f, a1 = 0.f;
-            if (image < images && ch0 < c.channels) {
-                const float* weight = c.weight ? c.weight + image / c.images * c.weight_stride + ch0 : nullptr;
-                for (int i = lane; i < D; i += team) {
-                    const float wi = weight ? weight[i] : 1.f;
-                    a0 += wi * c0[unit * tc + in + i];
-                    a1 += wi * c1[unit * tc + in + i];
-                }
-            }
-            a0 = team_sum(a0, team);
-            a1 = team_sum(a1, team);
-            if (lane == 0) { g0[g] = a0 / n; g1[g] = a1 / n; }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-            gA[a] = rstd[a] * g0[l.unit * t.groups + group[a]];
-            gB[a] = rstd[a] * g1[l.unit * t.groups + group[a]];
-        }
-    } else {
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-            gA[a] = rstd[a] * f.group_sums[2 * (first_group + group[a])];
-            gB[a] = rstd[a] * f.group_sums[2 * (first_group + group[a]) + 1];
-        }
+        rA[a] = h.rstd[a] * s.g0[l.unit * t.groups + h.group[a]];
+        rrB[a] = h.rstd[a] * h.rstd[a] * s.g0[(t.units + l.unit) * t.groups + h.group[a]];
     }
     const Place<V, FLAT> to(c, t, l, c.outs);
 #pragma unroll
-    for (int a = 0; a < A; ++a) gB[a] *= rstd[a];
-#pragma unroll
     for (int k = 0; k < NV; ++k) {
-        float v[V], d[V];
-        if (MODE == TILE_APPLY) gradient(k, d, v);
+        float d[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int a = WHOLE_PACK ? 0 : i;
-            if (MODE == TILE_WHOLE) { v[i] = dz[k][i]; d[i] = to_float(xv[k][i]) - mean[a]; }
-            v[i] = v[i] * (w[i] * c.drop.scale) - gA[a] - d[i] * gB[a];
-        }
-        tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
+        for (int i = 0; i < V; ++i) d[i] = to_float(xv[k][i]) - h.mean[WHOLE_PACK ? 0 : i];
+        write_dx<E, V, FLAT, WHOLE_PACK>(c, t, l, h, to, k, d, dz[k], rA, rrB);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <class E> hipError_t tiled_backward(const NormCall& c, const Tile& t, void* workspace, hipStream_t st);
+// sums of a chunk per channel, in turns of GRAD_PACKS packs per lane, the next turn's on their way
+template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+__global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
+    constexpr int NV = GRAD_PACKS;
+    extern __shared__ float lds[];
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+    const Lane<V, FLAT> l(c, t);
+    const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
+    typename Pack<E, V>::type xn[NV], gn[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+        gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
+    }
+    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    float s0[V], s1[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
+    for (int turn = 0; turn < t.nv; turn += NV) {
+        typename Pack<E, V>::type xv[NV], gv[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) { xv[k] = xn[k]; gv[k] = gn[k]; }
+        if (turn + NV < t.nv) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn + NV + k);
+                gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, turn + NV + k);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float d[V], g[V];
+            h.template gradient<SILU, DROP>(c, l, turn + k, xv[k], gv[k], d, g);
+            add_pack<V, FLAT>(l.valid(t, turn + k), d, g, s0, s1);
+        }
+    }
+    channel_sums(f, l, h, SumSpace(lds, blockDim.x * V, t.channels, blockDim.x), s0, s1);
+}
+
+// dweight and dbias: a learner's sums over its images and their chunks.  A workgroup (the largest power of two of its lanes): `wide`
+// channels (another), the rows dealt out to the lanes of a channel, then halves of these onto each other.
+__device__ __forceinline__ void add_parameters(const BackwardCall& f, uint32_t block, float* lds) {
+    const NormCall& c = f.n;
+    const int threads = 1 << (31 - __builtin_clz(blockDim.x)), wide = f.param_wide, lane = threadIdx.x;
+    const uint32_t set = block / (uint32_t)f.param_blocks;
+    const int ch = (int)(block - set * f.param_blocks) * wide + lane % wide, share = lane / wide, shares = threads / wide;
+    const int64_t rows = c.images * f.chunks;
+    float a = 0.f, b = 0.f;
+    if (lane < threads && ch < c.channels) {
+        const float* p = f.parts + set * rows * 2 * c.channels + ch;
+#pragma unroll 8
+        for (int64_t r = share; r < rows; r += shares) { a += p[r * 2 * c.channels]; b += p[r * 2 * c.channels + c.channels]; }
+    }
+    if (lane < threads) { lds[lane] = a; lds[threads + lane] = b; }
+    __syncthreads();
+    for (int s = threads / 2; s >= wide; s /= 2) {
+        if (lane < s) { lds[lane] += lds[lane + s]; lds[threads + lane] += lds[threads + lane + s]; }
+        __syncthreads();
+    }
+    if (lane < wide && ch < c.channels) {
+        if (c.dbias) c.dbias[set * c.dbias_stride + ch] = lds[lane];
+        if (c.dweight) c.dweight[set * c.dweight_stride + ch] = lds[threads + lane];
+    }
+}
+
+// dx of an image read again, last tiles first (what the sums read last is what a cache still holds); behind the tiles, the parameters
+template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+__global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
+    constexpr int A = WHOLE_PACK ? 1 : V, NV = APPLY_PACKS;
+    extern __shared__ float lds[];
+    if (blockIdx.x >= f.tiles) { add_parameters(f, blockIdx.x - f.tiles, lds); return; }
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+    const Lane<V, FLAT> l(c, t, true, f.tiles);
+    const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys), to(c, t, l, c.outs);
+    typename Pack<E, V>::type xv[NV], gv[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+        gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
+    }
+    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    float rA[A], rrB[A];
+    if (f.group_sums) {
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            rA[a] = h.rstd[a] * f.group_sums[2 * (h.first_group + h.group[a])];
+            rrB[a] = h.rstd[a] * h.rstd[a] * f.group_sums[2 * (h.first_group + h.group[a]) + 1];
+        }
+    } else {
+        const SumSpace s(lds, 0, t.channels, blockDim.x);
+        const float* parts = f.parts + (int64_t)l.image * f.chunks * 2 * c.channels + l.block * t.channels;
+        add_up(s, t.channels, f.chunks,
+               [&](int sum, int j, float& a0, float& a1) {
+                   if ((int)l.block * t.channels + sum >= c.channels) return;
+                   a0 += parts[(int64_t)j * 2 * c.channels + sum];
+                   a1 += parts[(int64_t)j * 2 * c.channels + c.channels + sum];
+               },
+               [](int, float, float) {});
+        __syncthreads();
+        group_means(c, t, l, s);
+        __syncthreads();
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            rA[a] = h.rstd[a] * s.g0[h.group[a]];
+            rrB[a] = h.rstd[a] * h.rstd[a] * s.g0[t.groups + h.group[a]];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float d[V], g[V];
+        h.template gradient<SILU, DROP>(c, l, k, xv[k], gv[k], d, g);
+        write_dx<E, V, FLAT, WHOLE_PACK>(c, t, l, h, to, k, d, g, rA, rrB);
+    }
+}
+
+// A and B of a group from the sums of its image's chunks: a workgroup per group
+template <int T>
+__global__ void __launch_bounds__(T) norm_group_kernel(BackwardCall f, float* group_sums) {
+    __shared__ float lds[8];                         // (T = 256: four wavefronts)
+    const NormCall& c = f.n;
+    const uint32_t image = blockIdx.x / (uint32_t)c.groups, set = image / (uint32_t)c.images;
+    const int D = c.channels / c.groups, first = (int)(blockIdx.x - image * c.groups) * D;
+    const float* p = f.parts + (int64_t)image * f.chunks * 2 * c.channels + first;
+    const float* w = c.weight ? c.weight + set * c.weight_stride + first : nullptr;
+    float a = 0.f, b = 0.f;
+    for (int r = threadIdx.x / D, i = threadIdx.x - r * D; r < f.chunks;) {
+        const float wi = w ? w[i] : 1.f;
+        a += wi * p[(int64_t)r * 2 * c.channels + i];
+        b += wi * p[(int64_t)r * 2 * c.channels + c.channels + i];
+        i += T;
+        if (i >= D) { const int over = i / D; r += over; i -= over * D; }
+    }
+    a = team_sum(a, 64);
+    b = team_sum(b, 64);
+    if (threadIdx.x % 64 == 0) { lds[threadIdx.x / 64] = a; lds[4 + threadIdx.x / 64] = b; }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        const float* q = lds + 4 * threadIdx.x;
+        group_sums[2 * (int64_t)blockIdx.x + threadIdx.x] = ((q[0] + q[1]) + (q[2] + q[3])) / ((float)c.positions * (float)D);
+    }
+}
+
+template <int T>
+__global__ void __launch_bounds__(T) norm_param_kernel(BackwardCall f) {
+    extern __shared__ float lds[];
+    add_parameters(f, blockIdx.x, lds);
+}
+
+// ---- launches ----
+
+// the tiles' workgroups and `more` behind them
+template <class Kernel>
+hipError_t start_backward(Kernel kernel, BackwardCall& f, size_t lds, int64_t more, hipStream_t st) {
+    const Tile& t = f.t;
+    const int64_t images = f.n.sets * f.n.images, tiles = (images + t.units - 1) / t.units * t.blocks * t.chunks;
+    if (tiles + more >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    if (lds > LDS_PLAIN) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    f.tiles = (uint32_t)tiles;
+    kernel<<<dim3((unsigned)(tiles + more)), dim3(t.threads), lds, st>>>(f);
+    return hipGetLastError();
+}
+
+// workgroups that add up the parameters' gradients
+inline int64_t param_blocks(BackwardCall& f) {
+    const NormCall& c = f.n;
+    if (!c.dweight && !c.dbias) return 0;
+    f.param_wide = 64;
+    while (f.param_wide > 1 && f.param_wide / 2 >= c.channels) f.param_wide /= 2;
+    f.param_blocks = (c.channels + f.param_wide - 1) / f.param_wide;
+    return c.sets * f.param_blocks;
+}
+
+template <class E, int V, bool FLAT, bool WHOLE_PACK>
+hipError_t backward_twice(BackwardCall& f, const NormTiles& t, float* workspace, hipStream_t st) {
+    const NormCall& c = f.n;
+    const int64_t images = c.sets * c.images, groups = images * c.groups;
+    f.parts = workspace;
+    f.chunks = t.sums.chunks;
+    f.t = t.sums;
+    return with_options(c, [&](auto silu, auto drop) {
+        hipError_t e = start_backward(norm_sums_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, 0, st);
+        if (e != hipSuccess) return e;
+        // The workgroups that write dx add up the chunks of their channels themselves, where that is little beside their tile.
+        if ((int64_t)f.chunks * t.apply.channels > JOINED_PARTS) {
+            float* group_sums = workspace + images * f.chunks * 2 * c.channels;
+            f.group_sums = group_sums;
+            norm_group_kernel<256><<<dim3((unsigned)groups), dim3(256), 0, st>>>(f, group_sums);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        f.t = t.apply;
+        const int64_t params = param_blocks(f);
+        const size_t space = (size_t)(2 * f.t.threads + 2 * (f.t.channels + f.t.groups)) * sizeof(float);
+        return start_backward(norm_dx_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, space, params, st);
+    });
+}
+
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK>
+hipError_t backward_whole(BackwardCall& f, hipStream_t st) {
+    return with_options(f.n, [&](auto silu, auto drop) {
+        return start_backward(norm_backward_kernel<E, V, NV, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, 0, st);
+    });
+}
+
+template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles& tiles, void* workspace, hipStream_t st) {
+    BackwardCall f = {};
+    f.n = c;
+    f.x_extent = extent_of(c, c.xs);
+    f.dy_extent = extent_of(c, c.dys);
+    const bool whole = tiles.whole.nv != 0;
+    f.t = whole ? tiles.whole : tiles.sums;
+    return with_layout<E>(f.t, [&](auto vec, auto flat, auto whole_pack) {
+        constexpr int V = vec.value;
+        constexpr bool FLAT = flat.value, PACK = whole_pack.value;
+        if (!whole) return backward_twice<E, V, FLAT, PACK>(f, tiles, (float*)workspace, st);
+        f.chunks = 1;
+        const int64_t params = param_blocks(f);
+        f.parts = params ? (float*)workspace : nullptr;
+        hipError_t e;
+        switch (f.t.nv) {
+            case 1: e = backward_whole<E, V, 1, FLAT, PACK>(f, st); break;
+            case 2: e = backward_whole<E, V, 2, FLAT, PACK>(f, st); break;
+            default: e = backward_whole<E, V, backward_packs(FLAT, V), FLAT, PACK>(f, st);
+        }
+        if (e != hipSuccess || !params) return e;
+        norm_param_kernel<1024><<<dim3((unsigned)params), dim3(1024), 2 * 1024 * sizeof(float), st>>>(f);
+        return hipGetLastError();
+    });
+}
 
 }  // namespace kavg

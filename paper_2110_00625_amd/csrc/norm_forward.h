@@ -2,7 +2,7 @@
 //     m = mean x,  v = mean (x - m)^2,  r = (v + eps)^(-1/2),  y = drop(act(weight_c r (x - m) + bias_c)).
 // A lane takes mean and squared distances from it of its own elements (per group, or per channel where a pack straddles groups), the
 // lanes of a group are joined as means of parts: m = sum n_i m_i / n, n v = sum (q_i + n_i (m_i - m)^2), which loses nothing where the
-// mean is far from zero.  Images cut into chunks leave (m, n v) of every chunk and are joined the same way by a kernel of their own.
+// mean is far from zero.  The chunks of an image that is read twice, and the turns of a chunk, are joined the same way.
 #pragma once
 #include "norm_tile.h"
 
@@ -12,141 +12,120 @@ struct ForwardCall {
     NormCall n;
     Tile t;
     int64_t x_extent;
-    float* parts;          // [image][group][chunk] of (mean, squares), chunks only
-    const float *mean, *rstd;      // results from finished sums
+    float* parts;                  // [image][group][chunk] of (mean, squares)
+    // results from finished sums: mean and rstd, or, where they are null, the parts of `chunks` chunks, all but the last of `whole` values
+    const float *mean, *rstd;
+    int chunks;
+    float whole, last;
 };
 
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, int MODE>
-__global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V;            // sums of a lane
-    extern __shared__ float lds[];
-    const NormCall& c = f.n;
-    const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t);
-    const int D = c.channels / c.groups;
-    const Place<V, FLAT> from(c, t, l, c.xs);
-    typename Pack<E, V>::type xv[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+// mean and sum of squared distances of a group's values from its parts: a team of lanes, part j with n(j) values, mean m(j), squares q(j)
+template <class N, class M, class Q>
+__device__ __forceinline__ void join_parts(int terms, int lane, int team, float n, N count, M mean_of, Q squares_of, float* mean, float* squares) {
+    float s = 0.f;
+    for (int j = lane; j < terms; j += team) s += count(j) * mean_of(j);
+    const float m = team_sum(s, team) / n;
+    float q = 0.f;
+    for (int j = lane; j < terms; j += team) { const float d = mean_of(j) - m; q += squares_of(j) + count(j) * d * d; }
+    *mean = m;
+    *squares = team_sum(q, team);
+}
 
-    float w[V], b[V];
-    const auto parameters = [&] {
+// sum[a], sq[a]: squared distances from mean[a] of a lane's NV packs, n of them valid (flat: of each element's)
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, class Valid>
+__device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[WHOLE_PACK ? 1 : V], float (&sq)[WHOLE_PACK ? 1 : V],
+                                             int (&count)[FLAT ? V : 1]) {
+    constexpr int A = WHOLE_PACK ? 1 : V;
+    float sum[A];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int ch = l.channel(c, i);
-            w[i] = c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f;
-            b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
-        }
-    };
-    int group[A];                                    // in the tile
+    for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
 #pragma unroll
-    for (int a = 0; a < A; ++a) group[a] = fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s);
-    float mean[A], rstd[A];
-
-    if (MODE != TILE_APPLY) {
-        const int threads = blockDim.x;
-        float* part_sum = lds;                       // [lane][A]
-        float* part_sq = lds + threads * A;
-        float* stat = part_sq + threads * A;         // [unit][group of the tile] mean, then rstd
-        // of the chunk: whole rounds of the lanes, and rows (flat: elements) of the last one
-        const int64_t all = FLAT ? l.run : t.rows, step = FLAT ? (int64_t)t.cols * V : t.lane_rows;
-        const int64_t before = (int64_t)l.chunk * NV * step, here = all - before < NV * step ? all - before : NV * step;
-        const int rounds = (int)(here / step), rest = (int)(here - rounds * step);
-        float sum[A], sq[A];
+    for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] = 0;
 #pragma unroll
-        for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int n = l.valid(t, k);
-            if (WHOLE_PACK) { if (n) sum[0] = pack_sum<V>(xv[k], sum[0]); }
-            else if (n == V) {
+    for (int k = 0; k < NV; ++k) {
+        const int n = valid(k);
+        if (n == V) {
+            if (WHOLE_PACK) sum[0] = pack_sum<V>(xv[k], sum[0]);
+            else {
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += to_float(xv[k][i]);
-            } else if (FLAT && n) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += i < n ? to_float(xv[k][i]) : 0.f;
             }
-            keep_packed(xv[k]);
+        } else if (FLAT && n) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += i < n ? to_float(xv[k][i]) : 0.f;
         }
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-            const int n = l.on ? (rounds + ((FLAT ? (int)l.col * V + a : (int)l.row) < rest)) * (WHOLE_PACK ? V : 1) : 0;
-            mean[a] = n ? sum[a] / (float)n : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int n = l.valid(t, k);
-            if (n == V) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
-            } else if (FLAT && n) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
-            }
-            keep_packed(xv[k]);
-        }
-#pragma unroll
-        for (int a = 0; a < A; ++a) { part_sum[threadIdx.x * A + a] = sum[a]; part_sq[threadIdx.x * A + a] = sq[a]; }
-        if (MODE != TILE_SUMS) parameters();         // (on their way while the groups are joined)
-        __syncthreads();
-        // a team of lanes per group: parts (place, channel or pack) of the group, row by row
-        const int per = WHOLE_PACK ? D / V : D, slots = (FLAT ? c.channels : t.channels) / (WHOLE_PACK ? V : 1);
-        const int places = FLAT ? t.cols * V / c.channels : t.lane_rows, terms = places * per, sums = t.units * t.groups;
-        const int team = team_of(threads, sums, terms), lane = threadIdx.x % team;
-        const float n = (float)(FLAT ? here / c.channels : here) * (float)D;
-        for (int g = threadIdx.x / team; g < sums; g += threads / team) {
-            const int unit = g / t.groups, in = g - unit * t.groups, base = unit * t.cols * t.lane_rows * A + in * per;
-            float s = 0.f;
-            for (int j = lane, r = lane / per, i = lane - r * per; j < terms; j += team) {
-                s += part_sum[base + r * slots + i];
-                i += team;
-                while (i >= per) { i -= per; ++r; }
-            }
-            const float m = team_sum(s, team) / n;
-            float q = 0.f;
-            for (int j = lane, r = lane / per, i = lane - r * per; j < terms; j += team) {
-                const int place = FLAT ? r * slots + in * per + i : r;
-                const float cnt = (float)((rounds + (place < rest)) * (WHOLE_PACK ? V : 1));
-                const float d = cnt > 0.f ? part_sum[base + r * slots + i] / cnt - m : 0.f;
-                q += part_sq[base + r * slots + i] + cnt * d * d;
-                i += team;
-                while (i >= per) { i -= per; ++r; }
-            }
-            q = team_sum(q, team);
-            if (lane == 0) {
-                const int64_t image = (int64_t)l.image - l.unit + unit;
-                const int group_ = (int)l.block * t.groups + in;
-                const bool there = image < c.sets * c.images && group_ < c.groups;
-                const int64_t at = image * c.groups + group_;
-                if (MODE == TILE_SUMS) {
-                    if (there) { f.parts[(at * t.chunks + l.chunk) * 2] = m; f.parts[(at * t.chunks + l.chunk) * 2 + 1] = q; }
-                } else {
-                    const float rs = 1.f / sqrtf(q / n + c.eps);
-                    stat[g] = m;
-                    stat[sums + g] = rs;
-                    if (c.mean && there) { c.mean[at] = m; c.rstd[at] = rs; }
-                }
-            }
-        }
-        if (MODE == TILE_SUMS) return;
-        __syncthreads();
-#pragma unroll
-        for (int a = 0; a < A; ++a) { mean[a] = stat[l.unit * t.groups + group[a]]; rstd[a] = stat[sums + l.unit * t.groups + group[a]]; }
-    } else {
-        parameters();
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-            const int64_t at = l.on ? (int64_t)l.image * c.groups + l.block * t.groups + group[a] : 0;
-            mean[a] = f.mean[at];
-            rstd[a] = f.rstd[at];
-        }
+        for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] += n > a;
+        keep_packed(xv[k]);
     }
+#pragma unroll
+    for (int a = 0; a < A; ++a) mean[a] = count[FLAT ? a : 0] ? sum[a] / (float)(count[FLAT ? a : 0] * (WHOLE_PACK ? V : 1)) : 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int n = valid(k);
+        if (n == V) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
+        } else if (FLAT && n) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
+        }
+        keep_packed(xv[k]);
+    }
+}
+
+// The lanes' moments joined per group of the tile: done(unit, group in the tile, mean, squares) in one lane of each.  lds: 2 * lanes * A floats.
+template <int V, bool FLAT, bool WHOLE_PACK, class Done>
+__device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Chunk<V, FLAT>& chunk, float* lds,
+                                           const float (&mean)[WHOLE_PACK ? 1 : V], const float (&sq)[WHOLE_PACK ? 1 : V], Done done) {
+    constexpr int A = WHOLE_PACK ? 1 : V;
+    const int threads = blockDim.x, D = c.channels / c.groups;
+    float* part_mean = lds;                          // [lane][A]: [unit][place][channel or pack]
+    float* part_sq = lds + threads * A;
+#pragma unroll
+    for (int a = 0; a < A; ++a) { part_mean[threadIdx.x * A + a] = mean[a]; part_sq[threadIdx.x * A + a] = sq[a]; }
+    __syncthreads();
+    const int per = WHOLE_PACK ? D / V : D, slots = (FLAT ? c.channels : t.channels) / (WHOLE_PACK ? V : 1);
+    const int places = FLAT ? t.cols * V / c.channels : t.lane_rows, terms = places * per, groups = t.units * t.groups;
+    const int team = team_of(threads, groups, terms), lane = threadIdx.x % team;
+    for (int g = threadIdx.x / team; g < groups; g += threads / team) {
+        const int unit = g / t.groups, in = g - unit * t.groups, base = unit * t.cols * t.lane_rows * A + in * per;
+        // part j of the group: place j / per
+        const auto place = [&](int j) { return (int)fastdiv(j, t.per_m, t.per_s); };
+        const auto slot = [&](int j) { const int r = place(j); return r * slots + j - r * per; };
+        float m, q;
+        join_parts(terms, lane, team, chunk.positions * (float)D,
+                   [&](int j) { return (float)(chunk.rounds_of(FLAT ? slot(j) + in * per : place(j)) * (WHOLE_PACK ? V : 1)); },
+                   [&](int j) { return part_mean[base + slot(j)]; }, [&](int j) { return part_sq[base + slot(j)]; }, &m, &q);
+        if (lane == 0) done(unit, in, m, q);
+    }
+}
+
+template <int V, bool FLAT>
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int ch = l.channel(c, i);
+        w[i] = c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f;
+        b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
+    }
+}
+
+// group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
+template <int V, bool FLAT, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
+#pragma unroll
+    for (int a = 0; a < A; ++a) group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s) : 0;
+}
+
+// y from packs in registers
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+__device__ __forceinline__ void write_results(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const typename Pack<E, V>::type (&xv)[NV],
+                                              const float (&mean)[WHOLE_PACK ? 1 : V], const float (&rstd)[WHOLE_PACK ? 1 : V], float (&w)[V], float (&b)[V]) {
     const Place<V, FLAT> to(c, t, l, c.outs);
     const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] *= rstd[WHOLE_PACK ? 0 : i];
-    // drop's scale commutes with ReLU
-    if (c.activation != KAVG_ACT_SILU) {
+    if (DROP && !SILU) {                             // (drop's scale commutes with ReLU)
 #pragma unroll
         for (int i = 0; i < V; ++i) { w[i] *= c.drop.scale; b[i] *= c.drop.scale; }
     }
@@ -154,42 +133,229 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     for (int k = 0; k < NV; ++k) {
         float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]) * w[i] + b[i];
-        if (c.activation == KAVG_ACT_SILU) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activate<KAVG_ACT_SILU>(v[i]) * c.drop.scale;
-        } else if (c.activation == KAVG_ACT_RELU) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activate<KAVG_ACT_RELU>(v[i]);
+        for (int i = 0; i < V; ++i) {
+            v[i] = activate<SILU>((to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]) * w[i] + b[i], c.floor);
+            if (DROP && SILU) v[i] *= c.drop.scale;
         }
-        if (c.drop.threshold) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, v);
+        if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, v);
         tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
     }
 }
 
-// mean and 1/sqrt(v + eps) of a group from its chunks: a wavefront per group
-template <int T>
-__global__ void __launch_bounds__(T) norm_join_kernel(const float* parts, int chunks, int64_t groups, float whole, float last, float eps, float* mean, float* rstd,
-                                                      float* mean2, float* rstd2) {
-    const int64_t g = (int64_t)blockIdx.x * (T / 64) + threadIdx.x / 64;
-    const int lane = threadIdx.x % 64;
-    if (g >= groups) return;
-    const float2* p = (const float2*)parts + g * chunks;
-    const float n = whole * (float)(chunks - 1) + last;
-    float s = 0.f;
-    for (int i = lane; i < chunks; i += 64) s += p[i].x * (i < chunks - 1 ? whole : last);
-    const float m = team_sum(s, 64) / n;
-    float q = 0.f;
-    for (int i = lane; i < chunks; i += 64) { const float d = p[i].x - m; q += p[i].y + (i < chunks - 1 ? whole : last) * d * d; }
-    q = team_sum(q, 64);
-    if (lane == 0) {
-        const float r = 1.f / sqrtf(q / n + eps);
-        mean[g] = m;
-        rstd[g] = r;
-        if (mean2) { mean2[g] = m; rstd2[g] = r; }
-    }
+// images that a workgroup holds
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+__global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
+    constexpr int A = WHOLE_PACK ? 1 : V;
+    extern __shared__ float lds[];
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+    const Lane<V, FLAT> l(c, t);
+    const Place<V, FLAT> from(c, t, l, c.xs);
+    typename Pack<E, V>::type xv[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+
+    const Chunk<V, FLAT> chunk(c, t, l);
+    float mean[A], rstd[A], w[V], b[V];
+    int group[A], count[FLAT ? V : 1];
+    lane_moments<E, V, NV, FLAT, WHOLE_PACK>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
+    lane_parameters(c, l, w, b);                     // (on their way while the groups are joined)
+    lane_groups<V, FLAT, A>(c, t, l, group);
+    float* stat = lds + 2 * blockDim.x * A;          // [unit][group of the tile] mean, then rstd
+    const int groups = t.units * t.groups, D = c.channels / c.groups;
+    join_lanes<V, FLAT, WHOLE_PACK>(c, t, l, chunk, lds, mean, rstd, [&](int unit, int in, float m, float q) {
+        const float r = 1.f / sqrtf(q / (chunk.positions * (float)D) + c.eps);
+        stat[unit * t.groups + in] = m;
+        stat[groups + unit * t.groups + in] = r;
+        const uint32_t image = l.image - l.unit + unit;
+        const int g = (int)l.block * t.groups + in;
+        if (c.mean && image < (uint32_t)(c.sets * c.images) && g < c.groups) {
+            c.mean[(int64_t)image * c.groups + g] = m;
+            c.rstd[(int64_t)image * c.groups + g] = r;
+        }
+    });
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < A; ++a) { mean[a] = stat[l.unit * t.groups + group[a]]; rstd[a] = stat[groups + l.unit * t.groups + group[a]]; }
+    write_results<E, V, NV, FLAT, WHOLE_PACK, SILU, DROP>(c, t, l, xv, mean, rstd, w, b);
 }
 
-template <class E> hipError_t tiled_forward(const NormCall& c, const Tile& t, void* workspace, hipStream_t st);
+// moments of a chunk, in turns of SUM_PACKS packs per lane, the next turn's on their way
+template <class E, int V, bool FLAT, bool WHOLE_PACK>
+__global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
+    constexpr int A = WHOLE_PACK ? 1 : V, NV = SUM_PACKS;
+    extern __shared__ float lds[];
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+    const Lane<V, FLAT> l(c, t);
+    const Place<V, FLAT> from(c, t, l, c.xs);
+    typename Pack<E, V>::type next[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+    float mean[A], sq[A];
+    int before[FLAT ? V : 1];
+#pragma unroll
+    for (int a = 0; a < A; ++a) mean[a] = sq[a] = 0.f;
+#pragma unroll
+    for (int a = 0; a < (FLAT ? V : 1); ++a) before[a] = 0;
+    for (int turn = 0; turn < t.nv; turn += NV) {
+        typename Pack<E, V>::type xv[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) xv[k] = next[k];
+        if (turn + NV < t.nv) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn + NV + k);
+        }
+        float m[A], q[A];
+        int count[FLAT ? V : 1];
+        lane_moments<E, V, NV, FLAT, WHOLE_PACK>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const float n = (float)(count[FLAT ? a : 0] * (WHOLE_PACK ? V : 1)), old = (float)(before[FLAT ? a : 0] * (WHOLE_PACK ? V : 1));
+            const float share = n > 0.f ? n / (n + old) : 0.f, d = m[a] - mean[a];
+            mean[a] += d * share;
+            sq[a] += q[a] + d * d * (old * share);
+        }
+#pragma unroll
+        for (int a = 0; a < (FLAT ? V : 1); ++a) before[a] += count[a];
+    }
+    const Chunk<V, FLAT> chunk(c, t, l);
+    join_lanes<V, FLAT, WHOLE_PACK>(c, t, l, chunk, lds, mean, sq, [&](int unit, int in, float m, float q) {
+        const int g = (int)l.block * t.groups + in;
+        if (g >= c.groups) return;
+        float* to = f.parts + (((int64_t)l.image * c.groups + g) * t.chunks + l.chunk) * 2;
+        to[0] = m;
+        to[1] = q;
+    });
+}
+
+__device__ __forceinline__ void join_chunks(const float* parts, int chunks, float whole, float last, int lane, int team, float* mean, float* squares) {
+    const float2* p = (const float2*)parts;
+    join_parts(chunks, lane, team, whole * (float)(chunks - 1) + last, [&](int j) { return j < chunks - 1 ? whole : last; },
+               [&](int j) { return p[j].x; }, [&](int j) { return p[j].y; }, mean, squares);
+}
+
+// mean and 1/sqrt(v + eps) of a group from its chunks: a wavefront per group
+template <int T>
+__global__ void __launch_bounds__(T) norm_join_kernel(ForwardCall f, int64_t groups, float* mean, float* rstd) {
+    const int64_t g = (int64_t)blockIdx.x * (T / 64) + threadIdx.x / 64;
+    if (g >= groups) return;
+    float m, q;
+    join_chunks(f.parts + 2 * g * f.chunks, f.chunks, f.whole, f.last, threadIdx.x % 64, 64, &m, &q);
+    if (threadIdx.x % 64) return;
+    const float r = 1.f / sqrtf(q / (f.whole * (float)(f.chunks - 1) + f.last) + f.n.eps);
+    mean[g] = m;
+    rstd[g] = r;
+    if (f.n.mean) { f.n.mean[g] = m; f.n.rstd[g] = r; }
+}
+
+// Results of an image read again.  Last tiles first: what the sums read last is what a cache still holds.
+template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+__global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
+    constexpr int A = WHOLE_PACK ? 1 : V, NV = APPLY_PACKS;
+    extern __shared__ float lds[];
+    const NormCall& c = f.n;
+    const Tile& t = f.t;
+    const Lane<V, FLAT> l(c, t, true);
+    const Place<V, FLAT> from(c, t, l, c.xs);
+    typename Pack<E, V>::type xv[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+    float mean[A], rstd[A], w[V], b[V];
+    int group[A];
+    lane_parameters(c, l, w, b);
+    lane_groups<V, FLAT, A>(c, t, l, group);
+    const int64_t first = (int64_t)l.image * c.groups + l.block * t.groups;
+    if (f.mean) {
+#pragma unroll
+        for (int a = 0; a < A; ++a) { mean[a] = l.on ? f.mean[first + group[a]] : 0.f; rstd[a] = l.on ? f.rstd[first + group[a]] : 0.f; }
+    } else {
+        const int team = team_of(blockDim.x, t.groups, f.chunks), lane = threadIdx.x % team;
+        for (int g = threadIdx.x / team; g < t.groups; g += blockDim.x / team) {
+            if ((int)l.block * t.groups + g >= c.groups) break;
+            float m, q;
+            const int64_t at = (int64_t)l.image * c.groups + l.block * t.groups + g;
+            join_chunks(f.parts + 2 * at * f.chunks, f.chunks, f.whole, f.last, lane, team, &m, &q);
+            if (lane) continue;
+            const float r = 1.f / sqrtf(q / (f.whole * (float)(f.chunks - 1) + f.last) + c.eps);
+            lds[g] = m;
+            lds[t.groups + g] = r;
+            if (c.mean && l.chunk == 0) { c.mean[at] = m; c.rstd[at] = r; }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int a = 0; a < A; ++a) { mean[a] = lds[group[a]]; rstd[a] = lds[t.groups + group[a]]; }
+    }
+    write_results<E, V, NV, FLAT, WHOLE_PACK, SILU, DROP>(c, t, l, xv, mean, rstd, w, b);
+}
+
+// ---- launches ----
+
+template <class Kernel>
+hipError_t start_forward(Kernel kernel, const ForwardCall& f, size_t lds, hipStream_t st) {
+    const Tile& t = f.t;
+    const int64_t images = f.n.sets * f.n.images, grid = (images + t.units - 1) / t.units * t.blocks * t.chunks;
+    if (grid >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    if (lds > LDS_PLAIN) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<dim3((unsigned)grid), dim3(t.threads), lds, st>>>(f);
+    return hipGetLastError();
+}
+
+template <class E, int V, bool FLAT, bool WHOLE_PACK>
+hipError_t forward_twice(ForwardCall& f, const NormTiles& t, float* workspace, hipStream_t st) {
+    const NormCall& c = f.n;
+    const int64_t groups = c.sets * c.images * c.groups, whole = chunk_positions(c, t.sums);
+    const float D = (float)(c.channels / c.groups);
+    f.parts = workspace;
+    f.chunks = t.sums.chunks;
+    f.whole = (float)whole * D;
+    f.last = (float)(c.positions - whole * (f.chunks - 1)) * D;
+    f.t = t.sums;
+    hipError_t e = start_forward(norm_moments_kernel<E, V, FLAT, WHOLE_PACK>, f, f.t.lds, st);
+    if (e != hipSuccess) return e;
+    // The workgroups that write the results join the chunks of their groups themselves, where that is little beside their tile.
+    if ((int64_t)f.chunks * t.apply.groups > JOINED_PARTS) {
+        float* mean = workspace + 2 * groups * f.chunks;
+        f.mean = mean;
+        f.rstd = mean + groups;
+        norm_join_kernel<256><<<dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, st>>>(f, groups, mean, mean + groups);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    f.t = t.apply;
+    return with_options(c, [&](auto silu, auto drop) {
+        return start_forward(norm_apply_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, 2 * f.t.groups * sizeof(float), st);
+    });
+}
+
+template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK>
+hipError_t forward_whole(const ForwardCall& f, hipStream_t st) {
+    return with_options(f.n, [&](auto silu, auto drop) {
+        return start_forward(norm_forward_kernel<E, V, NV, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, st);
+    });
+}
+
+template <class E> hipError_t tiled_forward(const NormCall& c, const NormTiles& tiles, void* workspace, hipStream_t st) {
+    ForwardCall f = {};
+    f.n = c;
+    f.x_extent = extent_of(c, c.xs);
+    const bool whole = tiles.whole.nv != 0;
+    f.t = whole ? tiles.whole : tiles.sums;
+    return with_layout<E>(f.t, [&](auto vec, auto flat, auto whole_pack) {
+        constexpr int V = vec.value;
+        constexpr bool FLAT = flat.value, PACK = whole_pack.value;
+        if (!whole) return forward_twice<E, V, FLAT, PACK>(f, tiles, (float*)workspace, st);
+        switch (f.t.nv) {
+            case 1: return forward_whole<E, V, 1, FLAT, PACK>(f, st);
+            case 2: return forward_whole<E, V, 2, FLAT, PACK>(f, st);
+            case 4: return forward_whole<E, V, 4, FLAT, PACK>(f, st);
+            case 8: return forward_whole<E, V, 8, FLAT, PACK>(f, st);
+            default: return forward_whole<E, V, FLAT ? FLAT_PACKS : FORWARD_PACKS, FLAT, PACK>(f, st);
+        }
+    });
+}
 
 }  // namespace kavg

@@ -9,10 +9,12 @@
 //          cols * V is a multiple of the channels, so a lane's packs still hold the same channels (going round after the last one).
 //   V = 1  neither.
 //
-// An image that one workgroup cannot hold is cut into chunks of NV * lane_rows rows; small images share a workgroup (units).
+// An image that one workgroup cannot hold is read twice: first for its sums, by workgroups that go through a chunk of it in turns, then
+// for its results.  Small images share a workgroup (units).
 #pragma once
 #include "layers.h"
 #include "fastdiv.h"
+#include <type_traits>
 
 namespace kavg {
 
@@ -24,16 +26,50 @@ struct Tile {
     int channels, groups;    // of a tile
     int blocks, chunks;      // tiles of an image: along its channels, along its rows
     int rows;                // of an image
-    uint32_t unit_m, col_m, d_m; int unit_s, col_s, d_s;     // divisions by lanes per unit, cols, channels per group
+    // divisions by lanes per unit, cols, channels per group, sums of a row per group (packs, or channels)
+    uint32_t unit_m, col_m, d_m, per_m; int unit_s, col_s, d_s, per_s;
     size_t lds;
 };
 
-constexpr int FLAT_PACKS = 8;    // the most packs per lane of a flat tile (its sums are per channel, and its last pack needs care: more spill)
-constexpr int BACKWARD_PACKS = 4;   // of the backward pass, which holds x and dz (in fp32) of each
-enum { TILE_WHOLE = 0, TILE_SUMS = 1, TILE_APPLY = 2 };      // sums and results; sums alone (chunks); results from finished sums
+// Tiles of a call: one for a workgroup that holds its part of an image (whole.nv > 0), or two, for sums and for results.
+struct NormTiles { Tile whole, sums, apply; };
+
+constexpr int FORWARD_PACKS = 16;  // the most packs per lane
+constexpr int FLAT_PACKS = 8;      // of a flat tile (its sums are per channel, and its last pack needs care: more spill)
+// of the backward pass, which holds x and dz (in fp32) of each
+constexpr int backward_packs(bool flat, int vec) { return flat && vec == 8 ? 2 : 4; }
+constexpr int SUM_PACKS = 4;       // of a turn of the forward sums, which holds two turns
+constexpr int GRAD_PACKS = 2;      // of a turn of the backward sums
+constexpr int APPLY_PACKS = 4;
+
+constexpr int JOINED_PARTS = 2048; // chunks times groups that the workgroups of the results join themselves
+constexpr size_t LDS_PLAIN = 64 * 1024;      // more than that has to be asked for
+
+// elements of a tensor from its first to its last
+inline int64_t extent_of(const NormCall& c, const Strides& s) {
+    return (c.sets - 1) * s.set + (c.images - 1) * s.image + (c.positions - 1) * s.row + c.channels;
+}
 
 // false: no tile fits (groups too wide for a workgroup)
-bool norm_tile(const NormCall& c, bool contiguous, bool backward, Tile* t);
+bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t);
+// values of a group in a whole chunk, in positions
+inline int64_t chunk_positions(const NormCall& c, const Tile& t) { return (int64_t)t.nv * (t.flat ? (int64_t)t.cols * t.vec / c.channels : t.lane_rows); }
+
+template <class E> hipError_t tiled_forward(const NormCall& c, const NormTiles& t, void* workspace, hipStream_t st);
+template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles& t, void* workspace, hipStream_t st);
+
+// f(constants: elements of a pack, flat, whole packs) of a tile
+template <class E, class F> hipError_t with_layout(const Tile& t, F f) {
+    constexpr std::integral_constant<int, 16 / (int)sizeof(E)> pack = {};
+    if (t.vec == 1) return f(std::integral_constant<int, 1>(), std::false_type(), std::true_type());
+    if (t.flat) return f(pack, std::true_type(), std::false_type());
+    return t.whole_pack ? f(pack, std::false_type(), std::true_type()) : f(pack, std::false_type(), std::false_type());
+}
+// f(constants: SiLU, dropout)
+template <class F> hipError_t with_options(const NormCall& c, F f) {
+    if (c.drop.threshold) return c.silu ? f(std::true_type(), std::true_type()) : f(std::false_type(), std::true_type());
+    return c.silu ? f(std::true_type(), std::false_type()) : f(std::false_type(), std::false_type());
+}
 
 #if defined(__HIPCC__)
 
@@ -52,8 +88,10 @@ template <int V, bool FLAT> struct Lane {
     bool on;
     int64_t run;                                    // flat: elements of an image
 
-    __device__ __forceinline__ Lane(const NormCall& c, const Tile& t) {
-        const uint32_t b = xcd_order(blockIdx.x, gridDim.x), per_unit = t.cols * t.lane_rows;
+    __device__ __forceinline__ Lane(const NormCall& c, const Tile& t, bool backwards = false, uint32_t tiles = gridDim.x) {
+        uint32_t b = xcd_order(blockIdx.x, tiles);
+        if (backwards) b = tiles - 1 - b;
+        const uint32_t per_unit = t.cols * t.lane_rows;
         const uint32_t rest = b / (uint32_t)t.chunks;
         chunk = b - rest * t.chunks;
         const uint32_t first = rest / (uint32_t)t.blocks;
@@ -109,6 +147,22 @@ template <int V, bool FLAT> struct Place {
         // (a lane without a pack 0 reads the image's first row)
         if (!l.valid(t, 0)) first = l.set * s.set + l.image_in_set * s.image + (FLAT ? 0 : l.first_channel);
     }
+};
+
+// of the chunk: rows (flat: elements) of a round of the lanes, whole rounds, and rows of the last one; its positions
+template <int V, bool FLAT> struct Chunk {
+    int64_t step;
+    int rounds, rest;
+    float positions;
+    __device__ __forceinline__ Chunk(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) {
+        step = FLAT ? (int64_t)t.cols * V : t.lane_rows;
+        const int64_t all = (FLAT ? l.run : t.rows) - (int64_t)l.chunk * t.nv * step, here = all < t.nv * step ? all : t.nv * step;
+        rounds = (int)((uint32_t)(here / step));
+        rest = (int)(here - rounds * step);
+        positions = (float)(FLAT ? here / c.channels : here);
+    }
+    // rounds in which a place of the lanes (row; flat: element) is the image's
+    __device__ __forceinline__ int rounds_of(int place) const { return rounds + (place < rest); }
 };
 
 // Pack k of a tensor; pack 0 once more where the image has no such pack.  One at a flat image's end may reach past it, into the next image,
