@@ -23,8 +23,8 @@ struct BackwardCall {
 };
 
 // What a lane keeps of its channels: m, r, weight_c r, bias_c.
-template <int V, bool FLAT, bool WHOLE_PACK> struct Channels {
-    static constexpr int A = WHOLE_PACK ? 1 : V;
+template <int V, bool FLAT, int GRAN> struct Channels {
+    static constexpr int A = V / GRAN;
     float w[V], b[V], mean[A], rstd[A];
     int group[A];                                    // in the tile
     int64_t first_group;                             // of the tile (of a lane without work, whose groups may not exist: the first of all)
@@ -34,14 +34,14 @@ template <int V, bool FLAT, bool WHOLE_PACK> struct Channels {
         first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s) : 0;
+            group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.d_m, t.d_s) : 0;
             mean[a] = c.mean[first_group + group[a]];
             rstd[a] = c.rstd[first_group + group[a]];
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int ch = l.channel(c, i);
-            w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[WHOLE_PACK ? 0 : i];
+            w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[i / GRAN];
             b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
         }
         number = l.number(c, t);
@@ -53,7 +53,7 @@ template <int V, bool FLAT, bool WHOLE_PACK> struct Channels {
         float z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            d[i] = to_float(x[i]) - mean[WHOLE_PACK ? 0 : i];
+            d[i] = to_float(x[i]) - mean[i / GRAN];
             z[i] = d[i] * w[i] + b[i];
             g[i] = to_float(dy[i]);
         }
@@ -76,7 +76,7 @@ __device__ __forceinline__ void add_pack(int n, const float (&d)[V], const float
 }
 
 // `shares` lanes for each of `sums` sums
-__device__ __forceinline__ int shares_of(int threads, int sums, int terms) { return sums >= threads ? 1 : terms < threads / sums ? terms : threads / sums; }
+KAVG_FD int shares_of(int threads, int sums, int terms) { return sums >= threads ? 1 : terms < threads / sums ? terms : threads / sums; }
 
 // LDS of the sums
 struct SumSpace {
@@ -120,15 +120,15 @@ __device__ __forceinline__ void add_up(const SumSpace& s, int sums, int terms, T
 }
 
 // the lanes' sums per channel: into LDS and, where wanted, to the parts
-template <int V, bool FLAT, bool WHOLE_PACK>
-__device__ __forceinline__ void channel_sums(const BackwardCall& f, const Lane<V, FLAT>& l, const Channels<V, FLAT, WHOLE_PACK>& h, const SumSpace& s,
+template <int V, bool FLAT, int GRAN>
+__device__ __forceinline__ void channel_sums(const BackwardCall& f, const Lane<V, FLAT>& l, const Channels<V, FLAT, GRAN>& h, const SumSpace& s,
                                              const float (&s0)[V], const float (&s1)[V]) {
     const NormCall& c = f.n;
     const Tile& t = f.t;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         s.p0[threadIdx.x * V + i] = l.on ? s0[i] * c.drop.scale : 0.f;
-        s.p1[threadIdx.x * V + i] = l.on ? s1[i] * (c.drop.scale * h.rstd[WHOLE_PACK ? 0 : i]) : 0.f;
+        s.p1[threadIdx.x * V + i] = l.on ? s1[i] * (c.drop.scale * h.rstd[i / GRAN]) : 0.f;
     }
     __syncthreads();
     const int tc = t.channels, sums = t.units * tc, places = FLAT ? t.cols * V / tc : t.lane_rows, per_unit = t.cols * t.lane_rows * V;
@@ -172,18 +172,18 @@ template <int V, bool FLAT> __device__ __forceinline__ void group_means(const No
 }
 
 // dx of pack k from dz (without scale) and x - m
-template <class E, int V, bool FLAT, bool WHOLE_PACK>
-__device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Channels<V, FLAT, WHOLE_PACK>& h, const Place<V, FLAT>& to, int k,
-                                         const float (&d)[V], float (&g)[V], const float (&rA)[WHOLE_PACK ? 1 : V], const float (&rrB)[WHOLE_PACK ? 1 : V]) {
+template <class E, int V, bool FLAT, int GRAN>
+__device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Channels<V, FLAT, GRAN>& h, const Place<V, FLAT>& to, int k,
+                                         const float (&d)[V], float (&g)[V], const float (&rA)[V / GRAN], const float (&rrB)[V / GRAN]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) g[i] = g[i] * (h.w[i] * c.drop.scale) - rA[WHOLE_PACK ? 0 : i] - d[i] * rrB[WHOLE_PACK ? 0 : i];
+    for (int i = 0; i < V; ++i) g[i] = g[i] * (h.w[i] * c.drop.scale) - rA[i / GRAN] - d[i] * rrB[i / GRAN];
     tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, g);
 }
 
 // images that a workgroup holds
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+template <class E, int V, int NV, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V;
+    constexpr int A = V / GRAN;
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
             gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
         }
     }
-    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    const Channels<V, FLAT, GRAN> h(c, t, l);
     float dz[NV][V], s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
@@ -225,14 +225,14 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     for (int k = 0; k < NV; ++k) {
         float d[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) d[i] = to_float(xv[k][i]) - h.mean[WHOLE_PACK ? 0 : i];
-        write_dx<E, V, FLAT, WHOLE_PACK>(c, t, l, h, to, k, d, dz[k], rA, rrB);
+        for (int i = 0; i < V; ++i) d[i] = to_float(xv[k][i]) - h.mean[i / GRAN];
+        write_dx<E, V, FLAT, GRAN>(c, t, l, h, to, k, d, dz[k], rA, rrB);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 // sums of a chunk per channel, in turns of GRAD_PACKS packs per lane, the next turn's on their way
-template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     constexpr int NV = GRAD_PACKS;
     extern __shared__ float lds[];
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
         xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
         gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
     }
-    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    const Channels<V, FLAT, GRAN> h(c, t, l);
     float s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
@@ -297,23 +297,24 @@ __device__ __forceinline__ void add_parameters(const BackwardCall& f, uint32_t b
     }
 }
 
-// dx of an image read again, last tiles first (what the sums read last is what a cache still holds); behind the tiles, the parameters
-template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+// dx of an image read again, by the workgroups that read the same tiles for the sums, on the same XCD and the last first: those are what
+// its cache still holds.  Behind the tiles, the parameters.
+template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V, NV = APPLY_PACKS;
+    constexpr int A = V / GRAN, NV = GRAD_PACKS;
     extern __shared__ float lds[];
     if (blockIdx.x >= f.tiles) { add_parameters(f, blockIdx.x - f.tiles, lds); return; }
     const NormCall& c = f.n;
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, true, f.tiles);
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys), to(c, t, l, c.outs);
-    typename Pack<E, V>::type xv[NV], gv[NV];
+    typename Pack<E, V>::type xn[NV], gn[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
-        gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
+        xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
+        gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, t.nv - NV + k);
     }
-    const Channels<V, FLAT, WHOLE_PACK> h(c, t, l);
+    const Channels<V, FLAT, GRAN> h(c, t, l);
     float rA[A], rrB[A];
     if (f.group_sums) {
 #pragma unroll
@@ -322,15 +323,33 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
             rrB[a] = h.rstd[a] * h.rstd[a] * f.group_sums[2 * (h.first_group + h.group[a]) + 1];
         }
     } else {
+        // every workgroup adds up the chunks of its channels, JOINED_PARTS of them per lane at most
         const SumSpace s(lds, 0, t.channels, blockDim.x);
+        const int left = c.channels - (int)l.block * t.channels, sums = t.channels < left ? t.channels : left;
         const float* parts = f.parts + (int64_t)l.image * f.chunks * 2 * c.channels + l.block * t.channels;
-        add_up(s, t.channels, f.chunks,
-               [&](int sum, int j, float& a0, float& a1) {
-                   if ((int)l.block * t.channels + sum >= c.channels) return;
-                   a0 += parts[(int64_t)j * 2 * c.channels + sum];
-                   a1 += parts[(int64_t)j * 2 * c.channels + c.channels + sum];
-               },
-               [](int, float, float) {});
+        const int shares = shares_of(blockDim.x, t.channels, f.chunks);
+        for (int i = threadIdx.x; i < t.channels * shares; i += blockDim.x) {
+            const int share = (int)((uint32_t)i / (uint32_t)t.channels), sum = i - share * t.channels;
+            float p0[JOINED_PARTS], p1[JOINED_PARTS], a0 = 0.f, a1 = 0.f;
+#pragma unroll
+            for (int j = 0; j < JOINED_PARTS; ++j) {
+                const int chunk = share + j * shares;
+                const float* p = parts + (chunk < f.chunks && sum < sums ? (int64_t)chunk * 2 * c.channels + sum : 0);
+                p0[j] = p[0];
+                p1[j] = p[c.channels];
+            }
+#pragma unroll
+            for (int j = 0; j < JOINED_PARTS; ++j) if (share + j * shares < f.chunks) { a0 += p0[j]; a1 += p1[j]; }
+            s.q0[i] = a0;
+            s.q1[i] = a1;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < t.channels; i += blockDim.x) {
+            float a0 = 0.f, a1 = 0.f;
+            for (int j = 0; j < shares; ++j) { a0 += s.q0[j * t.channels + i]; a1 += s.q1[j * t.channels + i]; }
+            s.c0[i] = a0;
+            s.c1[i] = a1;
+        }
         __syncthreads();
         group_means(c, t, l, s);
         __syncthreads();
@@ -340,11 +359,23 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
             rrB[a] = h.rstd[a] * h.rstd[a] * s.g0[t.groups + h.group[a]];
         }
     }
+    for (int turn = t.nv - NV; turn >= 0; turn -= NV) {
+        typename Pack<E, V>::type xv[NV], gv[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        float d[V], g[V];
-        h.template gradient<SILU, DROP>(c, l, k, xv[k], gv[k], d, g);
-        write_dx<E, V, FLAT, WHOLE_PACK>(c, t, l, h, to, k, d, g, rA, rrB);
+        for (int k = 0; k < NV; ++k) { xv[k] = xn[k]; gv[k] = gn[k]; }
+        if (turn) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn - NV + k);
+                gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, turn - NV + k);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float d[V], g[V];
+            h.template gradient<SILU, DROP>(c, l, turn + k, xv[k], gv[k], d, g);
+            write_dx<E, V, FLAT, GRAN>(c, t, l, h, to, turn + k, d, g, rA, rrB);
+        }
     }
 }
 
@@ -408,7 +439,7 @@ inline int64_t param_blocks(BackwardCall& f) {
     return c.sets * f.param_blocks;
 }
 
-template <class E, int V, bool FLAT, bool WHOLE_PACK>
+template <class E, int V, bool FLAT, int GRAN>
 hipError_t backward_twice(BackwardCall& f, const NormTiles& t, float* workspace, hipStream_t st) {
     const NormCall& c = f.n;
     const int64_t images = c.sets * c.images, groups = images * c.groups;
@@ -416,10 +447,10 @@ hipError_t backward_twice(BackwardCall& f, const NormTiles& t, float* workspace,
     f.chunks = t.sums.chunks;
     f.t = t.sums;
     return with_options(c, [&](auto silu, auto drop) {
-        hipError_t e = start_backward(norm_sums_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, 0, st);
+        hipError_t e = start_backward(norm_sums_kernel<E, V, FLAT, GRAN, silu.value, drop.value>, f, f.t.lds, 0, st);
         if (e != hipSuccess) return e;
         // The workgroups that write dx add up the chunks of their channels themselves, where that is little beside their tile.
-        if ((int64_t)f.chunks * t.apply.channels > JOINED_PARTS) {
+        if (t.apply.channels > t.apply.threads || f.chunks > JOINED_PARTS * shares_of(t.apply.threads, t.apply.channels, f.chunks)) {
             float* group_sums = workspace + images * f.chunks * 2 * c.channels;
             f.group_sums = group_sums;
             norm_group_kernel<256><<<dim3((unsigned)groups), dim3(256), 0, st>>>(f, group_sums);
@@ -429,14 +460,14 @@ hipError_t backward_twice(BackwardCall& f, const NormTiles& t, float* workspace,
         f.t = t.apply;
         const int64_t params = param_blocks(f);
         const size_t space = (size_t)(2 * f.t.threads + 2 * (f.t.channels + f.t.groups)) * sizeof(float);
-        return start_backward(norm_dx_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, space, params, st);
+        return start_backward(norm_dx_kernel<E, V, FLAT, GRAN, silu.value, drop.value>, f, space, params, st);
     });
 }
 
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK>
+template <class E, int V, int NV, bool FLAT, int GRAN>
 hipError_t backward_whole(BackwardCall& f, hipStream_t st) {
     return with_options(f.n, [&](auto silu, auto drop) {
-        return start_backward(norm_backward_kernel<E, V, NV, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, 0, st);
+        return start_backward(norm_backward_kernel<E, V, NV, FLAT, GRAN, silu.value, drop.value>, f, f.t.lds, 0, st);
     });
 }
 
@@ -447,18 +478,19 @@ template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles&
     f.dy_extent = extent_of(c, c.dys);
     const bool whole = tiles.whole.nv != 0;
     f.t = whole ? tiles.whole : tiles.sums;
-    return with_layout<E>(f.t, [&](auto vec, auto flat, auto whole_pack) {
+    return with_layout<E>(f.t, [&](auto vec, auto flat, auto gran) {
         constexpr int V = vec.value;
-        constexpr bool FLAT = flat.value, PACK = whole_pack.value;
-        if (!whole) return backward_twice<E, V, FLAT, PACK>(f, tiles, (float*)workspace, st);
+        constexpr int G = gran.value;
+        constexpr bool FLAT = flat.value;
+        if (!whole) return backward_twice<E, V, FLAT, G>(f, tiles, (float*)workspace, st);
         f.chunks = 1;
         const int64_t params = param_blocks(f);
         f.parts = params ? (float*)workspace : nullptr;
         hipError_t e;
         switch (f.t.nv) {
-            case 1: e = backward_whole<E, V, 1, FLAT, PACK>(f, st); break;
-            case 2: e = backward_whole<E, V, 2, FLAT, PACK>(f, st); break;
-            default: e = backward_whole<E, V, backward_packs(FLAT, V), FLAT, PACK>(f, st);
+            case 1: e = backward_whole<E, V, 1, FLAT, G>(f, st); break;
+            case 2: e = backward_whole<E, V, 2, FLAT, G>(f, st); break;
+            default: e = backward_whole<E, V, backward_packs(FLAT, V), FLAT, G>(f, st);
         }
         if (e != hipSuccess || !params) return e;
         norm_param_kernel<1024><<<dim3((unsigned)params), dim3(1024), 2 * 1024 * sizeof(float), st>>>(f);

@@ -32,10 +32,10 @@ __device__ __forceinline__ void join_parts(int terms, int lane, int team, float 
 }
 
 // sum[a], sq[a]: squared distances from mean[a] of a lane's NV packs, n of them valid (flat: of each element's)
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, class Valid>
-__device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[WHOLE_PACK ? 1 : V], float (&sq)[WHOLE_PACK ? 1 : V],
+template <class E, int V, int NV, bool FLAT, int GRAN, class Valid>
+__device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[V / GRAN], float (&sq)[V / GRAN],
                                              int (&count)[FLAT ? V : 1]) {
-    constexpr int A = WHOLE_PACK ? 1 : V;
+    constexpr int A = V / GRAN;
     float sum[A];
 #pragma unroll
     for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
@@ -45,47 +45,44 @@ __device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV]
     for (int k = 0; k < NV; ++k) {
         const int n = valid(k);
         if (n == V) {
-            if (WHOLE_PACK) sum[0] = pack_sum<V>(xv[k], sum[0]);
-            else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += to_float(xv[k][i]);
-            }
+            for (int a = 0; a < A; ++a) sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]);
         } else if (FLAT && n) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[WHOLE_PACK ? 0 : i] += i < n ? to_float(xv[k][i]) : 0.f;
+            for (int i = 0; i < V; ++i) sum[i / GRAN] += i < n ? to_float(xv[k][i]) : 0.f;
         }
 #pragma unroll
         for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] += n > a;
         keep_packed(xv[k]);
     }
 #pragma unroll
-    for (int a = 0; a < A; ++a) mean[a] = count[FLAT ? a : 0] ? sum[a] / (float)(count[FLAT ? a : 0] * (WHOLE_PACK ? V : 1)) : 0.f;
+    for (int a = 0; a < A; ++a) mean[a] = count[FLAT ? a : 0] ? sum[a] / (float)(count[FLAT ? a : 0] * GRAN) : 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int n = valid(k);
         if (n == V) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
+            for (int i = 0; i < V; ++i) { const float d = to_float(xv[k][i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
         } else if (FLAT && n) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]; sq[WHOLE_PACK ? 0 : i] += d * d; }
+            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(xv[k][i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
         }
         keep_packed(xv[k]);
     }
 }
 
 // The lanes' moments joined per group of the tile: done(unit, group in the tile, mean, squares) in one lane of each.  lds: 2 * lanes * A floats.
-template <int V, bool FLAT, bool WHOLE_PACK, class Done>
+template <int V, bool FLAT, int GRAN, class Done>
 __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Chunk<V, FLAT>& chunk, float* lds,
-                                           const float (&mean)[WHOLE_PACK ? 1 : V], const float (&sq)[WHOLE_PACK ? 1 : V], Done done) {
-    constexpr int A = WHOLE_PACK ? 1 : V;
+                                           const float (&mean)[V / GRAN], const float (&sq)[V / GRAN], Done done) {
+    constexpr int A = V / GRAN;
     const int threads = blockDim.x, D = c.channels / c.groups;
     float* part_mean = lds;                          // [lane][A]: [unit][place][channel or pack]
     float* part_sq = lds + threads * A;
 #pragma unroll
     for (int a = 0; a < A; ++a) { part_mean[threadIdx.x * A + a] = mean[a]; part_sq[threadIdx.x * A + a] = sq[a]; }
     __syncthreads();
-    const int per = WHOLE_PACK ? D / V : D, slots = (FLAT ? c.channels : t.channels) / (WHOLE_PACK ? V : 1);
+    const int per = D / GRAN, slots = (FLAT ? c.channels : t.channels) / GRAN;
     const int places = FLAT ? t.cols * V / c.channels : t.lane_rows, terms = places * per, groups = t.units * t.groups;
     const int team = team_of(threads, groups, terms), lane = threadIdx.x % team;
     for (int g = threadIdx.x / team; g < groups; g += threads / team) {
@@ -95,7 +92,7 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
         const auto slot = [&](int j) { const int r = place(j); return r * slots + j - r * per; };
         float m, q;
         join_parts(terms, lane, team, chunk.positions * (float)D,
-                   [&](int j) { return (float)(chunk.rounds_of(FLAT ? slot(j) + in * per : place(j)) * (WHOLE_PACK ? V : 1)); },
+                   [&](int j) { return (float)(chunk.rounds_of(FLAT ? slot(j) + in * per : place(j)) * GRAN); },
                    [&](int j) { return part_mean[base + slot(j)]; }, [&](int j) { return part_sq[base + slot(j)]; }, &m, &q);
         if (lane == 0) done(unit, in, m, q);
     }
@@ -112,40 +109,39 @@ __device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V,
 }
 
 // group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
-template <int V, bool FLAT, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
+template <int V, bool FLAT, int GRAN, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
 #pragma unroll
-    for (int a = 0; a < A; ++a) group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a, t.d_m, t.d_s) : 0;
+    for (int a = 0; a < A; ++a) group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.d_m, t.d_s) : 0;
 }
 
-// y from packs in registers
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
-__device__ __forceinline__ void write_results(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const typename Pack<E, V>::type (&xv)[NV],
-                                              const float (&mean)[WHOLE_PACK ? 1 : V], const float (&rstd)[WHOLE_PACK ? 1 : V], float (&w)[V], float (&b)[V]) {
-    const Place<V, FLAT> to(c, t, l, c.outs);
-    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
+template <int V, int GRAN, bool SILU, bool DROP>
+__device__ __forceinline__ void scale_parameters(const NormCall& c, const float (&rstd)[V / GRAN], float (&w)[V], float (&b)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i] *= rstd[WHOLE_PACK ? 0 : i];
+    for (int i = 0; i < V; ++i) w[i] *= rstd[i / GRAN];
     if (DROP && !SILU) {                             // (drop's scale commutes with ReLU)
 #pragma unroll
         for (int i = 0; i < V; ++i) { w[i] *= c.drop.scale; b[i] *= c.drop.scale; }
     }
+}
+
+// y of pack k
+template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
+__device__ __forceinline__ void write_result(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Place<V, FLAT>& to, int k, uint64_t number,
+                                             const typename Pack<E, V>::type& x, const float (&mean)[V / GRAN], const float (&w)[V], const float (&b)[V]) {
+    float v[V];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        float v[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            v[i] = activate<SILU>((to_float(xv[k][i]) - mean[WHOLE_PACK ? 0 : i]) * w[i] + b[i], c.floor);
-            if (DROP && SILU) v[i] *= c.drop.scale;
-        }
-        if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, v);
-        tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
+    for (int i = 0; i < V; ++i) {
+        v[i] = activate<SILU>((to_float(x[i]) - mean[i / GRAN]) * w[i] + b[i], c.floor);
+        if (DROP && SILU) v[i] *= c.drop.scale;
     }
+    if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number, v);
+    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
 }
 
 // images that a workgroup holds
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+template <class E, int V, int NV, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V;
+    constexpr int A = V / GRAN;
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
@@ -158,12 +154,12 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     const Chunk<V, FLAT> chunk(c, t, l);
     float mean[A], rstd[A], w[V], b[V];
     int group[A], count[FLAT ? V : 1];
-    lane_moments<E, V, NV, FLAT, WHOLE_PACK>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
+    lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
     lane_parameters(c, l, w, b);                     // (on their way while the groups are joined)
-    lane_groups<V, FLAT, A>(c, t, l, group);
+    lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
     float* stat = lds + 2 * blockDim.x * A;          // [unit][group of the tile] mean, then rstd
     const int groups = t.units * t.groups, D = c.channels / c.groups;
-    join_lanes<V, FLAT, WHOLE_PACK>(c, t, l, chunk, lds, mean, rstd, [&](int unit, int in, float m, float q) {
+    join_lanes<V, FLAT, GRAN>(c, t, l, chunk, lds, mean, rstd, [&](int unit, int in, float m, float q) {
         const float r = 1.f / sqrtf(q / (chunk.positions * (float)D) + c.eps);
         stat[unit * t.groups + in] = m;
         stat[groups + unit * t.groups + in] = r;
@@ -177,13 +173,17 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     __syncthreads();
 #pragma unroll
     for (int a = 0; a < A; ++a) { mean[a] = stat[l.unit * t.groups + group[a]]; rstd[a] = stat[groups + l.unit * t.groups + group[a]]; }
-    write_results<E, V, NV, FLAT, WHOLE_PACK, SILU, DROP>(c, t, l, xv, mean, rstd, w, b);
+    scale_parameters<V, GRAN, SILU, DROP>(c, rstd, w, b);
+    const Place<V, FLAT> to(c, t, l, c.outs);
+    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, k, number + k * number_step, xv[k], mean, w, b);
 }
 
 // moments of a chunk, in turns of SUM_PACKS packs per lane, the next turn's on their way
-template <class E, int V, bool FLAT, bool WHOLE_PACK>
+template <class E, int V, bool FLAT, int GRAN>
 __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V, NV = SUM_PACKS;
+    constexpr int A = V / GRAN, NV = SUM_PACKS;
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
@@ -208,10 +208,10 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
         }
         float m[A], q[A];
         int count[FLAT ? V : 1];
-        lane_moments<E, V, NV, FLAT, WHOLE_PACK>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
+        lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            const float n = (float)(count[FLAT ? a : 0] * (WHOLE_PACK ? V : 1)), old = (float)(before[FLAT ? a : 0] * (WHOLE_PACK ? V : 1));
+            const float n = (float)(count[FLAT ? a : 0] * GRAN), old = (float)(before[FLAT ? a : 0] * GRAN);
             const float share = n > 0.f ? n / (n + old) : 0.f, d = m[a] - mean[a];
             mean[a] += d * share;
             sq[a] += q[a] + d * d * (old * share);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
         for (int a = 0; a < (FLAT ? V : 1); ++a) before[a] += count[a];
     }
     const Chunk<V, FLAT> chunk(c, t, l);
-    join_lanes<V, FLAT, WHOLE_PACK>(c, t, l, chunk, lds, mean, sq, [&](int unit, int in, float m, float q) {
+    join_lanes<V, FLAT, GRAN>(c, t, l, chunk, lds, mean, sq, [&](int unit, int in, float m, float q) {
         const int g = (int)l.block * t.groups + in;
         if (g >= c.groups) return;
         float* to = f.parts + (((int64_t)l.image * c.groups + g) * t.chunks + l.chunk) * 2;
@@ -229,64 +229,89 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
     });
 }
 
-__device__ __forceinline__ void join_chunks(const float* parts, int chunks, float whole, float last, int lane, int team, float* mean, float* squares) {
-    const float2* p = (const float2*)parts;
-    join_parts(chunks, lane, team, whole * (float)(chunks - 1) + last, [&](int j) { return j < chunks - 1 ? whole : last; },
-               [&](int j) { return p[j].x; }, [&](int j) { return p[j].y; }, mean, squares);
-}
-
 // mean and 1/sqrt(v + eps) of a group from its chunks: a wavefront per group
 template <int T>
 __global__ void __launch_bounds__(T) norm_join_kernel(ForwardCall f, int64_t groups, float* mean, float* rstd) {
     const int64_t g = (int64_t)blockIdx.x * (T / 64) + threadIdx.x / 64;
     if (g >= groups) return;
     float m, q;
-    join_chunks(f.parts + 2 * g * f.chunks, f.chunks, f.whole, f.last, threadIdx.x % 64, 64, &m, &q);
+    const float2* p = (const float2*)f.parts + g * f.chunks;
+    const float all = f.whole * (float)(f.chunks - 1) + f.last;
+    join_parts(f.chunks, threadIdx.x % 64, 64, all, [&](int j) { return j < f.chunks - 1 ? f.whole : f.last; },
+               [&](int j) { return p[j].x; }, [&](int j) { return p[j].y; }, &m, &q);
     if (threadIdx.x % 64) return;
-    const float r = 1.f / sqrtf(q / (f.whole * (float)(f.chunks - 1) + f.last) + f.n.eps);
+    const float r = 1.f / sqrtf(q / all + f.n.eps);
     mean[g] = m;
     rstd[g] = r;
     if (f.n.mean) { f.n.mean[g] = m; f.n.rstd[g] = r; }
 }
 
-// Results of an image read again.  Last tiles first: what the sums read last is what a cache still holds.
-template <class E, int V, bool FLAT, bool WHOLE_PACK, bool SILU, bool DROP>
+// Results of an image read again, by the workgroups that read the same tiles for the sums, on the same XCD and the last first: those are
+// what its cache still holds.
+template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
-    constexpr int A = WHOLE_PACK ? 1 : V, NV = APPLY_PACKS;
+    constexpr int A = V / GRAN, NV = APPLY_PACKS;
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, true);
-    const Place<V, FLAT> from(c, t, l, c.xs);
-    typename Pack<E, V>::type xv[NV];
+    const Place<V, FLAT> from(c, t, l, c.xs), to(c, t, l, c.outs);
+    typename Pack<E, V>::type next[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+    for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
     float mean[A], rstd[A], w[V], b[V];
     int group[A];
     lane_parameters(c, l, w, b);
-    lane_groups<V, FLAT, A>(c, t, l, group);
+    lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
     const int64_t first = (int64_t)l.image * c.groups + l.block * t.groups;
     if (f.mean) {
 #pragma unroll
         for (int a = 0; a < A; ++a) { mean[a] = l.on ? f.mean[first + group[a]] : 0.f; rstd[a] = l.on ? f.rstd[first + group[a]] : 0.f; }
     } else {
+        // every workgroup joins the chunks of its groups, JOINED_PARTS of them per lane at most
         const int team = team_of(blockDim.x, t.groups, f.chunks), lane = threadIdx.x % team;
         for (int g = threadIdx.x / team; g < t.groups; g += blockDim.x / team) {
             if ((int)l.block * t.groups + g >= c.groups) break;
-            float m, q;
-            const int64_t at = (int64_t)l.image * c.groups + l.block * t.groups + g;
-            join_chunks(f.parts + 2 * at * f.chunks, f.chunks, f.whole, f.last, lane, team, &m, &q);
+            const float2* parts = (const float2*)f.parts + (first + g) * f.chunks;
+            float2 p[JOINED_PARTS];
+            float n[JOINED_PARTS];
+#pragma unroll
+            for (int j = 0; j < JOINED_PARTS; ++j) {
+                const int i = lane + j * team;
+                p[j] = parts[i < f.chunks ? i : 0];
+                n[j] = i < f.chunks - 1 ? f.whole : i < f.chunks ? f.last : 0.f;
+            }
+            const float all = f.whole * (float)(f.chunks - 1) + f.last;
+            float s = 0.f, q = 0.f;
+#pragma unroll
+            for (int j = 0; j < JOINED_PARTS; ++j) if (n[j] > 0.f) s += n[j] * p[j].x;
+            const float m = team_sum(s, team) / all;
+#pragma unroll
+            for (int j = 0; j < JOINED_PARTS; ++j) if (n[j] > 0.f) q += p[j].y + n[j] * (p[j].x - m) * (p[j].x - m);
+            q = team_sum(q, team);
             if (lane) continue;
-            const float r = 1.f / sqrtf(q / (f.whole * (float)(f.chunks - 1) + f.last) + c.eps);
+            const float r = 1.f / sqrtf(q / all + c.eps);
             lds[g] = m;
             lds[t.groups + g] = r;
-            if (c.mean && l.chunk == 0) { c.mean[at] = m; c.rstd[at] = r; }
+            if (c.mean && l.chunk == 0) { c.mean[first + g] = m; c.rstd[first + g] = r; }
         }
         __syncthreads();
 #pragma unroll
         for (int a = 0; a < A; ++a) { mean[a] = lds[group[a]]; rstd[a] = lds[t.groups + group[a]]; }
     }
-    write_results<E, V, NV, FLAT, WHOLE_PACK, SILU, DROP>(c, t, l, xv, mean, rstd, w, b);
+    scale_parameters<V, GRAN, SILU, DROP>(c, rstd, w, b);
+    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
+    for (int turn = t.nv - NV; turn >= 0; turn -= NV) {
+        typename Pack<E, V>::type xv[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) xv[k] = next[k];
+        if (turn) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn - NV + k);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, turn + k, number + (turn + k) * number_step, xv[k], mean, w, b);
+    }
 }
 
 // ---- launches ----
@@ -304,7 +329,7 @@ hipError_t start_forward(Kernel kernel, const ForwardCall& f, size_t lds, hipStr
     return hipGetLastError();
 }
 
-template <class E, int V, bool FLAT, bool WHOLE_PACK>
+template <class E, int V, bool FLAT, int GRAN>
 hipError_t forward_twice(ForwardCall& f, const NormTiles& t, float* workspace, hipStream_t st) {
     const NormCall& c = f.n;
     const int64_t groups = c.sets * c.images * c.groups, whole = chunk_positions(c, t.sums);
@@ -314,10 +339,10 @@ hipError_t forward_twice(ForwardCall& f, const NormTiles& t, float* workspace, h
     f.whole = (float)whole * D;
     f.last = (float)(c.positions - whole * (f.chunks - 1)) * D;
     f.t = t.sums;
-    hipError_t e = start_forward(norm_moments_kernel<E, V, FLAT, WHOLE_PACK>, f, f.t.lds, st);
+    hipError_t e = start_forward(norm_moments_kernel<E, V, FLAT, GRAN>, f, f.t.lds, st);
     if (e != hipSuccess) return e;
     // The workgroups that write the results join the chunks of their groups themselves, where that is little beside their tile.
-    if ((int64_t)f.chunks * t.apply.groups > JOINED_PARTS) {
+    if (f.chunks > JOINED_PARTS * team_of(t.apply.threads, t.apply.groups, f.chunks)) {
         float* mean = workspace + 2 * groups * f.chunks;
         f.mean = mean;
         f.rstd = mean + groups;
@@ -327,14 +352,14 @@ hipError_t forward_twice(ForwardCall& f, const NormTiles& t, float* workspace, h
     }
     f.t = t.apply;
     return with_options(c, [&](auto silu, auto drop) {
-        return start_forward(norm_apply_kernel<E, V, FLAT, WHOLE_PACK, silu.value, drop.value>, f, 2 * f.t.groups * sizeof(float), st);
+        return start_forward(norm_apply_kernel<E, V, FLAT, GRAN, silu.value, drop.value>, f, 2 * f.t.groups * sizeof(float), st);
     });
 }
 
-template <class E, int V, int NV, bool FLAT, bool WHOLE_PACK>
+template <class E, int V, int NV, bool FLAT, int GRAN>
 hipError_t forward_whole(const ForwardCall& f, hipStream_t st) {
     return with_options(f.n, [&](auto silu, auto drop) {
-        return start_forward(norm_forward_kernel<E, V, NV, FLAT, WHOLE_PACK, silu.value, drop.value>, f, f.t.lds, st);
+        return start_forward(norm_forward_kernel<E, V, NV, FLAT, GRAN, silu.value, drop.value>, f, f.t.lds, st);
     });
 }
 
@@ -344,16 +369,17 @@ template <class E> hipError_t tiled_forward(const NormCall& c, const NormTiles& 
     f.x_extent = extent_of(c, c.xs);
     const bool whole = tiles.whole.nv != 0;
     f.t = whole ? tiles.whole : tiles.sums;
-    return with_layout<E>(f.t, [&](auto vec, auto flat, auto whole_pack) {
+    return with_layout<E>(f.t, [&](auto vec, auto flat, auto gran) {
         constexpr int V = vec.value;
-        constexpr bool FLAT = flat.value, PACK = whole_pack.value;
-        if (!whole) return forward_twice<E, V, FLAT, PACK>(f, tiles, (float*)workspace, st);
+        constexpr int G = gran.value;
+        constexpr bool FLAT = flat.value;
+        if (!whole) return forward_twice<E, V, FLAT, G>(f, tiles, (float*)workspace, st);
         switch (f.t.nv) {
-            case 1: return forward_whole<E, V, 1, FLAT, PACK>(f, st);
-            case 2: return forward_whole<E, V, 2, FLAT, PACK>(f, st);
-            case 4: return forward_whole<E, V, 4, FLAT, PACK>(f, st);
-            case 8: return forward_whole<E, V, 8, FLAT, PACK>(f, st);
-            default: return forward_whole<E, V, FLAT ? FLAT_PACKS : FORWARD_PACKS, FLAT, PACK>(f, st);
+            case 1: return forward_whole<E, V, 1, FLAT, G>(f, st);
+            case 2: return forward_whole<E, V, 2, FLAT, G>(f, st);
+            case 4: return forward_whole<E, V, 4, FLAT, G>(f, st);
+            case 8: return forward_whole<E, V, 8, FLAT, G>(f, st);
+            default: return forward_whole<E, V, FLAT ? FLAT_PACKS : FORWARD_PACKS, FLAT, G>(f, st);
         }
     });
 }

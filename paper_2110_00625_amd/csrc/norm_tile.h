@@ -20,7 +20,8 @@ namespace kavg {
 
 struct Tile {
     int nv, vec;             // packs per lane, elements per pack
-    bool flat, whole_pack;   // whole_pack: a pack lies in one group
+    bool flat;
+    int gran;                // elements of a pack that always lie in one group: all, half of them, or 1
     int threads, units;      // lanes of a workgroup, images of a workgroup
     int cols, lane_rows;     // packs per row, rows that the lanes of a unit cover together
     int channels, groups;    // of a tile
@@ -42,7 +43,7 @@ constexpr int SUM_PACKS = 4;       // of a turn of the forward sums, which holds
 constexpr int GRAD_PACKS = 2;      // of a turn of the backward sums
 constexpr int APPLY_PACKS = 4;
 
-constexpr int JOINED_PARTS = 2048; // chunks times groups that the workgroups of the results join themselves
+constexpr int JOINED_PARTS = 4;    // chunks per lane that the workgroups of the results join themselves
 constexpr size_t LDS_PLAIN = 64 * 1024;      // more than that has to be asked for
 
 // elements of a tensor from its first to its last
@@ -55,15 +56,25 @@ bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t)
 // values of a group in a whole chunk, in positions
 inline int64_t chunk_positions(const NormCall& c, const Tile& t) { return (int64_t)t.nv * (t.flat ? (int64_t)t.cols * t.vec / c.channels : t.lane_rows); }
 
+// lanes that add up `terms` terms each of `sums` sums together: a power of two, at most a wavefront
+KAVG_FD int team_of(int threads, int sums, int terms) {
+    int team = 64;
+    while (team > 1 && (team / 2 >= terms || threads / team < sums)) team /= 2;
+    return team;
+}
+
 template <class E> hipError_t tiled_forward(const NormCall& c, const NormTiles& t, void* workspace, hipStream_t st);
 template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles& t, void* workspace, hipStream_t st);
 
-// f(constants: elements of a pack, flat, whole packs) of a tile
+// f(constants: elements of a pack, flat, elements of it in one group) of a tile
 template <class E, class F> hipError_t with_layout(const Tile& t, F f) {
-    constexpr std::integral_constant<int, 16 / (int)sizeof(E)> pack = {};
-    if (t.vec == 1) return f(std::integral_constant<int, 1>(), std::false_type(), std::true_type());
-    if (t.flat) return f(pack, std::true_type(), std::false_type());
-    return t.whole_pack ? f(pack, std::false_type(), std::true_type()) : f(pack, std::false_type(), std::false_type());
+    constexpr int V = 16 / (int)sizeof(E);
+    constexpr std::integral_constant<int, V> pack = {};
+    constexpr std::integral_constant<int, 1> one = {};
+    if (t.vec == 1) return f(one, std::false_type(), one);
+    if (t.flat) return f(pack, std::true_type(), one);
+    if (t.gran == V) return f(pack, std::false_type(), pack);
+    return t.gran == V / 2 ? f(pack, std::false_type(), std::integral_constant<int, V / 2>()) : f(pack, std::false_type(), one);
 }
 // f(constants: SiLU, dropout)
 template <class F> hipError_t with_options(const NormCall& c, F f) {
@@ -75,9 +86,10 @@ template <class F> hipError_t with_options(const NormCall& c, F f) {
 
 // Workgroup -> tile: workgroup g runs on XCD g mod 8, and tiles next to each other share lines of memory and parameters, so each
 // XCD takes a contiguous range of them.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t g, uint32_t n) {
-    const uint32_t per = n / 8, extra = n % 8, x = g % 8;
-    return x * per + (x < extra ? x : extra) + g / 8;
+// backwards: an XCD's range from its end.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t g, uint32_t n, bool backwards) {
+    const uint32_t per = n / 8, extra = n % 8, x = g % 8, at = g / 8;
+    return x * per + (x < extra ? x : extra) + (backwards ? per + (x < extra) - 1 - at : at);
 }
 
 // where a lane works
@@ -89,8 +101,7 @@ template <int V, bool FLAT> struct Lane {
     int64_t run;                                    // flat: elements of an image
 
     __device__ __forceinline__ Lane(const NormCall& c, const Tile& t, bool backwards = false, uint32_t tiles = gridDim.x) {
-        uint32_t b = xcd_order(blockIdx.x, tiles);
-        if (backwards) b = tiles - 1 - b;
+        const uint32_t b = xcd_order(blockIdx.x, tiles, backwards);
         const uint32_t per_unit = t.cols * t.lane_rows;
         const uint32_t rest = b / (uint32_t)t.chunks;
         chunk = b - rest * t.chunks;
@@ -213,34 +224,24 @@ template <int V, bool FLAT> __device__ __forceinline__ void tile_mask(const Drop
     else drop_mask<V, false>(d, e, v);
 }
 
-// sum + the elements of a pack, in bf16 two at a time (exact products with one, fp32 sums)
-template <int V> __device__ __forceinline__ float pack_sum(typename Pack<float, V>::type v, float sum) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) sum += v[i];
-    return sum;
-}
-template <int V> __device__ __forceinline__ float pack_sum(typename Pack<__bf16, V>::type v, float sum) {
+// sum + N elements of a pack from the first-th on, in bf16 two at a time (exact products with one, fp32 sums)
+template <int N, class P> __device__ __forceinline__ float pack_sum(const P& v, int first, float sum) {
     typedef __bf16 pair __attribute__((ext_vector_type(2)));
-    if constexpr (V == 1) return sum + (float)v[0];
-    else {
+    if constexpr (sizeof(v[0]) == 2 && N > 1) {
         const pair ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
-        for (int i = 0; i < V; i += 2) { const pair p = {v[i], v[i + 1]}; sum = __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false); }
-        return sum;
+        for (int i = 0; i < N; i += 2) { const pair p = {v[first + i], v[first + i + 1]}; sum = __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += to_float(v[first + i]);
     }
+    return sum;
 }
 
 __device__ __forceinline__ float team_sum(float v, int team) {
     for (int m = team / 2; m; m /= 2) v += __shfl_xor(v, m);
     return v;
 }
-// lanes that add up `terms` terms each of `sums` sums together: a power of two, at most a wavefront
-__device__ __forceinline__ int team_of(int threads, int sums, int terms) {
-    int team = 64;
-    while (team > 1 && (team / 2 >= terms || threads / team < sums)) team /= 2;
-    return team;
-}
-
 #endif
 
 }  // namespace kavg

@@ -16,7 +16,7 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // LDS of the sums (whole tiles need no less)
 size_t lds_bytes(const Tile& t, bool backward) {
-    if (!backward) return (size_t)(2 * t.threads * (t.whole_pack ? 1 : t.vec) + 2 * t.units * t.groups) * sizeof(float);
+    if (!backward) return (size_t)(2 * t.threads * (t.vec / t.gran) + 2 * t.units * t.groups) * sizeof(float);
     return (size_t)(2 * t.threads * t.vec + 2 * t.threads + 2 * t.units * (t.channels + t.groups)) * sizeof(float);
 }
 
@@ -26,7 +26,7 @@ bool finish(const NormCall& c, bool backward, Tile* t) {
     fastdiv_make(t->cols * t->lane_rows, &t->unit_m, &t->unit_s);
     fastdiv_make(t->cols, &t->col_m, &t->col_s);
     fastdiv_make(D, &t->d_m, &t->d_s);
-    fastdiv_make(t->whole_pack ? D / t->vec : D, &t->per_m, &t->per_s);
+    fastdiv_make(D / t->gran, &t->per_m, &t->per_s);
     t->lds = lds_bytes(*t, backward);
     return t->lds <= 160 * 1024;
 }
@@ -49,10 +49,8 @@ bool twice(const NormCall& c, bool backward, const Tile& t, int64_t rows, NormTi
     n->sums = n->apply = t;
     n->sums.units = n->apply.units = 1;
     const int64_t turns = up(rows, (int64_t)turn * t.lane_rows), chunks = std::min(turns, up(SUM_GROUPS, images * t.blocks));
-    n->sums.nv = (int)(turn * up(turns, chunks));
-    n->sums.chunks = (int)up(rows, (int64_t)n->sums.nv * t.lane_rows);
-    n->apply.nv = APPLY_PACKS;
-    n->apply.chunks = (int)up(rows, (int64_t)APPLY_PACKS * t.lane_rows);
+    n->sums.nv = n->apply.nv = (int)(turn * up(turns, chunks));
+    n->sums.chunks = n->apply.chunks = (int)up(rows, (int64_t)n->sums.nv * t.lane_rows);
     return finish(c, backward, &n->sums) && finish(c, backward, &n->apply);
 }
 
@@ -63,7 +61,7 @@ bool rows_tiles(const NormCall& c, int vec, int elem, int most, bool backward, N
     const int64_t images = c.sets * c.images, pieces = c.channels / least;
     Tile t = {};
     t.vec = vec;
-    t.whole_pack = D % vec == 0;
+    t.gran = D % vec == 0 ? vec : D % (vec / 2) == 0 ? vec / 2 : 1;          // (vec = 1: the first)
     t.rows = (int)c.positions;
     // tiles of rows' segments of so many bytes, or of a piece if that is more
     const auto cut = [&](int64_t segment) {
@@ -99,6 +97,7 @@ bool flat_tiles(const NormCall& c, int vec, int most, bool backward, NormTiles* 
     const int64_t packs = up(run, vec);
     Tile t = {};
     t.flat = true;
+    t.gran = 1;
     t.vec = vec;
     t.channels = c.channels;
     t.groups = c.groups;
