@@ -2,7 +2,6 @@
 // (counter_stream.h), so the backward pass draws it again and nothing is stored.  Bound by memory: an element is read and written once,
 // and a draw of 64 bits serves four of them.
 #include "layers.h"
-#include "fastdiv.h"
 #include <cmath>
 
 namespace kavg {
@@ -20,7 +19,7 @@ constexpr int T = 256;
 // not divide its length, is the last V elements, of which the pack before has had `skip`: they are read for nothing and not written
 // (in place they may have changed by then).  No load stands behind a branch: a lane with nothing to do reads the last pack.
 template <class E, int U, bool ROWS, bool ALIGNED, bool RESIDUAL>
-__device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first, uint64_t per_row, uint32_t div_m, int div_s) {
+__device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first, uint64_t per_row, Divisor by_row) {
     constexpr int V = 16 / sizeof(E);
     typedef typename Pack<E, V>::type pack;
     const uint64_t total = per_row * c.rows;
@@ -37,7 +36,7 @@ __device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first,
         if (none) i = (uint32_t)(total - 1 - first);
         row[u] = 0;
         if (ROWS) {
-            const uint32_t r = fastdiv(pack0 + i, div_m, div_s);
+            const uint32_t r = divide(pack0 + i, by_row);
             row[u] = row0 + r;
             col[u] = (uint64_t)(pack0 + i - r * (uint32_t)per_row) * V;
         } else col[u] = (first + i) * V;
@@ -69,12 +68,12 @@ __device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first,
 }
 
 template <class E, int U, bool ROWS, bool ALIGNED, bool RESIDUAL>
-__global__ void __launch_bounds__(T) dropout_kernel(DropCall c, uint64_t per_row, uint32_t div_m, int div_s) {
+__global__ void __launch_bounds__(T) dropout_kernel(DropCall c, uint64_t per_row, Divisor by_row) {
     constexpr int V = 16 / sizeof(E);
     const uint64_t first = (uint64_t)blockIdx.x * (U * T);
-    if (ROWS) packs_of_lane<E, U, true, ALIGNED, RESIDUAL>(c, first, per_row, div_m, div_s);
-    else if (first + U * T <= (uint64_t)c.cols / V) packs_of_lane<E, U, false, true, RESIDUAL>(c, first, per_row, 0, 0);
-    else packs_of_lane<E, U, false, false, RESIDUAL>(c, first, per_row, 0, 0);     // the end of the tensor
+    if (ROWS) packs_of_lane<E, U, true, ALIGNED, RESIDUAL>(c, first, per_row, by_row);
+    else if (first + U * T <= (uint64_t)c.cols / V) packs_of_lane<E, U, false, true, RESIDUAL>(c, first, per_row, by_row);
+    else packs_of_lane<E, U, false, false, RESIDUAL>(c, first, per_row, by_row);     // the end of the tensor
 }
 
 // rows of fewer than V elements: an element per lane
@@ -91,12 +90,10 @@ __global__ void __launch_bounds__(T) dropout_short_kernel(DropCall c) {
 
 template <class E, int U, bool ROWS, bool ALIGNED>
 void start(const DropCall& c, uint64_t per_row, hipStream_t st) {
-    uint32_t m = 0;
-    int s = 0;
-    if (ROWS) fastdiv_make((uint32_t)per_row, &m, &s);
+    const Divisor by_row = ROWS ? divisor((uint32_t)per_row) : Divisor{0, 0};
     const dim3 grid((unsigned)((per_row * c.rows + U * T - 1) / (U * T)));
-    if (c.residual) dropout_kernel<E, U, ROWS, ALIGNED, true><<<grid, dim3(T), 0, st>>>(c, per_row, m, s);
-    else dropout_kernel<E, U, ROWS, ALIGNED, false><<<grid, dim3(T), 0, st>>>(c, per_row, m, s);
+    if (c.residual) dropout_kernel<E, U, ROWS, ALIGNED, true><<<grid, dim3(T), 0, st>>>(c, per_row, by_row);
+    else dropout_kernel<E, U, ROWS, ALIGNED, false><<<grid, dim3(T), 0, st>>>(c, per_row, by_row);
 }
 
 template <class E>

@@ -34,7 +34,7 @@ template <int V, bool FLAT, int GRAN> struct Channels {
         first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.d_m, t.d_s) : 0;
+            group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
             mean[a] = c.mean[first_group + group[a]];
             rstd[a] = c.rstd[first_group + group[a]];
         }
@@ -132,7 +132,7 @@ __device__ __forceinline__ void channel_sums(const BackwardCall& f, const Lane<V
     }
     __syncthreads();
     const int tc = t.channels, sums = t.units * tc, places = FLAT ? t.cols * V / tc : t.lane_rows, per_unit = t.cols * t.lane_rows * V;
-    const uint32_t image0 = l.image - l.unit, images = (uint32_t)(c.sets * c.images);
+    const uint32_t image0 = l.first_image, images = (uint32_t)(c.sets * c.images);
     add_up(s, sums, places,
            [&](int sum, int j, float& a0, float& a1) {
                const int unit = t.units > 1 ? sum / tc : 0, at = unit * per_unit + sum - unit * tc + j * tc;
@@ -152,7 +152,7 @@ __device__ __forceinline__ void channel_sums(const BackwardCall& f, const Lane<V
 template <int V, bool FLAT> __device__ __forceinline__ void group_means(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const SumSpace& s) {
     const int D = c.channels / c.groups, threads = blockDim.x, groups = t.units * t.groups, team = team_of(threads, groups, D), lane = threadIdx.x % team;
     const float n = (float)c.positions * (float)D;
-    const uint32_t image0 = l.image - l.unit, images = (uint32_t)(c.sets * c.images);
+    const uint32_t image0 = l.first_image, images = (uint32_t)(c.sets * c.images);
     for (int g = threadIdx.x / team; g < groups; g += threads / team) {
         const int unit = t.units > 1 ? g / t.groups : 0, in = (g - unit * t.groups) * D, ch0 = (int)l.block * t.channels + in;
         const uint32_t image = image0 + unit;
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     typename Pack<E, V>::type xv[NV], gv[NV];
     {
         const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
@@ -206,6 +206,8 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
         float d[V];
         h.template gradient<SILU, DROP>(c, l, k, xv[k], gv[k], d, dz[k]);
         add_pack<V, FLAT>(l.valid(t, k), d, dz[k], s0, s1);
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm volatile("" : "+v"(dz[k][i]));      // (finished, and no select left for later)
         keep_packed(xv[k]);
         __builtin_amdgcn_sched_barrier(0);           // (a pack's registers at a time)
     }
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
     typename Pack<E, V>::type xn[NV], gn[NV];
 #pragma unroll
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
     if (blockIdx.x >= f.tiles) { add_parameters(f, blockIdx.x - f.tiles, lds); return; }
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t, true, f.tiles);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(f.tiles, true));
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys), to(c, t, l, c.outs);
     typename Pack<E, V>::type xn[NV], gn[NV];
 #pragma unroll
@@ -490,7 +492,7 @@ template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles&
         switch (f.t.nv) {
             case 1: e = backward_whole<E, V, 1, FLAT, G>(f, st); break;
             case 2: e = backward_whole<E, V, 2, FLAT, G>(f, st); break;
-            default: e = backward_whole<E, V, backward_packs(FLAT, V), FLAT, G>(f, st);
+            default: e = backward_whole<E, V, backward_packs(G, V), FLAT, G>(f, st);
         }
         if (e != hipSuccess || !params) return e;
         norm_param_kernel<1024><<<dim3((unsigned)params), dim3(1024), 2 * 1024 * sizeof(float), st>>>(f);

@@ -88,7 +88,7 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
     for (int g = threadIdx.x / team; g < groups; g += threads / team) {
         const int unit = g / t.groups, in = g - unit * t.groups, base = unit * t.cols * t.lane_rows * A + in * per;
         // part j of the group: place j / per
-        const auto place = [&](int j) { return (int)fastdiv(j, t.per_m, t.per_s); };
+        const auto place = [&](int j) { return (int)divide(j, t.by_per); };
         const auto slot = [&](int j) { const int r = place(j); return r * slots + j - r * per; };
         float m, q;
         join_parts(terms, lane, team, chunk.positions * (float)D,
@@ -111,7 +111,7 @@ __device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V,
 // group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
 template <int V, bool FLAT, int GRAN, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
 #pragma unroll
-    for (int a = 0; a < A; ++a) group[a] = l.on ? fastdiv(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.d_m, t.d_s) : 0;
+    for (int a = 0; a < A; ++a) group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
 }
 
 template <int V, int GRAN, bool SILU, bool DROP>
@@ -145,12 +145,13 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t);
-    const Place<V, FLAT> from(c, t, l, c.xs);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     typename Pack<E, V>::type xv[NV];
+    {
+        const Place<V, FLAT> from(c, t, l, c.xs);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
-
+        for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+    }
     const Chunk<V, FLAT> chunk(c, t, l);
     float mean[A], rstd[A], w[V], b[V];
     int group[A], count[FLAT ? V : 1];
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
         const float r = 1.f / sqrtf(q / (chunk.positions * (float)D) + c.eps);
         stat[unit * t.groups + in] = m;
         stat[groups + unit * t.groups + in] = r;
-        const uint32_t image = l.image - l.unit + unit;
+        const uint32_t image = l.first_image + unit;
         const int g = (int)l.block * t.groups + in;
         if (c.mean && image < (uint32_t)(c.sets * c.images) && g < c.groups) {
             c.mean[(int64_t)image * c.groups + g] = m;
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     const Place<V, FLAT> from(c, t, l, c.xs);
     typename Pack<E, V>::type next[NV];
 #pragma unroll
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
     extern __shared__ float lds[];
     const NormCall& c = f.n;
     const Tile& t = f.t;
-    const Lane<V, FLAT> l(c, t, true);
+    const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x, true));
     const Place<V, FLAT> from(c, t, l, c.xs), to(c, t, l, c.outs);
     typename Pack<E, V>::type next[NV];
 #pragma unroll
@@ -319,13 +320,12 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
 template <class Kernel>
 hipError_t start_forward(Kernel kernel, const ForwardCall& f, size_t lds, hipStream_t st) {
     const Tile& t = f.t;
-    const int64_t images = f.n.sets * f.n.images, grid = (images + t.units - 1) / t.units * t.blocks * t.chunks;
-    if (grid >= (int64_t)1 << 31) return hipErrorInvalidConfiguration;
+    const int64_t images = f.n.sets * f.n.images, tiles = (images + t.units - 1) / t.units * t.blocks * t.chunks;
     if (lds > LDS_PLAIN) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    kernel<<<dim3((unsigned)grid), dim3(t.threads), lds, st>>>(f);
+    kernel<<<dim3((unsigned)tiles), dim3(t.threads), lds, st>>>(f);
     return hipGetLastError();
 }
 

@@ -13,7 +13,6 @@
 // for its results.  Small images share a workgroup (units).
 #pragma once
 #include "layers.h"
-#include "fastdiv.h"
 #include <type_traits>
 
 namespace kavg {
@@ -28,7 +27,8 @@ struct Tile {
     int blocks, chunks;      // tiles of an image: along its channels, along its rows
     int rows;                // of an image
     // divisions by lanes per unit, cols, channels per group, sums of a row per group (packs, or channels)
-    uint32_t unit_m, col_m, d_m, per_m; int unit_s, col_s, d_s, per_s;
+    // tiles along the rows and the channels, images of a learner
+    Divisor by_unit, by_cols, by_d, by_per, by_chunks, by_blocks, by_images;
     size_t lds;
 };
 
@@ -38,7 +38,7 @@ struct NormTiles { Tile whole, sums, apply; };
 constexpr int FORWARD_PACKS = 16;  // the most packs per lane
 constexpr int FLAT_PACKS = 8;      // of a flat tile (its sums are per channel, and its last pack needs care: more spill)
 // of the backward pass, which holds x and dz (in fp32) of each
-constexpr int backward_packs(bool flat, int vec) { return flat && vec == 8 ? 2 : 4; }
+constexpr int backward_packs(int gran, int vec) { return gran == 1 && vec == 8 ? 2 : 4; }
 constexpr int SUM_PACKS = 4;       // of a turn of the forward sums, which holds two turns
 constexpr int GRAD_PACKS = 2;      // of a turn of the backward sums
 constexpr int APPLY_PACKS = 4;
@@ -84,43 +84,44 @@ template <class F> hipError_t with_options(const NormCall& c, F f) {
 
 #if defined(__HIPCC__)
 
-// Workgroup -> tile: workgroup g runs on XCD g mod 8, and tiles next to each other share lines of memory and parameters, so each
-// XCD takes a contiguous range of them.
-// backwards: an XCD's range from its end.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t g, uint32_t n, bool backwards) {
-    const uint32_t per = n / 8, extra = n % 8, x = g % 8, at = g / 8;
+// Workgroup g runs on XCD g mod 8, and tiles next to each other share lines of memory and parameters, so each XCD takes a contiguous range
+// of them.  backwards: its range from the end.
+__device__ __forceinline__ uint32_t tile_of_workgroup(uint32_t tiles, bool backwards = false) {
+    const uint32_t per = tiles / 8, extra = tiles % 8, x = blockIdx.x % 8, at = blockIdx.x / 8;
     return x * per + (x < extra ? x : extra) + (backwards ? per + (x < extra) - 1 - at : at);
 }
 
 // where a lane works
 template <int V, bool FLAT> struct Lane {
-    uint32_t chunk, block, image, unit, row, col;   // image: of all learners'; row, col: in the unit
-    uint32_t set, image_in_set;
+    uint32_t unit, row, col;                        // row, col: in the unit
+    bool in;                                        // the lane has a place in a unit
+    uint32_t chunk, block, first_image, image, set, image_in_set;     // of the tile; image: of all learners', of the lane's unit
     int first_channel;                              // of the lane's pack (flat: within the image's channels)
-    bool on;
-    int64_t run;                                    // flat: elements of an image
+    bool on;                                        // the place has an image and channels
+    int64_t run;                                    // elements of an image
 
-    __device__ __forceinline__ Lane(const NormCall& c, const Tile& t, bool backwards = false, uint32_t tiles = gridDim.x) {
-        const uint32_t b = xcd_order(blockIdx.x, tiles, backwards);
-        const uint32_t per_unit = t.cols * t.lane_rows;
-        const uint32_t rest = b / (uint32_t)t.chunks;
-        chunk = b - rest * t.chunks;
-        const uint32_t first = rest / (uint32_t)t.blocks;
-        block = rest - first * t.blocks;
-        unit = fastdiv(threadIdx.x, t.unit_m, t.unit_s);
-        uint32_t at = threadIdx.x - unit * per_unit;
-        image = first * t.units + unit;
-        on = unit < (uint32_t)t.units && image < (uint32_t)(c.sets * c.images);
-        if (!on) { at = 0; image = first * t.units; unit = 0; }
-        row = FLAT ? 0 : fastdiv(at, t.col_m, t.col_s);
+    __device__ __forceinline__ Lane(const NormCall& c, const Tile& t, uint32_t tile) {
+        unit = divide(threadIdx.x, t.by_unit);
+        in = unit < (uint32_t)t.units;
+        if (!in) unit = 0;
+        const uint32_t at = in ? threadIdx.x - unit * (t.cols * t.lane_rows) : 0;
+        row = FLAT ? 0 : divide(at, t.by_cols);
         col = at - row * t.cols;
         run = (int64_t)c.positions * c.channels;
+        const uint32_t rest = divide(tile, t.by_chunks);
+        chunk = tile - rest * t.chunks;
+        const uint32_t first = divide(rest, t.by_blocks);
+        block = rest - first * t.blocks;
+        first_image = first * t.units;
+        image = first_image + unit;
+        on = in && image < (uint32_t)(c.sets * c.images);
+        if (!on) image = first_image;
         if (FLAT) first_channel = (int)(col * V % (uint32_t)c.channels);
         else {
             first_channel = block * t.channels + col * V;
             if (first_channel >= c.channels) { on = false; first_channel = 0; }
         }
-        set = image / (uint32_t)c.images;
+        set = divide(image, t.by_images);
         image_in_set = image - set * (uint32_t)c.images;
     }
     __device__ __forceinline__ int channel(const NormCall& c, int i) const {
@@ -133,7 +134,9 @@ template <int V, bool FLAT> struct Lane {
     __device__ __forceinline__ int valid(const Tile& t, int k) const {
         const int r = image_row(t, k);
         if (!FLAT) return on && r < t.rows ? V : 0;
-        const int64_t left = run - ((int64_t)r * t.cols + col) * V;
+        uint32_t at = col;
+        asm volatile("" : "+v"(at));                // (asked again, worked out again: answers per pack and element would fill the scalar registers)
+        const int64_t left = run - ((int64_t)r * t.cols + at) * V;
         return !on || left <= 0 ? 0 : left < V ? (int)left : V;
     }
     // is k the last row of an image that is not made of whole rows (flat)?

@@ -23,10 +23,15 @@ size_t lds_bytes(const Tile& t, bool backward) {
 bool finish(const NormCall& c, bool backward, Tile* t) {
     const int D = c.channels / c.groups;
     t->threads = (int)up((int64_t)t->units * t->cols * t->lane_rows, 64) * 64;
-    fastdiv_make(t->cols * t->lane_rows, &t->unit_m, &t->unit_s);
-    fastdiv_make(t->cols, &t->col_m, &t->col_s);
-    fastdiv_make(D, &t->d_m, &t->d_s);
-    fastdiv_make(D / t->gran, &t->per_m, &t->per_s);
+    t->by_unit = divisor(t->cols * t->lane_rows);
+    t->by_cols = divisor(t->cols);
+    t->by_d = divisor(D);
+    t->by_per = divisor(D / t->gran);
+    t->by_chunks = divisor(t->chunks);
+    t->by_blocks = divisor(t->blocks);
+    t->by_images = divisor((uint32_t)c.images);
+    const int64_t tiles = up(c.sets * c.images, t->units) * t->blocks * t->chunks;
+    if (tiles >= (int64_t)1 << 30 || c.sets * c.images >= (int64_t)1 << 30) return false;      // (the divisors' range)
     t->lds = lds_bytes(*t, backward);
     return t->lds <= 160 * 1024;
 }
@@ -54,7 +59,7 @@ bool twice(const NormCall& c, bool backward, const Tile& t, int64_t rows, NormTi
     return finish(c, backward, &n->sums) && finish(c, backward, &n->apply);
 }
 
-bool rows_tiles(const NormCall& c, int vec, int elem, int most, bool backward, NormTiles* n) {
+bool rows_tiles(const NormCall& c, int vec, int elem, bool backward, NormTiles* n) {
     const int D = c.channels / c.groups;
     const int64_t least = std::lcm((int64_t)D, (int64_t)vec);          // channels of whole groups and whole packs
     if (least / vec > LANES || c.positions > (int64_t)1 << 30) return false;
@@ -63,6 +68,7 @@ bool rows_tiles(const NormCall& c, int vec, int elem, int most, bool backward, N
     t.vec = vec;
     t.gran = D % vec == 0 ? vec : D % (vec / 2) == 0 ? vec / 2 : 1;          // (vec = 1: the first)
     t.rows = (int)c.positions;
+    const int most = backward ? backward_packs(t.gran, vec) : FORWARD_PACKS;
     // tiles of rows' segments of so many bytes, or of a piece if that is more
     const auto cut = [&](int64_t segment) {
         const int64_t blocks = up(pieces, std::max<int64_t>(1, segment / (elem * least))), per = up(pieces, blocks);
@@ -127,9 +133,9 @@ size_t bytes_of(const NormCall& c, const NormTiles& t, bool backward) {
 
 bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t) {
     const int elem = c.dtype == KAVG_BF16 ? 2 : 4, vec = 16 / elem;
-    if (c.channels % vec == 0) return rows_tiles(c, vec, elem, backward ? backward_packs(false, vec) : FORWARD_PACKS, backward, t);
-    if (contiguous && flat_tiles(c, vec, backward ? backward_packs(true, vec) : FLAT_PACKS, backward, t)) return true;
-    return rows_tiles(c, 1, elem, backward ? backward_packs(false, 1) : FORWARD_PACKS, backward, t);
+    if (c.channels % vec == 0) return rows_tiles(c, vec, elem, backward, t);
+    if (contiguous && flat_tiles(c, vec, backward ? backward_packs(1, vec) : FLAT_PACKS, backward, t)) return true;
+    return rows_tiles(c, 1, elem, backward, t);
 }
 
 size_t norm_workspace(const NormCall& c, bool backward) {
