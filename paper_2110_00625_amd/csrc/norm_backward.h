@@ -22,7 +22,7 @@ struct BackwardCall {
     int param_wide, param_blocks;
 };
 
-// What a lane keeps of its channels: m, r, weight_c r, bias_c.
+// What a lane keeps of its channels: m, r, weight_c (then times r), bias_c.
 template <int V, bool FLAT, int GRAN> struct Channels {
     static constexpr int A = V / GRAN;
     float w[V], b[V], mean[A], rstd[A];
@@ -38,14 +38,25 @@ template <int V, bool FLAT, int GRAN> struct Channels {
             mean[a] = c.mean[first_group + group[a]];
             rstd[a] = c.rstd[first_group + group[a]];
         }
+        const Parameter weight(c.weight, c.weight_stride, l.set, &no_weight), bias(c.bias, c.bias_stride, l.set, &no_bias);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int ch = l.channel(c, i);
-            w[i] = (c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f) * rstd[i / GRAN];
-            b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
-        }
+        for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
         number = l.number(c, t);
         number_step = l.number_step(c, t);
+    }
+    // the tile's weights into LDS, by the lanes of the first place
+    __device__ __forceinline__ void share(const Tile& t, const Lane<V, FLAT>& l, float* lds) const {
+        if (l.on && l.row == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int ch = (int)l.col * V + i;
+                if (!FLAT || ch < t.channels) lds[l.unit * t.channels + ch] = w[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void scale() {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] *= rstd[i / GRAN];
     }
     // of pack k: x - m, and dz without drop's scale
     template <bool SILU, bool DROP, class P>
@@ -84,7 +95,8 @@ struct SumSpace {
     float *q0, *q1;          // [share][unit][channel]
     float *c0, *c1;          // [unit][channel]: sums of dz, dz xh
     float* g0;               // [unit][group]: A, then B
-    __device__ __forceinline__ SumSpace(float* lds, int packs, int sums, int threads) {
+    float* w;                // [unit][channel]: weights
+    __device__ __forceinline__ SumSpace(float* lds, int packs, int sums, int groups, int threads) {
         p0 = lds;
         p1 = p0 + packs;
         q0 = p1 + packs;
@@ -92,6 +104,7 @@ struct SumSpace {
         c0 = q1 + threads;
         c1 = c0 + sums;
         g0 = c1 + sums;
+        w = g0 + 2 * groups;
     }
 };
 
@@ -158,11 +171,10 @@ template <int V, bool FLAT> __device__ __forceinline__ void group_means(const No
         const uint32_t image = image0 + unit;
         float a0 = 0.f, a1 = 0.f;
         if (image < images && ch0 < c.channels) {
-            const float* weight = c.weight ? c.weight + (t.units > 1 ? image / (uint32_t)c.images : l.set) * c.weight_stride + ch0 : nullptr;
             for (int i = lane; i < D; i += team) {
-                const float wi = weight ? weight[i] : 1.f;
-                a0 += wi * s.c0[unit * t.channels + in + i];
-                a1 += wi * s.c1[unit * t.channels + in + i];
+                const int at = unit * t.channels + in + i;
+                a0 += s.w[at] * s.c0[at];
+                a1 += s.w[at] * s.c1[at];
             }
         }
         a0 = team_sum(a0, team);
@@ -188,6 +200,8 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     const NormCall& c = f.n;
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
+    // (loads return in order: what the first pack needs is asked for before the packs)
+    Channels<V, FLAT, GRAN> h(c, t, l);
     typename Pack<E, V>::type xv[NV], gv[NV];
     {
         const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
@@ -197,7 +211,9 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
             gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
         }
     }
-    const Channels<V, FLAT, GRAN> h(c, t, l);
+    const SumSpace s(lds, blockDim.x * V, t.units * t.channels, t.units * t.groups, blockDim.x);
+    h.share(t, l, s.w);
+    h.scale();
     float dz[NV][V], s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
@@ -211,7 +227,6 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
         keep_packed(xv[k]);
         __builtin_amdgcn_sched_barrier(0);           // (a pack's registers at a time)
     }
-    const SumSpace s(lds, blockDim.x * V, t.units * t.channels, blockDim.x);
     channel_sums(f, l, h, s, s0, s1);
     __syncthreads();
     group_means(c, t, l, s);
@@ -242,13 +257,14 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
+    Channels<V, FLAT, GRAN> h(c, t, l);
     typename Pack<E, V>::type xn[NV], gn[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
         gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
     }
-    const Channels<V, FLAT, GRAN> h(c, t, l);
+    h.scale();
     float s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
@@ -270,7 +286,7 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
             add_pack<V, FLAT>(l.valid(t, turn + k), d, g, s0, s1);
         }
     }
-    channel_sums(f, l, h, SumSpace(lds, blockDim.x * V, t.channels, blockDim.x), s0, s1);
+    channel_sums(f, l, h, SumSpace(lds, blockDim.x * V, t.channels, t.groups, blockDim.x), s0, s1);
 }
 
 // dweight and dbias: a learner's sums over its images and their chunks.  A workgroup (the largest power of two of its lanes): `wide`
@@ -310,41 +326,44 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, tile_of_workgroup(f.tiles, true));
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys), to(c, t, l, c.outs);
+    Channels<V, FLAT, GRAN> h(c, t, l);
     typename Pack<E, V>::type xn[NV], gn[NV];
+    const auto first_packs = [&] {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
-        gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, t.nv - NV + k);
-    }
-    const Channels<V, FLAT, GRAN> h(c, t, l);
+        for (int k = 0; k < NV; ++k) {
+            xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
+            gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, t.nv - NV + k);
+        }
+    };
     float rA[A], rrB[A];
     if (f.group_sums) {
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-            rA[a] = h.rstd[a] * f.group_sums[2 * (h.first_group + h.group[a])];
-            rrB[a] = h.rstd[a] * h.rstd[a] * f.group_sums[2 * (h.first_group + h.group[a]) + 1];
-        }
+        for (int a = 0; a < A; ++a) { rA[a] = f.group_sums[2 * (h.first_group + h.group[a])]; rrB[a] = f.group_sums[2 * (h.first_group + h.group[a]) + 1]; }
+        first_packs();
+        h.scale();
+#pragma unroll
+        for (int a = 0; a < A; ++a) { rA[a] *= h.rstd[a]; rrB[a] *= h.rstd[a] * h.rstd[a]; }
     } else {
         // every workgroup adds up the chunks of its channels, JOINED_PARTS of them per lane at most
-        const SumSpace s(lds, 0, t.channels, blockDim.x);
+        const SumSpace s(lds, 0, t.channels, t.groups, blockDim.x);
         const int left = c.channels - (int)l.block * t.channels, sums = t.channels < left ? t.channels : left;
         const float* parts = f.parts + (int64_t)l.image * f.chunks * 2 * c.channels + l.block * t.channels;
-        const int shares = shares_of(blockDim.x, t.channels, f.chunks);
-        for (int i = threadIdx.x; i < t.channels * shares; i += blockDim.x) {
-            const int share = (int)((uint32_t)i / (uint32_t)t.channels), sum = i - share * t.channels;
-            float p0[JOINED_PARTS], p1[JOINED_PARTS], a0 = 0.f, a1 = 0.f;
+        const int shares = shares_of(blockDim.x, t.channels, f.chunks), i = threadIdx.x;       // (t.channels * shares lanes at most)
+        const int share = (int)((uint32_t)i / (uint32_t)t.channels), sum = i - share * t.channels;
+        float p0[JOINED_PARTS], p1[JOINED_PARTS], a0 = 0.f, a1 = 0.f;
 #pragma unroll
-            for (int j = 0; j < JOINED_PARTS; ++j) {
-                const int chunk = share + j * shares;
-                const float* p = parts + (chunk < f.chunks && sum < sums ? (int64_t)chunk * 2 * c.channels + sum : 0);
-                p0[j] = p[0];
-                p1[j] = p[c.channels];
-            }
-#pragma unroll
-            for (int j = 0; j < JOINED_PARTS; ++j) if (share + j * shares < f.chunks) { a0 += p0[j]; a1 += p1[j]; }
-            s.q0[i] = a0;
-            s.q1[i] = a1;
+        for (int j = 0; j < JOINED_PARTS; ++j) {
+            const int chunk = share + j * shares;
+            const float* p = parts + (share < shares && chunk < f.chunks && sum < sums ? (int64_t)chunk * 2 * c.channels + sum : 0);
+            p0[j] = p[0];
+            p1[j] = p[c.channels];
         }
+        first_packs();                               // (behind the parts, which come first)
+        h.share(t, l, s.w);
+        h.scale();
+#pragma unroll
+        for (int j = 0; j < JOINED_PARTS; ++j) if (share + j * shares < f.chunks) { a0 += p0[j]; a1 += p1[j]; }
+        if (share < shares) { s.q0[i] = a0; s.q1[i] = a1; }
         __syncthreads();
         for (int i = threadIdx.x; i < t.channels; i += blockDim.x) {
             float a0 = 0.f, a1 = 0.f;
@@ -461,7 +480,7 @@ hipError_t backward_twice(BackwardCall& f, const NormTiles& t, float* workspace,
         }
         f.t = t.apply;
         const int64_t params = param_blocks(f);
-        const size_t space = (size_t)(2 * f.t.threads + 2 * (f.t.channels + f.t.groups)) * sizeof(float);
+        const size_t space = (size_t)(2 * f.t.threads + 3 * f.t.channels + 2 * f.t.groups) * sizeof(float);
         return start_backward(norm_dx_kernel<E, V, FLAT, GRAN, silu.value, drop.value>, f, space, params, st);
     });
 }
@@ -492,6 +511,7 @@ template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles&
         switch (f.t.nv) {
             case 1: e = backward_whole<E, V, 1, FLAT, G>(f, st); break;
             case 2: e = backward_whole<E, V, 2, FLAT, G>(f, st); break;
+            case 4: e = backward_whole<E, V, backward_packs(G, V) < 4 ? backward_packs(G, V) : 4, FLAT, G>(f, st); break;
             default: e = backward_whole<E, V, backward_packs(G, V), FLAT, G>(f, st);
         }
         if (e != hipSuccess || !params) return e;

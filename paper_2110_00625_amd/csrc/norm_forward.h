@@ -100,12 +100,9 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
 
 template <int V, bool FLAT>
 __device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
+    const Parameter weight(c.weight, c.weight_stride, l.set, &no_weight), bias(c.bias, c.bias_stride, l.set, &no_bias);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int ch = l.channel(c, i);
-        w[i] = c.weight ? c.weight[l.set * c.weight_stride + ch] : 1.f;
-        b[i] = c.bias ? c.bias[l.set * c.bias_stride + ch] : 0.f;
-    }
+    for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
 }
 
 // group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
@@ -257,23 +254,29 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
     const Tile& t = f.t;
     const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x, true));
     const Place<V, FLAT> from(c, t, l, c.xs), to(c, t, l, c.outs);
-    typename Pack<E, V>::type next[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
+    // (loads return in order: what the first pack needs is asked for before the packs)
     float mean[A], rstd[A], w[V], b[V];
     int group[A];
     lane_parameters(c, l, w, b);
     lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
+    typename Pack<E, V>::type next[NV];
+    const auto first_packs = [&] {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
+    };
     const int64_t first = (int64_t)l.image * c.groups + l.block * t.groups;
     if (f.mean) {
 #pragma unroll
         for (int a = 0; a < A; ++a) { mean[a] = l.on ? f.mean[first + group[a]] : 0.f; rstd[a] = l.on ? f.rstd[first + group[a]] : 0.f; }
+        first_packs();
     } else {
         // every workgroup joins the chunks of its groups, JOINED_PARTS of them per lane at most
         const int team = team_of(blockDim.x, t.groups, f.chunks), lane = threadIdx.x % team;
-        for (int g = threadIdx.x / team; g < t.groups; g += blockDim.x / team) {
-            if ((int)l.block * t.groups + g >= c.groups) break;
-            const float2* parts = (const float2*)f.parts + (first + g) * f.chunks;
+        const float all = f.whole * (float)(f.chunks - 1) + f.last;
+        bool asked = false;
+        for (int g = threadIdx.x / team; g < t.groups || !asked; g += blockDim.x / team) {
+            const bool there = g < t.groups && (int)l.block * t.groups + g < c.groups;
+            const float2* parts = (const float2*)f.parts + (there ? (first + g) * f.chunks : 0);
             float2 p[JOINED_PARTS];
             float n[JOINED_PARTS];
 #pragma unroll
@@ -282,7 +285,8 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
                 p[j] = parts[i < f.chunks ? i : 0];
                 n[j] = i < f.chunks - 1 ? f.whole : i < f.chunks ? f.last : 0.f;
             }
-            const float all = f.whole * (float)(f.chunks - 1) + f.last;
+            if (!asked) first_packs();               // (behind the parts, which come first)
+            asked = true;
             float s = 0.f, q = 0.f;
 #pragma unroll
             for (int j = 0; j < JOINED_PARTS; ++j) if (n[j] > 0.f) s += n[j] * p[j].x;
@@ -290,7 +294,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
 #pragma unroll
             for (int j = 0; j < JOINED_PARTS; ++j) if (n[j] > 0.f) q += p[j].y + n[j] * (p[j].x - m) * (p[j].x - m);
             q = team_sum(q, team);
-            if (lane) continue;
+            if (lane || !there) continue;
             const float r = 1.f / sqrtf(q / all + c.eps);
             lds[g] = m;
             lds[t.groups + g] = r;

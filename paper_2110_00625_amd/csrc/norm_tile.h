@@ -38,7 +38,7 @@ struct NormTiles { Tile whole, sums, apply; };
 constexpr int FORWARD_PACKS = 16;  // the most packs per lane
 constexpr int FLAT_PACKS = 8;      // of a flat tile (its sums are per channel, and its last pack needs care: more spill)
 // of the backward pass, which holds x and dz (in fp32) of each
-constexpr int backward_packs(int gran, int vec) { return gran == 1 && vec == 8 ? 2 : 4; }
+constexpr int backward_packs(int gran, int vec) { return vec == 8 ? gran == 1 ? 2 : 4 : 8; }
 constexpr int SUM_PACKS = 4;       // of a turn of the forward sums, which holds two turns
 constexpr int GRAD_PACKS = 2;      // of a turn of the backward sums
 constexpr int APPLY_PACKS = 4;
@@ -184,7 +184,8 @@ template <int V, bool FLAT> struct Chunk {
 // a branch.
 template <class E, int V, bool FLAT>
 __device__ __forceinline__ typename Pack<E, V>::type tile_load(const Tile& t, const Lane<V, FLAT>& l, const E* p, const Place<V, FLAT>& at0, int64_t extent, int k) {
-    const int64_t at = at0.first + (l.valid(t, k) ? k * at0.step : 0);
+    int64_t at = at0.first + (l.valid(t, k) ? k * at0.step : 0);
+    asm("" : "+v"(at));                              // (or the compiler makes that a copy of pack 0, behind a branch and a wait for it)
     if (!FLAT) return pack_load<E, V>(p + at);
     typename Pack<E, V>::type v = pack_load<E, V>(p + (at + V <= extent ? at : extent - V));
     if (l.ragged(t, k) && at + V > extent) {
@@ -208,6 +209,15 @@ __device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l
         for (int i = 0; i < V; ++i) if (i < n) p[i] = o[i];
     }
 }
+
+// a learner's parameters, or in their place one number for all channels: no load behind a branch
+static __device__ float no_weight = 1.f, no_bias = 0.f;      // (never written; not const, for constants lie in another kind of memory)
+struct Parameter {
+    const float* p;
+    int each;
+    __device__ __forceinline__ Parameter(const float* of, int64_t stride, uint32_t set, const float* none) : p(of ? of + set * stride : none), each(of ? 1 : 0) {}
+    __device__ __forceinline__ float operator[](int ch) const { return p[ch * each]; }
+};
 
 // Packs stay packed between their uses (the compiler would keep a bf16 pack's floats, twice the registers).
 template <class P> __device__ __forceinline__ void keep_packed(P& v) {

@@ -17,7 +17,7 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // LDS of the sums (whole tiles need no less)
 size_t lds_bytes(const Tile& t, bool backward) {
     if (!backward) return (size_t)(2 * t.threads * (t.vec / t.gran) + 2 * t.units * t.groups) * sizeof(float);
-    return (size_t)(2 * t.threads * t.vec + 2 * t.threads + 2 * t.units * (t.channels + t.groups)) * sizeof(float);
+    return (size_t)(2 * t.threads * t.vec + 2 * t.threads + t.units * (3 * t.channels + 2 * t.groups)) * sizeof(float);
 }
 
 bool finish(const NormCall& c, bool backward, Tile* t) {
