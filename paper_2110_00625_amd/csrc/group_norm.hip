@@ -129,22 +129,33 @@ hipError_t wide_backward(const NormCall& c, hipStream_t st) {
     return e;
 }
 
+hipError_t check(size_t want, const void* workspace, size_t bytes) {
+    if (want > bytes) return hipErrorOutOfMemory;
+    return want && (!workspace || ((uintptr_t)workspace & 15)) ? hipErrorInvalidValue : hipSuccess;
+}
+
 template <class E>
-hipError_t backward(const NormCall& c, void* workspace, hipStream_t st) {
+hipError_t backward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
     if (!c.sets) return hipSuccess;
     NormTiles t;
     const bool contiguous = c.xs.row == c.channels && c.dys.row == c.channels && c.outs.row == c.channels;
-    if (c.images && c.positions && norm_tiles(c, contiguous, true, &t)) return tiled_backward<E>(c, t, workspace, st);
+    if (c.images && c.positions && norm_tiles(c, contiguous, true, &t)) {
+        const hipError_t e = check(norm_workspace(c, t, true), workspace, bytes);
+        return e == hipSuccess ? tiled_backward<E>(c, t, workspace, st) : e;
+    }
     return c.silu ? wide_backward<E, true>(c, st) : wide_backward<E, false>(c, st);
 }
 
 template <class E>
-hipError_t forward(const NormCall& c, void* workspace, hipStream_t st) {
+hipError_t forward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
     const int64_t groups = c.sets * c.images * c.groups;
     if (!groups) return hipSuccess;
     NormTiles t;
     const bool contiguous = c.xs.row == c.channels && c.outs.row == c.channels;
-    if (c.positions && norm_tiles(c, contiguous, false, &t)) return tiled_forward<E>(c, t, workspace, st);
+    if (c.positions && norm_tiles(c, contiguous, false, &t)) {
+        const hipError_t e = check(norm_workspace(c, t, false), workspace, bytes);
+        return e == hipSuccess ? tiled_forward<E>(c, t, workspace, st) : e;
+    }
     const dim3 grid((unsigned)groups);
     if (c.silu) norm_wide_forward_kernel<E, true><<<grid, dim3(T), 0, st>>>(c);
     else norm_wide_forward_kernel<E, false><<<grid, dim3(T), 0, st>>>(c);
@@ -153,12 +164,12 @@ hipError_t forward(const NormCall& c, void* workspace, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_group_norm(const NormCall& c, void* workspace, hipStream_t st) {
-    return c.dtype == KAVG_BF16 ? forward<__bf16>(c, workspace, st) : forward<float>(c, workspace, st);
+hipError_t launch_group_norm(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
+    return c.dtype == KAVG_BF16 ? forward<__bf16>(c, workspace, bytes, st) : forward<float>(c, workspace, bytes, st);
 }
 
-hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, hipStream_t st) {
-    return c.dtype == KAVG_BF16 ? backward<__bf16>(c, workspace, st) : backward<float>(c, workspace, st);
+hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
+    return c.dtype == KAVG_BF16 ? backward<__bf16>(c, workspace, bytes, st) : backward<float>(c, workspace, bytes, st);
 }
 
 }  // namespace kavg

@@ -44,8 +44,9 @@ struct NormCall {
 };
 
 size_t norm_workspace(const NormCall& c, bool backward);
-hipError_t launch_group_norm(const NormCall& c, void* workspace, hipStream_t st);
-hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, hipStream_t st);
+// hipErrorOutOfMemory, hipErrorInvalidValue: a workspace too small, misaligned or not there, before anything is launched
+hipError_t launch_group_norm(const NormCall& c, void* workspace, size_t bytes, hipStream_t st);
+hipError_t launch_group_norm_backward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st);
 
 struct DropCall {
     int dtype;

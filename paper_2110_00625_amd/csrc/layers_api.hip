@@ -72,13 +72,9 @@ NormCall call_of(const kavg_norm* n, bool backward) {
     return c;
 }
 
-int workspace_ok(const kavg_norm* n, const NormCall& c, bool backward, const void* workspace, size_t bytes) {
-    const size_t want = empty(n) ? 0 : norm_workspace(c, backward);
-    if (want > bytes) return KAVG_ENOMEM;
-    return want && (!workspace || ((uintptr_t)workspace & 15)) ? KAVG_EINVAL : KAVG_OK;
+int status(hipError_t e) {
+    return e == hipSuccess ? KAVG_OK : e == hipErrorOutOfMemory ? KAVG_ENOMEM : e == hipErrorInvalidValue ? KAVG_EINVAL : KAVG_EDEVICE;
 }
-
-int status(hipError_t e) { return e == hipSuccess ? KAVG_OK : KAVG_EDEVICE; }
 
 }  // namespace
 
@@ -96,13 +92,12 @@ int kavg_group_norm(const kavg_norm* norm, const kavg_images* x, const float* we
     if (!norm_ok(norm) || !images_ok(norm, x, false) || !images_ok(norm, y, true) || !mean != !rstd) return KAVG_EINVAL;
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
     NormCall c = call_of(norm, false);
-    if (const int rc = workspace_ok(norm, c, false, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.out = y->data; c.outs = strides_of(norm, y);
     c.weight = weight; c.weight_stride = weight_stride;
     c.bias = bias; c.bias_stride = bias_stride;
     c.mean = mean; c.rstd = rstd;
-    return status(launch_group_norm(c, workspace, (hipStream_t)hip_stream));
+    return status(launch_group_norm(c, workspace, workspace_bytes, (hipStream_t)hip_stream));
 }
 
 int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const kavg_images* x, const float* mean, const float* rstd,
@@ -114,7 +109,6 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
     if (!params_ok(norm, weight, weight_stride, false) || !params_ok(norm, bias, bias_stride, false)) return KAVG_EINVAL;
     if (!params_ok(norm, dweight, dweight_stride, true) || !params_ok(norm, dbias, dbias_stride, true)) return KAVG_EINVAL;
     NormCall c = call_of(norm, true);
-    if (const int rc = workspace_ok(norm, c, true, workspace, workspace_bytes)) return rc;
     c.x = x->data; c.xs = strides_of(norm, x);
     c.dy = dy->data; c.dys = strides_of(norm, dy);
     c.out = dx->data; c.outs = strides_of(norm, dx);
@@ -123,7 +117,7 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
     c.mean = const_cast<float*>(mean); c.rstd = const_cast<float*>(rstd);
     c.dweight = dweight; c.dweight_stride = dweight_stride;
     c.dbias = dbias; c.dbias_stride = dbias_stride;
-    return status(launch_group_norm_backward(c, workspace, (hipStream_t)hip_stream));
+    return status(launch_group_norm_backward(c, workspace, workspace_bytes, (hipStream_t)hip_stream));
 }
 
 int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride, int64_t rows,

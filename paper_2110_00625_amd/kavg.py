@@ -264,14 +264,22 @@ def _norm(x, groups, eps, activation, drop, seed, site):
         _bad(str(e))
 
 
-def _workspace(norm, backward, x):
+def _workspace(norm, backward, x, like):
+    """(block, its address, its bytes); like: a float32 tensor of x's device, or None."""
     n = ctypes.c_size_t(0)
     if _lib.kavg_group_norm_workspace(norm, backward, ctypes.byref(n)) != KAVG_OK:
         _bad("kavg_group_norm rejected its sizes or options")
-    if not n.value:
+    n = n.value
+    if not n:
         return None, None, 0
-    block = _torch_module.empty(n.value, dtype=_torch_module.uint8, device=x.device)
-    return block, block.data_ptr(), n.value
+    block = like.new_empty((n + 3) // 4) if like is not None else _torch_module.empty(n, dtype=_torch_module.uint8, device=x.device)
+    return block, block.data_ptr(), n
+
+
+def _gradient(given, of):
+    if given is not None or of is None:
+        return given
+    return _torch_module.empty_like(of) if of.is_contiguous() else of.new_empty(of.shape)
 
 
 def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE, drop=0.0, seed=0, site=0, stats=False, out=None):
@@ -282,13 +290,15 @@ def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE,
     or [images, groups] in float32, which kavg_group_norm_backward wants."""
     torch = _torch_module or _torch()
     norm = _norm(x, groups, eps, activation, drop, seed, site)
-    block, at, nbytes = _workspace(norm, 0, x)
+    block, at, nbytes = _workspace(norm, 0, x, weight)
     y = _output(x, out)
     w, ws = _params(weight, x, "weight")
     b, bs = _params(bias, x, "bias")
     mean = rstd = m = r = None
     if stats:
-        mean, rstd = torch.empty((2,) + x.shape[:-2] + (groups,), dtype=torch.float32, device=x.device)
+        shape = x.shape[:-2] + (groups,)
+        mean = torch.empty(shape, dtype=torch.float32, device=x.device) if weight is None else weight.new_empty(shape)
+        rstd = torch.empty_like(mean)
         m, r = mean.data_ptr(), rstd.data_ptr()
     _call("kavg_group_norm", x, _lib.kavg_group_norm, norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), m, r, at, nbytes)
     return (y, mean, rstd) if stats else y
@@ -301,18 +311,16 @@ def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation
     learner's gradient vector; None where weight, bias are None)."""
     torch = _torch_module or _torch()
     norm = _norm(x, groups, 1.0, activation, drop, seed, site)       # (eps went into rstd)
-    block, at, nbytes = _workspace(norm, 1, x)
     _like(dy, x, "dy")
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous() or t.shape != x.shape[:-2] + (groups,):
-            _bad("%s is not what kavg_group_norm returned" % name)
+    shape = x.shape[:-2] + (groups,)
+    for t in (mean, rstd):
+        if t.shape != shape or t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous():
+            _bad("mean, rstd are not what kavg_group_norm returned")
+    block, at, nbytes = _workspace(norm, 1, x, mean)
     dx = _output(x, out)
     w, ws = _params(weight, x, "weight")
     b, bs = _params(bias, x, "bias")
-    if dweight is None and weight is not None:
-        dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
-    if dbias is None and bias is not None:
-        dbias = torch.empty(bias.shape, dtype=torch.float32, device=x.device)
+    dweight, dbias = _gradient(dweight, weight), _gradient(dbias, bias)
     gw, gws = _params(dweight, x, "dweight")
     gb, gbs = _params(dbias, x, "dbias")
     _call("kavg_group_norm_backward", x, _lib.kavg_group_norm_backward, norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(),

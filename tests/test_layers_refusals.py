@@ -62,6 +62,23 @@ def test_workspace_of_a_good_description(lib):
     assert lib.kavg_group_norm_workspace(None, 0, ctypes.byref(size)) == kavg.KAVG_EINVAL
 
 
+def test_workspaces_that_are_too_small(lib):
+    """Found before anything is launched."""
+    big = dict(sets=1, images=1, positions=1 << 20, channels=64, groups=8)
+    x = images()
+    for backward_ in (0, 1):
+        size = ctypes.c_size_t(0)
+        n = norm(**(big if backward_ == 0 else NORM))
+        assert lib.kavg_group_norm_workspace(n, backward_, ctypes.byref(size)) == kavg.KAVG_OK and size.value > 0
+
+        def call(block, nbytes):
+            if backward_:
+                return lib.kavg_group_norm_backward(n, x, x, AT, AT, AT, 8, AT, 8, x, AT, 8, AT, 8, block, nbytes, None)
+            return lib.kavg_group_norm(n, kavg._IMAGES.pack(AT, 0, 0, 64), AT, 0, AT, 0, kavg._IMAGES.pack(AT, 0, 0, 64), AT, AT, block, nbytes, None)
+        assert call(AT, size.value - 1) == kavg.KAVG_ENOMEM and call(None, 0) == kavg.KAVG_ENOMEM
+        assert call(None, size.value) == kavg.KAVG_EINVAL and call(AT + 4, size.value) == kavg.KAVG_EINVAL
+
+
 def test_operands_that_are_not_there(lib):
     E = kavg.KAVG_EINVAL
     for bad in (images(data=0), images(data=AT + 2), images(row=-8), images(images_=-32), images(sets=-96), images(row=1 << 50)):

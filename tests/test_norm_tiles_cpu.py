@@ -1,0 +1,179 @@
+"""Tiles of the group norm (csrc/norm_tile.h), on the host: the library's own choice for many shapes, and what its lanes then do,
+written down again here.  Every element of an image belongs to one lane's pack of one workgroup, no pack that is read leaves the
+tensor, and a workgroup stays within what the kernels are built for."""
+import ctypes
+import itertools
+import os
+
+import numpy as np
+import pytest
+
+from paper_2110_00625_amd import kavg
+
+I, L, P = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("set", L), ("image", L), ("row", L)]
+
+
+class NormCall(ctypes.Structure):
+    _fields_ = ([("dtype", I), ("silu", ctypes.c_bool), ("floor", ctypes.c_float), ("sets", L), ("images", L), ("positions", L),
+                 ("channels", I), ("groups", I), ("eps", ctypes.c_float), ("base", ctypes.c_uint64), ("threshold", ctypes.c_uint32),
+                 ("scale", ctypes.c_float), ("x", P), ("xs", Strides), ("dy", P), ("dys", Strides), ("out", P), ("outs", Strides)] +
+                [f for n in ("weight", "bias") for f in ((n, P), (n + "_stride", L))] + [("mean", P), ("rstd", P)] +
+                [f for n in ("dweight", "dbias") for f in ((n, P), (n + "_stride", L))])
+
+
+class Divisor(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_uint32), ("shift", I)]
+
+    def __call__(self, n):
+        n = np.asarray(n, dtype=np.uint64)
+        return ((n * np.uint64(self.m) >> np.uint64(32)) >> np.uint64(self.shift)).astype(np.int64) if self.m else n.astype(np.int64)
+
+
+class Tile(ctypes.Structure):
+    _fields_ = ([("nv", I), ("vec", I), ("flat", ctypes.c_bool)] +
+                [(n, I) for n in "gran threads units cols lane_rows channels groups blocks chunks rows".split()] +
+                [("by_" + n, Divisor) for n in "unit cols d per chunks blocks images".split()] + [("lds", ctypes.c_size_t)])
+
+
+class NormTiles(ctypes.Structure):
+    _fields_ = [("whole", Tile), ("sums", Tile), ("apply", Tile)]
+
+
+@pytest.fixture(scope="module")
+def tiles_of():
+    if not os.path.exists(kavg.LIB_PATH):
+        from paper_2110_00625_amd import build
+        build.build(verbose=False)
+    rule = kavg.load_library()._ZN4kavg10norm_tilesERKNS_8NormCallEbbPNS_9NormTilesE
+    rule.restype = ctypes.c_bool
+    rule.argtypes = [ctypes.POINTER(NormCall), ctypes.c_bool, ctypes.c_bool, ctypes.POINTER(NormTiles)]
+
+    def call(bf16, shape, contiguous, backward):
+        sets, images, positions, channels, groups = shape
+        c, t = NormCall(dtype=int(bf16), sets=sets, images=images, positions=positions, channels=channels, groups=groups), NormTiles()
+        return t if rule(ctypes.byref(c), contiguous, backward, ctypes.byref(t)) else None
+    return call
+
+
+def _walk(t, shape, most_lanes):
+    """(first element in the image or -1, elements of the pack that count, unit, image) of every lane and pack of all workgroups."""
+    sets, images, positions, channels, groups = shape
+    N, V, run = sets * images, t.vec, positions * channels
+    assert t.threads % 64 == 0 and t.threads <= most_lanes and t.units * t.cols * t.lane_rows <= t.threads
+    assert t.lds <= 160 * 1024
+    lane = np.arange(t.threads)
+    unit = t.by_unit(lane)
+    inside = unit < t.units
+    unit = np.where(inside, unit, 0)
+    at = np.where(inside, lane - unit * t.cols * t.lane_rows, 0)
+    row = 0 * at if t.flat else t.by_cols(at)
+    col = at - row * t.cols
+    tiles = -(-N // t.units) * t.blocks * t.chunks
+    assert tiles < 1 << 30
+    found = []
+    for tile in range(tiles):
+        rest = int(t.by_chunks(tile))
+        chunk = tile - rest * t.chunks
+        first = int(t.by_blocks(rest))
+        block = rest - first * t.blocks
+        assert 0 <= chunk < t.chunks and 0 <= block < t.blocks
+        image = first * t.units + unit
+        on = inside & (image < N)
+        image = np.where(on, image, first * t.units)
+        assert (image < N).all()
+        channel = 0 * col if t.flat else block * t.channels + col * V
+        on &= channel < channels
+        for k in range(t.nv):
+            r = (chunk * t.nv + k) * t.lane_rows + row
+            if t.flat:
+                start = (r * t.cols + col) * V
+                n = np.clip(run - start, 0, V)
+            else:
+                start = r * channels + channel
+                n = np.where(r < t.rows, V, 0)
+            n = np.where(on, n, 0)
+            found.append((image, np.where(n > 0, start, -1), n, block * t.groups + (0 if t.flat else (col * V) // (channels // groups)), channel))
+    return found
+
+
+def _check(t, shape, most_lanes):
+    sets, images, positions, channels, groups = shape
+    run, V, D = positions * channels, t.vec, channels // groups
+    count = np.zeros((sets * images, run), dtype=np.int32)
+    for image, start, n, group, channel in _walk(t, shape, most_lanes):
+        for i in range(V):
+            take = n > i
+            np.add.at(count, (image[take], start[take] + i), 1)
+        if not t.flat:                                       # a granule of a pack lies in one group
+            full = n > 0
+            for a in range(0, V, t.gran):
+                assert ((channel[full] + a) // D == (channel[full] + a + t.gran - 1) // D).all()
+            assert (channel[full] // D == group[full]).all()
+    assert (count == 1).all()
+    if t.flat:
+        assert t.cols * V % channels == 0 and sets * images * run >= V
+    else:
+        assert t.channels % D == 0 and t.channels % V == 0 and t.channels == t.cols * V
+
+
+SHAPES = [(1, 1, 1, 4, 2), (1, 3, 1, 1024, 16), (3, 2, 1, 40, 40), (1, 1, 2, 8, 1), (2, 3, 7, 12, 3), (3, 2, 33, 40, 5), (2, 2, 49, 91, 7), (1, 3, 5, 23, 23),
+          (1, 2, 30, 7, 1), (1, 2, 17, 2040, 8), (1, 1, 9, 2047, 23), (1, 2, 300, 320, 32), (2, 1, 1100, 128, 32), (1, 1, 4097, 8, 2), (1, 2, 1024, 64, 8),
+          (4, 33, 16, 32, 4), (1, 300, 3, 10, 5), (1, 1, 2500, 50, 5), (2, 1, 16383, 16, 4), (1, 1, 20000, 33, 3), (1, 1, 700, 513, 1), (1, 7, 50, 24, 8),
+          (2, 2, 129, 65, 13), (1, 1, 784, 40, 5), (1, 2, 1023, 20, 2), (1, 1, 513, 72, 3), (1, 1, 8191, 24, 3), (1, 5, 3, 5, 1), (1, 1, 100000, 1, 1), (1, 2, 1, 8, 8)]
+
+
+@pytest.mark.parametrize("bf16,backward,contiguous", list(itertools.product((False, True), repeat=3)))
+def test_every_element_once(tiles_of, bf16, backward, contiguous):
+    seen = set()
+    for shape in SHAPES:
+        t = tiles_of(bf16, shape, contiguous, backward)
+        if t is None:
+            seen.add("none")
+            continue
+        if t.whole.nv:
+            assert t.whole.chunks == 1 and t.whole.nv in ((1, 2, 4, 8) if backward else (1, 2, 4, 8, 16))
+            _check(t.whole, shape, 1024)
+        else:
+            assert t.sums.units == t.apply.units == 1 and (t.sums.nv, t.sums.chunks) == (t.apply.nv, t.apply.chunks)
+            assert t.sums.nv % (2 if backward else 4) == 0
+            _check(t.sums, shape, 512)
+        seen.add(("flat" if (t.whole.nv and t.whole.flat) or t.sums.flat else "rows", bool(t.whole.nv), t.whole.vec or t.sums.vec))
+    assert len(seen) >= (4 if contiguous else 3)
+
+
+def test_large_shapes_stay_in_range(tiles_of):
+    """Counts that reach the limits: 2^42 elements, many images, one image; no tile or its dividers out of range."""
+    rng = np.random.default_rng(1)
+    some = 0
+    for k in range(4000):
+        e = rng.uniform(0, 1, 5)
+        groups = int(2 ** (6 * e[0]))
+        channels = groups * int(2 ** (6 * e[1]))
+        sets, images = int(2 ** (4 * e[2])), int(2 ** (22 * e[3]))
+        positions = int(min(2 ** (30 * e[4]), 2 ** 42 / (sets * images * channels)))
+        if positions < 1 or sets * images * groups >= 1 << 31:
+            continue
+        for bf16, contiguous, backward in ((True, True, False), (False, False, True), (True, True, True)):
+            t = tiles_of(bf16, (sets, images, positions, channels, groups), contiguous, backward)
+            if t is None:
+                continue
+            some += 1
+            for u in (t.whole,) if t.whole.nv else (t.sums, t.apply):
+                assert 64 <= u.threads <= (1024 if t.whole.nv else 512) and u.lds <= 160 * 1024 and u.nv >= 1 and u.units >= 1
+                tiles = -(-sets * images // u.units) * u.blocks * u.chunks
+                assert tiles < 1 << 30
+                rows = -(-positions * channels // (u.cols * u.vec)) if u.flat else positions
+                assert u.rows == rows and (u.chunks - 1) * u.nv * u.lane_rows < rows <= u.chunks * u.nv * u.lane_rows
+                assert (rows + u.nv * u.lane_rows) < 1 << 31
+                d = channels // groups
+                n = np.array([0, 1, tiles - 1, rng.integers(0, tiles)])
+                assert (u.by_chunks(n) == n // u.chunks).all() and (u.by_blocks(n) == n // u.blocks).all()
+                m = np.array([0, sets * images - 1, rng.integers(0, sets * images)])
+                assert (u.by_images(m) == m // images).all()
+                q = np.arange(0, u.threads * u.vec)
+                assert (u.by_unit(q) == q // (u.cols * u.lane_rows)).all() and (u.by_cols(q) == q // u.cols).all() and (u.by_d(q) == q // d).all()
+    assert some > 3000
