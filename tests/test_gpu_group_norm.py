@@ -85,6 +85,17 @@ def test_against_64_bits(shape, dtype):
         _check(x, dy, w, b, shape[4], act, drop)
 
 
+# Many chunks for the lanes of few or many groups, packs of two halves in different groups, rows that are not whole lines, short and long,
+# images that just fit a workgroup.
+@pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
+@pytest.mark.parametrize("shape", [(1, 1, 20000, 64, 64), (1, 1, 20000, 33, 33), (2, 3, 50, 40, 10), (1, 1, 20000, 40, 10), (1, 3, 784, 40, 5), (1, 1, 5000, 320, 32),
+                                   (1, 1, 2048, 32, 4), (1, 1, 2049, 32, 4), (2, 300, 2, 16, 2), (1, 9, 1, 8, 8), (1, 2, 3, 8192, 1)], ids=lambda s: "-".join(map(str, s)))
+def test_edges_of_the_tiles(shape, dtype):
+    for k, (act, drop) in enumerate(((kavg.KAVG_ACT_SILU, 0.1), (kavg.KAVG_ACT_RELU, 0.0))):
+        x, dy, w, b = _inputs(shape, dtype, 31 * k + shape[2])
+        _check(x, dy, w, b, shape[4], act, drop)
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
 @pytest.mark.parametrize("shape", [(2, 3, 31, 24, 3), (1, 2, 1030, 64, 8), (2, 2, 20, 21, 3)], ids=lambda s: "-".join(map(str, s)))
 @pytest.mark.parametrize("pad,first", [(8, 0), (8, 8), (3, 1), (1, 0)])
