@@ -51,13 +51,13 @@ __device__ __forceinline__ void packs_of_lane(const DropCall& c, uint64_t first,
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        float v[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = to_float(xv[u][i]) * c.drop.scale;
-        if (c.drop.threshold) drop_mask<V, ALIGNED>(c.drop, row[u] * c.cols + col[u], v);
+        if (c.drop.threshold) drop_pack<E, V, ALIGNED>(c.drop, DropPlace(c.drop, row[u] * c.cols + col[u]), xv[u]);
         pack o;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = from_float<E>(RESIDUAL ? v[i] + to_float(rv[u][i]) : v[i]);
+        for (int i = 0; i < V; ++i) {
+            const float v = to_float(xv[u][i]) * c.drop.scale;
+            o[i] = from_float<E>(RESIDUAL ? v + to_float(rv[u][i]) : v);
+        }
         E* y = (E*)c.y + row[u] * c.y_stride + col[u];
         if (skip[u] == 0) pack_store<E, V>(y, o);
         else {

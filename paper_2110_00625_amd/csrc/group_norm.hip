@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(T) norm_wide_forward_kernel(NormCall c) {
         const int d = (int)(i % D), ch = c0 + d;
         const float xh = (to_float(x[s * c.xs.row + d]) - mean) * rstd;
         const float z = xh * (c.weight ? c.weight[at.set * c.weight_stride + ch] : 1.f) + (c.bias ? c.bias[at.set * c.bias_stride + ch] : 0.f);
-        float a = activate<SILU>(z, c.floor);
+        float a = SILU ? SILU_BACK * activate<true>(SILU_SCALE * z, 0.f) : activate<false>(z, c.floor);
         if (c.drop.threshold) a = drop_keeps(c.drop, first + (uint64_t)s * c.channels + d) ? a * c.drop.scale : 0.f;
         y[s * c.outs.row + d] = from_float<E>(a);
     }
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(T) norm_wide_forward_kernel(NormCall c) {
 template <class E, bool SILU>
 __device__ __forceinline__ float grad_z(const NormCall& c, float dy, float z, uint64_t e) {
     if (c.drop.threshold) dy = drop_keeps(c.drop, e) ? dy * c.drop.scale : 0.f;
-    return through_slope<SILU>(dy, z, c.floor);
+    return through_slope<SILU>(dy, SILU ? SILU_SCALE * z : z, c.floor);
 }
 
 // dx: one workgroup per group

@@ -22,27 +22,25 @@ struct BackwardCall {
     int param_wide, param_blocks;
 };
 
-// What a lane keeps of its channels: m, r, weight_c (then times r), bias_c.
+// What a lane keeps of its channels: m, r, weight_c (then times r, and with bias_c SiLU's factor), bias_c.
 template <int V, bool FLAT, int GRAN> struct Channels {
     static constexpr int A = V / GRAN;
     float w[V], b[V], mean[A], rstd[A];
     int group[A];                                    // in the tile
-    int64_t first_group;                             // of the tile (of a lane without work, whose groups may not exist: the first of all)
-    uint64_t number, number_step;
+    int64_t first_group;                             // of the tile
+    TileMask<V, FLAT> mask;
 
-    __device__ __forceinline__ Channels(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) {
-        first_group = l.on ? (int64_t)l.image * c.groups + l.block * t.groups : 0;
+    __device__ __forceinline__ Channels(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) : mask(c, t, l) {
+        first_group = l.groups_at(c, t);
 #pragma unroll
         for (int a = 0; a < A; ++a) {
             group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
             mean[a] = c.mean[first_group + group[a]];
             rstd[a] = c.rstd[first_group + group[a]];
         }
-        const Parameter weight(c.weight, c.weight_stride, l.set, &no_weight), bias(c.bias, c.bias_stride, l.set, &no_bias);
+        const Parameter weight(c.weight, l.set_at(t, c.weight_stride), &no_weight), bias(c.bias, l.set_at(t, c.bias_stride), &no_bias);
 #pragma unroll
         for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
-        number = l.number(c, t);
-        number_step = l.number_step(c, t);
     }
     // the tile's weights into LDS, by the lanes of the first place
     __device__ __forceinline__ void share(const Tile& t, const Lane<V, FLAT>& l, float* lds) const {
@@ -54,13 +52,22 @@ template <int V, bool FLAT, int GRAN> struct Channels {
             }
         }
     }
-    __device__ __forceinline__ void scale() {
+    template <bool SILU> __device__ __forceinline__ void scale() {
 #pragma unroll
-        for (int i = 0; i < V; ++i) w[i] *= rstd[i / GRAN];
+        for (int i = 0; i < V; ++i) {
+            w[i] *= rstd[i / GRAN];
+            if (SILU) { w[i] *= SILU_SCALE; b[i] *= SILU_SCALE; }
+        }
+    }
+    // what dx takes of its group: r A - m r^2 B and r^2 B
+    __device__ __forceinline__ void group_part(int a, float sum, float sum_xh, float (&rest)[A], float (&rrB)[A]) const {
+        rrB[a] = rstd[a] * rstd[a] * sum_xh;
+        rest[a] = rstd[a] * sum - mean[a] * rrB[a];
     }
     // of pack k: x - m, and dz without drop's scale
-    template <bool SILU, bool DROP, class P>
-    __device__ __forceinline__ void gradient(const NormCall& c, const Lane<V, FLAT>& l, int k, const P& x, const P& dy, float (&d)[V], float (&g)[V]) const {
+    template <class E, bool SILU, bool DROP>
+    __device__ __forceinline__ void gradient(const NormCall& c, int k, const typename Pack<E, V>::type& x, typename Pack<E, V>::type dy, float (&d)[V], float (&g)[V]) const {
+        if (DROP) mask.template drop<E>(c.drop, k, dy);
         float z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -68,7 +75,6 @@ template <int V, bool FLAT, int GRAN> struct Channels {
             z[i] = d[i] * w[i] + b[i];
             g[i] = to_float(dy[i]);
         }
-        if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number + k * number_step, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) g[i] = through_slope<SILU>(g[i], z[i], c.floor);
     }
@@ -116,6 +122,7 @@ __device__ __forceinline__ void add_up(const SumSpace& s, int sums, int terms, T
         for (int i = threadIdx.x; i < sums * shares; i += threads) {
             const int share = (int)((uint32_t)i / (uint32_t)sums), sum = i - share * sums;
             float a0 = 0.f, a1 = 0.f;
+#pragma unroll 4
             for (int j = share; j < terms; j += shares) term(sum, j, a0, a1);
             s.q0[i] = a0;
             s.q1[i] = a1;
@@ -124,8 +131,10 @@ __device__ __forceinline__ void add_up(const SumSpace& s, int sums, int terms, T
     }
     for (int i = threadIdx.x; i < sums; i += threads) {
         float a0 = 0.f, a1 = 0.f;
-        if (shares > 1) for (int j = 0; j < shares; ++j) { a0 += s.q0[j * sums + i]; a1 += s.q1[j * sums + i]; }
-        else for (int j = 0; j < terms; ++j) term(i, j, a0, a1);
+        if (shares > 1) {
+#pragma unroll 8
+            for (int j = 0; j < shares; ++j) { a0 += s.q0[j * sums + i]; a1 += s.q1[j * sums + i]; }
+        } else for (int j = 0; j < terms; ++j) term(i, j, a0, a1);
         s.c0[i] = a0;
         s.c1[i] = a1;
         done(i, a0, a1);
@@ -183,13 +192,15 @@ template <int V, bool FLAT> __device__ __forceinline__ void group_means(const No
     }
 }
 
-// dx of pack k from dz (without scale) and x - m
-template <class E, int V, bool FLAT, int GRAN>
+// dx of pack k from dz (without scale) and x: r weight_c dz - x r^2 B - (r A - m r^2 B).  (m r^2 B on its own is off by m r 2^-24 of r B, as is
+// what m's own rounding does to it.)
+template <bool SILU, class E, int V, bool FLAT, int GRAN>
 __device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Channels<V, FLAT, GRAN>& h, const Place<V, FLAT>& to, int k,
-                                         const float (&d)[V], float (&g)[V], const float (&rA)[V / GRAN], const float (&rrB)[V / GRAN]) {
+                                         const typename Pack<E, V>::type& x, float (&g)[V], const float (&rest)[V / GRAN], const float (&rrB)[V / GRAN]) {
+    const float scale = c.drop.scale * (SILU ? SILU_BACK : 1.f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) g[i] = g[i] * (h.w[i] * c.drop.scale) - rA[i / GRAN] - d[i] * rrB[i / GRAN];
-    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, g);
+    for (int i = 0; i < V; ++i) g[i] = __builtin_fmaf(g[i], h.w[i] * scale, -__builtin_fmaf(to_float(x[i]), rrB[i / GRAN], rest[i / GRAN]));
+    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, packed<E, V>(g));
 }
 
 // images that a workgroup holds
@@ -205,22 +216,21 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     typename Pack<E, V>::type xv[NV], gv[NV];
     {
         const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
-            gv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
-        }
+        load_packs<NV>(t, l, 0, [&](int k, auto whole) {
+            xv[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, k);
+            gv[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.dy, at, f.dy_extent, k);
+        });
     }
     const SumSpace s(lds, blockDim.x * V, t.units * t.channels, t.units * t.groups, blockDim.x);
     h.share(t, l, s.w);
-    h.scale();
+    h.template scale<SILU>();
     float dz[NV][V], s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         float d[V];
-        h.template gradient<SILU, DROP>(c, l, k, xv[k], gv[k], d, dz[k]);
+        h.template gradient<E, SILU, DROP>(c, k, xv[k], gv[k], d, dz[k]);
         add_pack<V, FLAT>(l.valid(t, k), d, dz[k], s0, s1);
 #pragma unroll
         for (int i = 0; i < V; ++i) asm volatile("" : "+v"(dz[k][i]));      // (finished, and no select left for later)
@@ -231,19 +241,13 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     __syncthreads();
     group_means(c, t, l, s);
     __syncthreads();
-    float rA[A], rrB[A];
+    float rest[A], rrB[A];
 #pragma unroll
-    for (int a = 0; a < A; ++a) {
-        rA[a] = h.rstd[a] * s.g0[l.unit * t.groups + h.group[a]];
-        rrB[a] = h.rstd[a] * h.rstd[a] * s.g0[(t.units + l.unit) * t.groups + h.group[a]];
-    }
+    for (int a = 0; a < A; ++a) h.group_part(a, s.g0[l.unit * t.groups + h.group[a]], s.g0[(t.units + l.unit) * t.groups + h.group[a]], rest, rrB);
     const Place<V, FLAT> to(c, t, l, c.outs);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        float d[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) d[i] = to_float(xv[k][i]) - h.mean[i / GRAN];
-        write_dx<E, V, FLAT, GRAN>(c, t, l, h, to, k, d, dz[k], rA, rrB);
+        write_dx<SILU, E, V, FLAT, GRAN>(c, t, l, h, to, k, xv[k], dz[k], rest, rrB);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -259,12 +263,14 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys);
     Channels<V, FLAT, GRAN> h(c, t, l);
     typename Pack<E, V>::type xn[NV], gn[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
-        gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, k);
-    }
-    h.scale();
+    const auto packs_from = [&](int first) {
+        load_packs<NV>(t, l, first, [&](int k, auto whole) {
+            xn[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, first + k);
+            gn[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.dy, at, f.dy_extent, first + k);
+        });
+    };
+    packs_from(0);
+    h.template scale<SILU>();
     float s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
@@ -272,17 +278,11 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
         typename Pack<E, V>::type xv[NV], gv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) { xv[k] = xn[k]; gv[k] = gn[k]; }
-        if (turn + NV < t.nv) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn + NV + k);
-                gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, turn + NV + k);
-            }
-        }
+        if (turn + NV < t.nv) packs_from(turn + NV);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float d[V], g[V];
-            h.template gradient<SILU, DROP>(c, l, turn + k, xv[k], gv[k], d, g);
+            h.template gradient<E, SILU, DROP>(c, turn + k, xv[k], gv[k], d, g);
             add_pack<V, FLAT>(l.valid(t, turn + k), d, g, s0, s1);
         }
     }
@@ -328,21 +328,21 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
     const Place<V, FLAT> from(c, t, l, c.xs), at(c, t, l, c.dys), to(c, t, l, c.outs);
     Channels<V, FLAT, GRAN> h(c, t, l);
     typename Pack<E, V>::type xn[NV], gn[NV];
-    const auto first_packs = [&] {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
-            gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, t.nv - NV + k);
-        }
+    const auto packs_from = [&](int first) {
+        load_packs<NV>(t, l, first, [&](int k, auto whole) {
+            xn[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, first + k);
+            gn[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.dy, at, f.dy_extent, first + k);
+        });
     };
-    float rA[A], rrB[A];
+    float rest[A], rrB[A];
     if (f.group_sums) {
+        float gA[A], gB[A];
 #pragma unroll
-        for (int a = 0; a < A; ++a) { rA[a] = f.group_sums[2 * (h.first_group + h.group[a])]; rrB[a] = f.group_sums[2 * (h.first_group + h.group[a]) + 1]; }
-        first_packs();
-        h.scale();
+        for (int a = 0; a < A; ++a) { gA[a] = f.group_sums[2 * (h.first_group + h.group[a])]; gB[a] = f.group_sums[2 * (h.first_group + h.group[a]) + 1]; }
+        packs_from(t.nv - NV);
+        h.template scale<SILU>();
 #pragma unroll
-        for (int a = 0; a < A; ++a) { rA[a] *= h.rstd[a]; rrB[a] *= h.rstd[a] * h.rstd[a]; }
+        for (int a = 0; a < A; ++a) h.group_part(a, gA[a], gB[a], rest, rrB);
     } else {
         // every workgroup adds up the chunks of its channels, JOINED_PARTS of them per lane at most
         const SumSpace s(lds, 0, t.channels, t.groups, blockDim.x);
@@ -358,9 +358,9 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
             p0[j] = p[0];
             p1[j] = p[c.channels];
         }
-        first_packs();                               // (behind the parts, which come first)
+        packs_from(t.nv - NV);                               // (behind the parts, which come first)
         h.share(t, l, s.w);
-        h.scale();
+        h.template scale<SILU>();
 #pragma unroll
         for (int j = 0; j < JOINED_PARTS; ++j) if (share + j * shares < f.chunks) { a0 += p0[j]; a1 += p1[j]; }
         if (share < shares) { s.q0[i] = a0; s.q1[i] = a1; }
@@ -375,27 +375,18 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
         group_means(c, t, l, s);
         __syncthreads();
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-            rA[a] = h.rstd[a] * s.g0[h.group[a]];
-            rrB[a] = h.rstd[a] * h.rstd[a] * s.g0[t.groups + h.group[a]];
-        }
+        for (int a = 0; a < A; ++a) h.group_part(a, s.g0[h.group[a]], s.g0[t.groups + h.group[a]], rest, rrB);
     }
     for (int turn = t.nv - NV; turn >= 0; turn -= NV) {
         typename Pack<E, V>::type xv[NV], gv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) { xv[k] = xn[k]; gv[k] = gn[k]; }
-        if (turn) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                xn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn - NV + k);
-                gn[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.dy, at, f.dy_extent, turn - NV + k);
-            }
-        }
+        if (turn) packs_from(turn - NV);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float d[V], g[V];
-            h.template gradient<SILU, DROP>(c, l, turn + k, xv[k], gv[k], d, g);
-            write_dx<E, V, FLAT, GRAN>(c, t, l, h, to, turn + k, d, g, rA, rrB);
+            h.template gradient<E, SILU, DROP>(c, turn + k, xv[k], gv[k], d, g);
+            write_dx<SILU, E, V, FLAT, GRAN>(c, t, l, h, to, turn + k, xv[k], g, rest, rrB);
         }
     }
 }

@@ -99,8 +99,8 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
 }
 
 template <int V, bool FLAT>
-__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
-    const Parameter weight(c.weight, c.weight_stride, l.set, &no_weight), bias(c.bias, c.bias_stride, l.set, &no_bias);
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
+    const Parameter weight(c.weight, l.set_at(t, c.weight_stride), &no_weight), bias(c.bias, l.set_at(t, c.bias_stride), &no_bias);
 #pragma unroll
     for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
 }
@@ -111,28 +111,32 @@ template <int V, bool FLAT, int GRAN, int A> __device__ __forceinline__ void lan
     for (int a = 0; a < A; ++a) group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
 }
 
+// weight times r; SiLU's factor into both, or drop's scale, which commutes with ReLU
 template <int V, int GRAN, bool SILU, bool DROP>
 __device__ __forceinline__ void scale_parameters(const NormCall& c, const float (&rstd)[V / GRAN], float (&w)[V], float (&b)[V]) {
+    const float scale = SILU ? SILU_SCALE : c.drop.scale;
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] *= rstd[i / GRAN];
-    if (DROP && !SILU) {                             // (drop's scale commutes with ReLU)
+    if (DROP || SILU) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) { w[i] *= c.drop.scale; b[i] *= c.drop.scale; }
+        for (int i = 0; i < V; ++i) { w[i] *= scale; b[i] *= scale; }
     }
 }
 
 // y of pack k
 template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
-__device__ __forceinline__ void write_result(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Place<V, FLAT>& to, int k, uint64_t number,
+__device__ __forceinline__ void write_result(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Place<V, FLAT>& to, int k, const TileMask<V, FLAT>& mask,
                                              const typename Pack<E, V>::type& x, const float (&mean)[V / GRAN], const float (&w)[V], const float (&b)[V]) {
+    const float after = SILU_BACK * (DROP ? c.drop.scale : 1.f);
     float v[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         v[i] = activate<SILU>((to_float(x[i]) - mean[i / GRAN]) * w[i] + b[i], c.floor);
-        if (DROP && SILU) v[i] *= c.drop.scale;
+        if (SILU) v[i] *= after;
     }
-    if (DROP) tile_mask<V, FLAT>(c.drop, l.run, number, v);
-    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, v);
+    typename Pack<E, V>::type o = packed<E, V>(v);
+    if (DROP) mask.template drop<E>(c.drop, k, o);
+    tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, o);
 }
 
 // images that a workgroup holds
@@ -146,14 +150,13 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     typename Pack<E, V>::type xv[NV];
     {
         const Place<V, FLAT> from(c, t, l, c.xs);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) xv[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+        load_packs<NV>(t, l, 0, [&](int k, auto whole) { xv[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, k); });
     }
     const Chunk<V, FLAT> chunk(c, t, l);
     float mean[A], rstd[A], w[V], b[V];
     int group[A], count[FLAT ? V : 1];
     lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
-    lane_parameters(c, l, w, b);                     // (on their way while the groups are joined)
+    lane_parameters(c, t, l, w, b);                     // (on their way while the groups are joined)
     lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
     float* stat = lds + 2 * blockDim.x * A;          // [unit][group of the tile] mean, then rstd
     const int groups = t.units * t.groups, D = c.channels / c.groups;
@@ -173,9 +176,9 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     for (int a = 0; a < A; ++a) { mean[a] = stat[l.unit * t.groups + group[a]]; rstd[a] = stat[groups + l.unit * t.groups + group[a]]; }
     scale_parameters<V, GRAN, SILU, DROP>(c, rstd, w, b);
     const Place<V, FLAT> to(c, t, l, c.outs);
-    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
+    const TileMask<V, FLAT> mask(c, t, l);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, k, number + k * number_step, xv[k], mean, w, b);
+    for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, k, mask, xv[k], mean, w, b);
 }
 
 // moments of a chunk, in turns of SUM_PACKS packs per lane, the next turn's on their way
@@ -188,8 +191,10 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
     const Lane<V, FLAT> l(c, t, tile_of_workgroup(gridDim.x));
     const Place<V, FLAT> from(c, t, l, c.xs);
     typename Pack<E, V>::type next[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, k);
+    const auto packs_from = [&](int first) {
+        load_packs<NV>(t, l, first, [&](int k, auto whole) { next[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, first + k); });
+    };
+    packs_from(0);
     float mean[A], sq[A];
     int before[FLAT ? V : 1];
 #pragma unroll
@@ -200,10 +205,7 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
         typename Pack<E, V>::type xv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) xv[k] = next[k];
-        if (turn + NV < t.nv) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn + NV + k);
-        }
+        if (turn + NV < t.nv) packs_from(turn + NV);
         float m[A], q[A];
         int count[FLAT ? V : 1];
         lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
@@ -257,18 +259,17 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
     // (loads return in order: what the first pack needs is asked for before the packs)
     float mean[A], rstd[A], w[V], b[V];
     int group[A];
-    lane_parameters(c, l, w, b);
+    lane_parameters(c, t, l, w, b);
     lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
     typename Pack<E, V>::type next[NV];
-    const auto first_packs = [&] {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, t.nv - NV + k);
+    const auto packs_from = [&](int first) {
+        load_packs<NV>(t, l, first, [&](int k, auto whole) { next[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, first + k); });
     };
-    const int64_t first = (int64_t)l.image * c.groups + l.block * t.groups;
+    const int64_t first = l.groups_at(c, t);
     if (f.mean) {
 #pragma unroll
         for (int a = 0; a < A; ++a) { mean[a] = l.on ? f.mean[first + group[a]] : 0.f; rstd[a] = l.on ? f.rstd[first + group[a]] : 0.f; }
-        first_packs();
+        packs_from(t.nv - NV);
     } else {
         // every workgroup joins the chunks of its groups, JOINED_PARTS of them per lane at most
         const int team = team_of(blockDim.x, t.groups, f.chunks), lane = threadIdx.x % team;
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
                 p[j] = parts[i < f.chunks ? i : 0];
                 n[j] = i < f.chunks - 1 ? f.whole : i < f.chunks ? f.last : 0.f;
             }
-            if (!asked) first_packs();               // (behind the parts, which come first)
+            if (!asked) packs_from(t.nv - NV);               // (behind the parts, which come first)
             asked = true;
             float s = 0.f, q = 0.f;
 #pragma unroll
@@ -305,17 +306,14 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
         for (int a = 0; a < A; ++a) { mean[a] = lds[group[a]]; rstd[a] = lds[t.groups + group[a]]; }
     }
     scale_parameters<V, GRAN, SILU, DROP>(c, rstd, w, b);
-    const uint64_t number = l.number(c, t), number_step = l.number_step(c, t);
+    const TileMask<V, FLAT> mask(c, t, l);
     for (int turn = t.nv - NV; turn >= 0; turn -= NV) {
         typename Pack<E, V>::type xv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) xv[k] = next[k];
-        if (turn) {
+        if (turn) packs_from(turn - NV);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) next[k] = tile_load<E, V, FLAT>(t, l, (const E*)c.x, from, f.x_extent, turn - NV + k);
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, turn + k, number + (turn + k) * number_step, xv[k], mean, w, b);
+        for (int k = 0; k < NV; ++k) write_result<E, V, FLAT, GRAN, SILU, DROP>(c, t, l, to, turn + k, mask, xv[k], mean, w, b);
     }
 }
 

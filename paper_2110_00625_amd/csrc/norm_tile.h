@@ -25,7 +25,7 @@ struct Tile {
     int cols, lane_rows;     // packs per row, rows that the lanes of a unit cover together
     int channels, groups;    // of a tile
     int blocks, chunks;      // tiles of an image: along its channels, along its rows
-    int rows;                // of an image
+    int rows, whole_rows;    // of an image; rounds of the lanes (flat: rows) that it fills
     // divisions by lanes per unit, cols, channels per group, sums of a row per group (packs, or channels)
     // tiles along the rows and the channels, images of a learner
     Divisor by_unit, by_cols, by_d, by_per, by_chunks, by_blocks, by_images;
@@ -92,20 +92,23 @@ __device__ __forceinline__ uint32_t tile_of_workgroup(uint32_t tiles, bool backw
     return x * per + (x < extra ? x : extra) + (backwards ? per + (x < extra) - 1 - at : at);
 }
 
-// where a lane works
+// Where a lane works.  What all lanes share (everything but unit, row and col where a workgroup has one image) is worked out in scalar
+// registers: in the vector ones these few 64-bit products were a seventh of the backward pass's instructions.
 template <int V, bool FLAT> struct Lane {
     uint32_t unit, row, col;                        // row, col: in the unit
     bool in;                                        // the lane has a place in a unit
-    uint32_t chunk, block, first_image, image, set, image_in_set;     // of the tile; image: of all learners', of the lane's unit
+    uint32_t chunk, block;                          // of the tile
+    uint32_t first_image, first_set, first_in_set;  // of the tile: number of all learners', learner, number of the learner's
+    uint32_t image, set, image_in_set;              // of the lane's unit
     int first_channel;                              // of the lane's pack (flat: within the image's channels)
     bool on;                                        // the place has an image and channels
     int64_t run;                                    // elements of an image
 
     __device__ __forceinline__ Lane(const NormCall& c, const Tile& t, uint32_t tile) {
-        unit = divide(threadIdx.x, t.by_unit);
-        in = unit < (uint32_t)t.units;
-        if (!in) unit = 0;
-        const uint32_t at = in ? threadIdx.x - unit * (t.cols * t.lane_rows) : 0;
+        unit = t.units > 1 ? divide(threadIdx.x, t.by_unit) : 0;
+        uint32_t at = threadIdx.x - unit * (t.cols * t.lane_rows);
+        in = unit < (uint32_t)t.units && at < (uint32_t)(t.cols * t.lane_rows);
+        if (!in) unit = at = 0;
         row = FLAT ? 0 : divide(at, t.by_cols);
         col = at - row * t.cols;
         run = (int64_t)c.positions * c.channels;
@@ -114,38 +117,57 @@ template <int V, bool FLAT> struct Lane {
         const uint32_t first = divide(rest, t.by_blocks);
         block = rest - first * t.blocks;
         first_image = first * t.units;
-        image = first_image + unit;
-        on = in && image < (uint32_t)(c.sets * c.images);
-        if (!on) image = first_image;
+        first_set = divide(first_image, t.by_images);
+        first_in_set = first_image - first_set * (uint32_t)c.images;
+        on = in;
+        image = first_image;
+        set = first_set;
+        image_in_set = first_in_set;
+        if (t.units > 1) {
+            on = in && first_image + unit < (uint32_t)(c.sets * c.images);
+            if (on) image += unit;
+            set = divide(image, t.by_images);
+            image_in_set = image - set * (uint32_t)c.images;
+        }
         if (FLAT) first_channel = (int)(col * V % (uint32_t)c.channels);
         else {
             first_channel = block * t.channels + col * V;
             if (first_channel >= c.channels) { on = false; first_channel = 0; }
         }
-        set = divide(image, t.by_images);
-        image_in_set = image - set * (uint32_t)c.images;
     }
     __device__ __forceinline__ int channel(const NormCall& c, int i) const {
         const int ch = first_channel + i;
         return FLAT && ch >= c.channels ? FLAT && V > c.channels ? ch % c.channels : ch - c.channels : ch;
     }
-    // row of the image of the lane's pack k
-    __device__ __forceinline__ int image_row(const Tile& t, int k) const { return (int)(chunk * t.nv + k) * t.lane_rows + (int)row; }
+    // where the lane's image, its learner's parameters, the tile's groups (a lane without work: groups that exist) and the first element of
+    // the image's number lie
+    __device__ __forceinline__ int64_t image_at(const Tile& t, const Strides& s) const {
+        return t.units > 1 ? set * s.set + image_in_set * s.image : first_set * s.set + first_in_set * s.image;
+    }
+    __device__ __forceinline__ int64_t set_at(const Tile& t, int64_t stride) const { return t.units > 1 ? set * stride : first_set * stride; }
+    __device__ __forceinline__ int64_t groups_at(const NormCall& c, const Tile& t) const {
+        return (t.units > 1 ? (int64_t)image * c.groups : (int64_t)first_image * c.groups) + block * t.groups;
+    }
+    __device__ __forceinline__ uint64_t number_of_image(const Tile& t) const { return t.units > 1 ? (uint64_t)image * run : (uint64_t)first_image * run; }
+    // row of the image of lane 0's pack k, and of the lane's
+    __device__ __forceinline__ int first_row(const Tile& t, int k) const { return (int)(chunk * t.nv + k) * t.lane_rows; }
+    __device__ __forceinline__ int image_row(const Tile& t, int k) const { return first_row(t, k) + (int)row; }
+    // is every lane's pack k one of the image's?  (The same in all lanes.)
+    __device__ __forceinline__ bool whole(const Tile& t, int k) const { return (int)(chunk * t.nv + k) < t.whole_rows; }
     // elements of pack k that are the image's
     __device__ __forceinline__ int valid(const Tile& t, int k) const {
         const int r = image_row(t, k);
         if (!FLAT) return on && r < t.rows ? V : 0;
+        if (whole(t, k)) return on ? V : 0;
         uint32_t at = col;
         asm volatile("" : "+v"(at));                // (asked again, worked out again: answers per pack and element would fill the scalar registers)
         const int64_t left = run - ((int64_t)r * t.cols + at) * V;
         return !on || left <= 0 ? 0 : left < V ? (int)left : V;
     }
-    // is k the last row of an image that is not made of whole rows (flat)?
-    __device__ __forceinline__ bool ragged(const Tile& t, int k) const { return FLAT && (int)(chunk * t.nv + k) == t.rows - 1; }
     // number of pack 0's first element in the whole tensor; what a pack more adds
     __device__ __forceinline__ uint64_t number(const NormCall& c, const Tile& t) const {
-        const uint64_t before = (uint64_t)image * run;
-        return before + (FLAT ? ((uint64_t)image_row(t, 0) * t.cols + col) * V : (uint64_t)image_row(t, 0) * c.channels + first_channel);
+        return number_of_image(t) + (FLAT ? (uint64_t)first_row(t, 0) * (t.cols * V) + col * V
+                                          : (uint64_t)first_row(t, 0) * c.channels + (uint64_t)row * (uint32_t)c.channels + first_channel);
     }
     __device__ __forceinline__ uint64_t number_step(const NormCall& c, const Tile& t) const {
         return FLAT ? (uint64_t)t.cols * V : (uint64_t)t.lane_rows * c.channels;
@@ -156,11 +178,11 @@ template <int V, bool FLAT> struct Lane {
 template <int V, bool FLAT> struct Place {
     int64_t first, step;
     __device__ __forceinline__ Place(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Strides& s) {
-        first = l.set * s.set + l.image_in_set * s.image;
-        if (FLAT) { first += ((int64_t)l.image_row(t, 0) * t.cols + l.col) * V; step = (int64_t)t.cols * V; }
-        else { first += l.image_row(t, 0) * s.row + l.first_channel; step = t.lane_rows * s.row; }
+        const int64_t image = l.image_at(t, s);
+        if (FLAT) { first = image + (int64_t)l.first_row(t, 0) * (t.cols * V) + l.col * V; step = (int64_t)t.cols * V; }
+        else { first = image + l.first_row(t, 0) * s.row + (int64_t)((uint64_t)l.row * (uint64_t)s.row) + l.first_channel; step = t.lane_rows * s.row; }
         // (a lane without a pack 0 reads the image's first row)
-        if (!l.valid(t, 0)) first = l.set * s.set + l.image_in_set * s.image + (FLAT ? 0 : l.first_channel);
+        if (!l.whole(t, 0) && !l.valid(t, 0)) first = image + (FLAT ? 0 : l.first_channel);
     }
 };
 
@@ -182,28 +204,51 @@ template <int V, bool FLAT> struct Chunk {
 
 // Pack k of a tensor; pack 0 once more where the image has no such pack.  One at a flat image's end may reach past it, into the next image,
 // which does no harm, but not past the tensor (extent): there it is put together from single elements.  No load but those stands behind
-// a branch.
-template <class E, int V, bool FLAT>
+// a branch that lanes take apart.
+template <class E, int V, bool FLAT, bool WHOLE>
 __device__ __forceinline__ typename Pack<E, V>::type tile_load(const Tile& t, const Lane<V, FLAT>& l, const E* p, const Place<V, FLAT>& at0, int64_t extent, int k) {
+    if (WHOLE) return pack_load<E, V>(p + at0.first + k * at0.step);
     int64_t at = at0.first + (l.valid(t, k) ? k * at0.step : 0);
     asm("" : "+v"(at));                              // (or the compiler makes that a copy of pack 0, behind a branch and a wait for it)
     if (!FLAT) return pack_load<E, V>(p + at);
     typename Pack<E, V>::type v = pack_load<E, V>(p + (at + V <= extent ? at : extent - V));
-    if (l.ragged(t, k) && at + V > extent) {
+    if (at + V > extent) {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = at + i < extent ? p[at + i] : (E)0.f;
     }
     return v;
 }
 
+// load(k, are they whole?) of the lane's packs first .. first+NV-1, all of them in one branch or the other
+template <int NV, int V, bool FLAT, class F> __device__ __forceinline__ void load_packs(const Tile& t, const Lane<V, FLAT>& l, int first, F load) {
+    if (l.whole(t, first + NV - 1)) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load(k, std::true_type());
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load(k, std::false_type());
+    }
+}
+
+template <class E, int V> __device__ __forceinline__ typename Pack<E, V>::type packed(const float (&v)[V]) {
+    typename Pack<E, V>::type o;
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {             // (two at a time, so that they are converted together)
+            const typename Pack<float, 2>::type two = {v[i], v[i + 1]};
+            const typename Pack<E, 2>::type r = __builtin_convertvector(two, typename Pack<E, 2>::type);
+            o[i] = r[0];
+            o[i + 1] = r[1];
+        }
+    } else o[0] = from_float<E>(v[0]);
+    return o;
+}
+
 template <class E, int V, bool FLAT>
-__device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l, E* p, const Place<V, FLAT>& at0, int k, const float (&v)[V]) {
+__device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l, E* p, const Place<V, FLAT>& at0, int k, const typename Pack<E, V>::type& o) {
     const int n = l.valid(t, k);
     if (!n) return;
     p += at0.first + k * at0.step;
-    typename Pack<E, V>::type o;
-#pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = from_float<E>(v[i]);
     if (!FLAT || n == V) pack_store<E, V>(p, o);
     else {
 #pragma unroll
@@ -216,7 +261,7 @@ static __device__ float no_weight = 1.f, no_bias = 0.f;      // (never written; 
 struct Parameter {
     const float* p;
     int each;
-    __device__ __forceinline__ Parameter(const float* of, int64_t stride, uint32_t set, const float* none) : p(of ? of + set * stride : none), each(of ? 1 : 0) {}
+    __device__ __forceinline__ Parameter(const float* of, int64_t at, const float* none) : p(of ? of + at : none), each(of ? 1 : 0) {}
     __device__ __forceinline__ float operator[](int ch) const { return p[ch * each]; }
 };
 
@@ -230,13 +275,27 @@ template <class P> __device__ __forceinline__ void keep_packed(P& v) {
     }
 }
 
-// v = elements from number e on, 0 where they are dropped.  (Rows: V = 4, 8 divides the channels, so e is a multiple of 4; flat: images of a
-// multiple of 4 elements)
-template <int V, bool FLAT> __device__ __forceinline__ void tile_mask(const DropRule& d, int64_t run, uint64_t e, float (&v)[V]) {
-    if constexpr (V == 1) v[0] = drop_keeps(d, e) ? v[0] : 0.f;
-    else if (!FLAT || run % 4 == 0) drop_mask<V, true>(d, e, v);
-    else drop_mask<V, false>(d, e, v);
-}
+// The lane's masks: a pack more is a whole number of draws further (V = 4, 8: the elements between two packs are a multiple of V), so that a
+// pack's state is an addition away.  Packs begin with a draw but in flat images that are not made of draws.
+template <int V, bool FLAT> struct TileMask {
+    uint64_t first, step;                           // V > 1: states of draws, else numbers of elements
+    uint32_t phase;
+    bool aligned;
+    __device__ __forceinline__ TileMask(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) {
+        const uint64_t e = l.number(c, t), each = l.number_step(c, t);
+        const DropPlace at(c.drop, e);
+        first = V > 1 ? at.state : e;
+        step = V > 1 ? each / 4 * SPLITMIX_GAMMA : each;
+        phase = at.phase;
+        aligned = !FLAT || l.run % 4 == 0;
+    }
+    // of pack k
+    template <class E> __device__ __forceinline__ void drop(const DropRule& d, int k, typename Pack<E, V>::type& v) const {
+        if constexpr (V == 1) v[0] = drop_keeps(d, first + k * step) ? v[0] : (E)0.f;
+        else if (aligned) drop_pack<E, V, true>(d, DropPlace(first + k * step, 0), v);
+        else drop_pack<E, V, false>(d, DropPlace(first + k * step, phase), v);
+    }
+};
 
 // sum + N elements of a pack from the first-th on, in bf16 two at a time (exact products with one, fp32 sums)
 template <int N, class P> __device__ __forceinline__ float pack_sum(const P& v, int first, float sum) {

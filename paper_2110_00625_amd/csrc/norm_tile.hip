@@ -22,6 +22,7 @@ size_t lds_bytes(const Tile& t, bool backward) {
 
 bool finish(const NormCall& c, bool backward, Tile* t) {
     const int D = c.channels / c.groups;
+    t->whole_rows = t->flat ? (int)(c.positions * c.channels / ((int64_t)t->cols * t->vec)) : t->rows / t->lane_rows;
     t->threads = (int)up((int64_t)t->units * t->cols * t->lane_rows, 64) * 64;
     t->by_unit = divisor(t->cols * t->lane_rows);
     t->by_cols = divisor(t->cols);

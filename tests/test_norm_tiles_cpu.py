@@ -35,7 +35,7 @@ class Divisor(ctypes.Structure):
 
 class Tile(ctypes.Structure):
     _fields_ = ([("nv", I), ("vec", I), ("flat", ctypes.c_bool)] +
-                [(n, I) for n in "gran threads units cols lane_rows channels groups blocks chunks rows".split()] +
+                [(n, I) for n in "gran threads units cols lane_rows channels groups blocks chunks rows whole_rows".split()] +
                 [("by_" + n, Divisor) for n in "unit cols d per chunks blocks images".split()] + [("lds", ctypes.c_size_t)])
 
 
