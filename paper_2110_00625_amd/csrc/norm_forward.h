@@ -31,9 +31,55 @@ __device__ __forceinline__ void join_parts(int terms, int lane, int team, float 
     *squares = team_sum(q, team);
 }
 
-// sum[a], sq[a]: squared distances from mean[a] of a lane's NV packs, n of them valid (flat: of each element's)
+// mean[a], sq[a]: of a lane's NV packs (flat: of each of their elements; GRAN elements of a pack otherwise) their mean and squared distances
+// from it.  All NV packs are the image's.
+template <class E, int V, int NV, int GRAN>
+__device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&xv)[NV], float (&mean)[V / GRAN], float (&sq)[V / GRAN]) {
+    constexpr int A = V / GRAN;
+    float sum[A];
+#pragma unroll
+    for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
+    if constexpr (sizeof(E) == 2 && GRAN > 1) {
+        // bf16: sums of values and of squares by dot products (half an instruction per element each; a mean and distances from it are four).
+        // n v = sum x^2 - n m^2 cancels where the mean is large against the spread: a wavefront that loses more than two bits in any lane
+        // takes the distances after all.
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+#pragma unroll
+            for (int a = 0; a < A; ++a) { sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]); sq[a] = pack_squares<GRAN>(xv[k], a * GRAN, sq[a]); }
+        }
+        bool lost = false;
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            mean[a] = sum[a] * (1.f / (NV * GRAN));
+            const float all = sq[a];
+            sq[a] = all - sum[a] * mean[a];
+            lost |= !(sq[a] >= 0.25f * all);
+        }
+        if (!__any(lost)) return;
+#pragma unroll
+        for (int a = 0; a < A; ++a) sq[a] = 0.f;
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+#pragma unroll
+            for (int a = 0; a < A; ++a) sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]);
+        }
+#pragma unroll
+        for (int a = 0; a < A; ++a) mean[a] = sum[a] * (1.f / (NV * GRAN));
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        auto v = xv[k];
+        keep_packed(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
+    }
+}
+
+// the same of packs of which valid(k) elements are the image's; count: packs (flat: of each element)
 template <class E, int V, int NV, bool FLAT, int GRAN, class Valid>
-__device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[V / GRAN], float (&sq)[V / GRAN],
+__device__ __forceinline__ void lane_moments(const typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[V / GRAN], float (&sq)[V / GRAN],
                                              int (&count)[FLAT ? V : 1]) {
     constexpr int A = V / GRAN;
     float sum[A];
@@ -53,21 +99,21 @@ __device__ __forceinline__ void lane_moments(typename Pack<E, V>::type (&xv)[NV]
         }
 #pragma unroll
         for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] += n > a;
-        keep_packed(xv[k]);
     }
 #pragma unroll
     for (int a = 0; a < A; ++a) mean[a] = count[FLAT ? a : 0] ? sum[a] / (float)(count[FLAT ? a : 0] * GRAN) : 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int n = valid(k);
+        auto v = xv[k];
+        keep_packed(v);
         if (n == V) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = to_float(xv[k][i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
+            for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
         } else if (FLAT && n) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(xv[k][i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
+            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
         }
-        keep_packed(xv[k]);
     }
 }
 
@@ -154,8 +200,15 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     }
     const Chunk<V, FLAT> chunk(c, t, l);
     float mean[A], rstd[A], w[V], b[V];
-    int group[A], count[FLAT ? V : 1];
-    lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
+    int group[A];
+    constexpr bool ASK = GRAN > 1 || NV <= FLAT_PACKS;      // (both ways of sixteen packs with sums per channel do not fit the registers)
+    if (ASK && l.whole(t, NV - 1)) whole_moments<E, V, NV, GRAN>(xv, mean, rstd);
+    else {
+        int count[FLAT ? V : 1];
+        lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) keep_packed(xv[k]);
     lane_parameters(c, t, l, w, b);                     // (on their way while the groups are joined)
     lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
     float* stat = lds + 2 * blockDim.x * A;          // [unit][group of the tile] mean, then rstd
@@ -196,28 +249,35 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
     };
     packs_from(0);
     float mean[A], sq[A];
-    int before[FLAT ? V : 1];
 #pragma unroll
     for (int a = 0; a < A; ++a) mean[a] = sq[a] = 0.f;
-#pragma unroll
-    for (int a = 0; a < (FLAT ? V : 1); ++a) before[a] = 0;
     for (int turn = 0; turn < t.nv; turn += NV) {
         typename Pack<E, V>::type xv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) xv[k] = next[k];
         if (turn + NV < t.nv) packs_from(turn + NV);
         float m[A], q[A];
+        if (l.whole(t, turn + NV - 1)) {
+            whole_moments<E, V, NV, GRAN>(xv, m, q);
+            const float old = (float)(turn * GRAN), share = (NV * GRAN) / (old + NV * GRAN), both = old * share;
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+                const float d = m[a] - mean[a];
+                mean[a] += d * share;
+                sq[a] += q[a] + d * d * both;
+            }
+            continue;
+        }
+        // (the image ends in this turn or did before: the turns in front of its end were whole)
         int count[FLAT ? V : 1];
         lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            const float n = (float)(count[FLAT ? a : 0] * GRAN), old = (float)(before[FLAT ? a : 0] * GRAN);
+            const float n = (float)(count[FLAT ? a : 0] * GRAN), old = (float)(turn * GRAN);
             const float share = n > 0.f ? n / (n + old) : 0.f, d = m[a] - mean[a];
             mean[a] += d * share;
             sq[a] += q[a] + d * d * (old * share);
         }
-#pragma unroll
-        for (int a = 0; a < (FLAT ? V : 1); ++a) before[a] += count[a];
     }
     const Chunk<V, FLAT> chunk(c, t, l);
     join_lanes<V, FLAT, GRAN>(c, t, l, chunk, lds, mean, sq, [&](int unit, int in, float m, float q) {

@@ -265,9 +265,9 @@ struct Parameter {
     __device__ __forceinline__ float operator[](int ch) const { return p[ch * each]; }
 };
 
-// Packs stay packed between their uses (the compiler would keep a bf16 pack's floats, twice the registers).
+// bf16 packs stay packed between their uses (the compiler would keep their floats, twice the registers).
 template <class P> __device__ __forceinline__ void keep_packed(P& v) {
-    if constexpr (sizeof(P) == 16) {
+    if constexpr (sizeof(P) == 16 && sizeof(v[0]) == 2) {
         typedef int words __attribute__((ext_vector_type(4)));
         words w = __builtin_bit_cast(words, v);
         asm volatile("" : "+v"(w));
@@ -308,6 +308,14 @@ template <int N, class P> __device__ __forceinline__ float pack_sum(const P& v, 
 #pragma unroll
         for (int i = 0; i < N; ++i) sum += to_float(v[first + i]);
     }
+    return sum;
+}
+
+// the same of squares (bf16)
+template <int N, class P> __device__ __forceinline__ float pack_squares(const P& v, int first, float sum) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < N; i += 2) { const pair p = {v[first + i], v[first + i + 1]}; sum = __builtin_amdgcn_fdot2_f32_bf16(p, p, sum, false); }
     return sum;
 }
 
