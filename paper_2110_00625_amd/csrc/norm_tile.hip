@@ -1,6 +1,7 @@
 // Tiles of the group norm: which ones a call takes.
 #include "norm_tile.h"
 #include <algorithm>
+#include <cstdint>
 #include <numeric>
 
 namespace kavg {
@@ -10,7 +11,7 @@ namespace {
 constexpr int MOST_LANES = 1024;
 constexpr int LANES = 512;                // two workgroups of them share a compute unit's registers
 constexpr int64_t FULL = 256 * 1024;      // lanes that fill the device's 256 compute units
-constexpr int64_t SUM_GROUPS = 512;       // workgroups wanted for sums: two per compute unit
+constexpr int64_t SUM_GROUPS = 512;       // workgroups of a round of sums: two per compute unit
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -54,7 +55,14 @@ bool twice(const NormCall& c, bool backward, const Tile& t, int64_t rows, NormTi
     n->whole.nv = 0;
     n->sums = n->apply = t;
     n->sums.units = n->apply.units = 1;
-    const int64_t turns = up(rows, (int64_t)turn * t.lane_rows), chunks = std::min(turns, up(SUM_GROUPS, images * t.blocks));
+    // Chunks: as many as make `round` rounds of the device's workgroups, for the number of rounds that costs least, in turns; a workgroup has
+    // about two turns' work beside its turns.  (Four chunks of each of 132 images, 528 workgroups, are two rounds, three are one: see below.)
+    const int64_t turns = up(rows, (int64_t)turn * t.lane_rows), tiles = images * t.blocks, first = up(tiles, SUM_GROUPS);
+    int64_t chunks = 1, least = INT64_MAX;
+    for (int64_t round = first; round < first + 4; ++round) {
+        const int64_t some = std::min(turns, round * SUM_GROUPS / tiles), cost = up(tiles * some, SUM_GROUPS) * (up(turns, some) + 2);
+        if (cost < least) { least = cost; chunks = some; }
+    }
     n->sums.nv = n->apply.nv = (int)(turn * up(turns, chunks));
     n->sums.chunks = n->apply.chunks = (int)up(rows, (int64_t)n->sums.nv * t.lane_rows);
     return finish(c, backward, &n->sums) && finish(c, backward, &n->apply);
