@@ -38,9 +38,7 @@ template <int V, bool FLAT, int GRAN> struct Channels {
             mean[a] = c.mean[first_group + group[a]];
             rstd[a] = c.rstd[first_group + group[a]];
         }
-        const Parameter weight(c.weight, l.set_at(t, c.weight_stride), &no_weight), bias(c.bias, l.set_at(t, c.bias_stride), &no_bias);
-#pragma unroll
-        for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
+        lane_parameters(c, t, l, w, b);
     }
     // the tile's weights into LDS, by the lanes of the first place
     __device__ __forceinline__ void share(const Tile& t, const Lane<V, FLAT>& l, float* lds) const {

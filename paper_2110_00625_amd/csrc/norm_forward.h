@@ -144,13 +144,6 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
     }
 }
 
-template <int V, bool FLAT>
-__device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
-    const Parameter weight(c.weight, l.set_at(t, c.weight_stride), &no_weight), bias(c.bias, l.set_at(t, c.bias_stride), &no_bias);
-#pragma unroll
-    for (int i = 0; i < V; ++i) { w[i] = weight[l.channel(c, i)]; b[i] = bias[l.channel(c, i)]; }
-}
-
 // group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
 template <int V, bool FLAT, int GRAN, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
 #pragma unroll

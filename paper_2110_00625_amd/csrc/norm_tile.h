@@ -92,6 +92,9 @@ __device__ __forceinline__ uint32_t tile_of_workgroup(uint32_t tiles, bool backw
     return x * per + (x < extra ? x : extra) + (backwards ? per + (x < extra) - 1 - at : at);
 }
 
+// v, worked out in scalar registers (what follows would be moved in front of the choice that led here, into vector registers)
+__device__ __forceinline__ int64_t scalar(int64_t v) { asm volatile("" : "+s"(v)); return v; }
+
 // Where a lane works.  What all lanes share (everything but unit, row and col where a workgroup has one image) is worked out in scalar
 // registers: in the vector ones these few 64-bit products were a seventh of the backward pass's instructions.
 template <int V, bool FLAT> struct Lane {
@@ -142,13 +145,21 @@ template <int V, bool FLAT> struct Lane {
     // where the lane's image, its learner's parameters, the tile's groups (a lane without work: groups that exist) and the first element of
     // the image's number lie
     __device__ __forceinline__ int64_t image_at(const Tile& t, const Strides& s) const {
-        return t.units > 1 ? set * s.set + image_in_set * s.image : first_set * s.set + first_in_set * s.image;
+        if (t.units > 1) return set * s.set + image_in_set * s.image;
+        return scalar(first_set * s.set + first_in_set * s.image);
     }
-    __device__ __forceinline__ int64_t set_at(const Tile& t, int64_t stride) const { return t.units > 1 ? set * stride : first_set * stride; }
+    __device__ __forceinline__ int64_t set_at(const Tile& t, int64_t stride) const {
+        if (t.units > 1) return set * stride;
+        return scalar(first_set * stride);
+    }
     __device__ __forceinline__ int64_t groups_at(const NormCall& c, const Tile& t) const {
-        return (t.units > 1 ? (int64_t)image * c.groups : (int64_t)first_image * c.groups) + block * t.groups;
+        if (t.units > 1) return (int64_t)image * c.groups + block * t.groups;
+        return scalar((int64_t)first_image * c.groups + block * t.groups);
     }
-    __device__ __forceinline__ uint64_t number_of_image(const Tile& t) const { return t.units > 1 ? (uint64_t)image * run : (uint64_t)first_image * run; }
+    __device__ __forceinline__ uint64_t number_of_image(const Tile& t) const {
+        if (t.units > 1) return (uint64_t)image * run;
+        return scalar((int64_t)first_image * run);
+    }
     // row of the image of lane 0's pack k, and of the lane's
     __device__ __forceinline__ int first_row(const Tile& t, int k) const { return (int)(chunk * t.nv + k) * t.lane_rows; }
     __device__ __forceinline__ int image_row(const Tile& t, int k) const { return first_row(t, k) + (int)row; }
@@ -166,8 +177,8 @@ template <int V, bool FLAT> struct Lane {
     }
     // number of pack 0's first element in the whole tensor; what a pack more adds
     __device__ __forceinline__ uint64_t number(const NormCall& c, const Tile& t) const {
-        return number_of_image(t) + (FLAT ? (uint64_t)first_row(t, 0) * (t.cols * V) + col * V
-                                          : (uint64_t)first_row(t, 0) * c.channels + (uint64_t)row * (uint32_t)c.channels + first_channel);
+        const int64_t before = scalar((int64_t)first_row(t, 0) * (FLAT ? t.cols * V : c.channels));
+        return number_of_image(t) + before + (FLAT ? col * V : (uint64_t)row * (uint32_t)c.channels + first_channel);
     }
     __device__ __forceinline__ uint64_t number_step(const NormCall& c, const Tile& t) const {
         return FLAT ? (uint64_t)t.cols * V : (uint64_t)t.lane_rows * c.channels;
@@ -179,8 +190,8 @@ template <int V, bool FLAT> struct Place {
     int64_t first, step;
     __device__ __forceinline__ Place(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Strides& s) {
         const int64_t image = l.image_at(t, s);
-        if (FLAT) { first = image + (int64_t)l.first_row(t, 0) * (t.cols * V) + l.col * V; step = (int64_t)t.cols * V; }
-        else { first = image + l.first_row(t, 0) * s.row + (int64_t)((uint64_t)l.row * (uint64_t)s.row) + l.first_channel; step = t.lane_rows * s.row; }
+        step = FLAT ? (int64_t)t.cols * V : t.lane_rows * s.row;
+        first = image + scalar(l.first_row(t, 0) * (FLAT ? step : s.row)) + (FLAT ? l.col * V : (int64_t)((uint64_t)l.row * (uint64_t)s.row) + l.first_channel);
         // (a lane without a pack 0 reads the image's first row)
         if (!l.whole(t, 0) && !l.valid(t, 0)) first = image + (FLAT ? 0 : l.first_channel);
     }
@@ -256,14 +267,30 @@ __device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l
     }
 }
 
-// a learner's parameters, or in their place one number for all channels: no load behind a branch
-static __device__ float no_weight = 1.f, no_bias = 0.f;      // (never written; not const, for constants lie in another kind of memory)
-struct Parameter {
-    const float* p;
-    int each;
-    __device__ __forceinline__ Parameter(const float* of, int64_t at, const float* none) : p(of ? of + at : none), each(of ? 1 : 0) {}
-    __device__ __forceinline__ float operator[](int ch) const { return p[ch * each]; }
-};
+// A learner's parameters of the lane's channels, or in their place one number for all of them; the branch is one that all lanes take.
+template <int V, bool FLAT>
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, const float* of, int64_t at, float none, float (&p)[V]) {
+    if (!of) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[i] = none;
+    } else if (FLAT) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[i] = of[at + l.channel(c, i)];
+    } else {
+        constexpr int N = V < 4 ? V : 4;
+#pragma unroll
+        for (int i = 0; i < V; i += N) {
+            const typename Pack<float, N>::type v = pack_load<float, N>(of + at + l.first_channel + i);
+#pragma unroll
+            for (int j = 0; j < N; ++j) p[i + j] = v[j];
+        }
+    }
+}
+template <int V, bool FLAT>
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
+    lane_parameters(c, l, c.weight, l.set_at(t, c.weight_stride), 1.f, w);
+    lane_parameters(c, l, c.bias, l.set_at(t, c.bias_stride), 0.f, b);
+}
 
 // bf16 packs stay packed between their uses (the compiler would keep their floats, twice the registers).
 template <class P> __device__ __forceinline__ void keep_packed(P& v) {
