@@ -267,20 +267,22 @@ __device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l
     }
 }
 
-// A learner's parameters of the lane's channels, or in their place one number for all of them; the branch is one that all lanes take.
+// A learner's parameters of the lane's channels, or in their place one number for all of them: no load behind a branch (a wait for it would
+// follow, in front of the packs').
+static __device__ float no_weight[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, no_bias[8] = {};      // (never written; not const, for constants
+                                                                                                    // lie in another kind of memory)
 template <int V, bool FLAT>
-__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, const float* of, int64_t at, float none, float (&p)[V]) {
-    if (!of) {
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, const float* of, int64_t at, const float* none, float (&p)[V]) {
+    const float* from = of ? of + at : none;
+    if (FLAT) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = none;
-    } else if (FLAT) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = of[at + l.channel(c, i)];
+        for (int i = 0; i < V; ++i) p[i] = from[of ? l.channel(c, i) : 0];
     } else {
         constexpr int N = V < 4 ? V : 4;
+        from += of ? l.first_channel : 0;
 #pragma unroll
         for (int i = 0; i < V; i += N) {
-            const typename Pack<float, N>::type v = pack_load<float, N>(of + at + l.first_channel + i);
+            const typename Pack<float, N>::type v = pack_load<float, N>(from + i);
 #pragma unroll
             for (int j = 0; j < N; ++j) p[i + j] = v[j];
         }
@@ -288,8 +290,8 @@ __device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V,
 }
 template <int V, bool FLAT>
 __device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
-    lane_parameters(c, l, c.weight, l.set_at(t, c.weight_stride), 1.f, w);
-    lane_parameters(c, l, c.bias, l.set_at(t, c.bias_stride), 0.f, b);
+    lane_parameters(c, l, c.weight, l.set_at(t, c.weight_stride), no_weight, w);
+    lane_parameters(c, l, c.bias, l.set_at(t, c.bias_stride), no_bias, b);
 }
 
 // bf16 packs stay packed between their uses (the compiler would keep their floats, twice the registers).
