@@ -218,19 +218,20 @@ def _output(x, out):
     return _torch_module.empty_like(x) if x.is_contiguous() else _torch_module.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
-def _call(name, x, fn, *args):
-    """fn on x's device and its current stream."""
+def _failed(name, rc):
+    raise KavgError(rc, "%s rejected its arguments" % name if rc == KAVG_EINVAL else "HIP launch failed")
+
+
+def _launch(x, fn, *args):
+    """What fn returns, on x's device and its current stream."""
     index = x.device.index
     try:
         if index == _torch_module.cuda.current_device():
-            rc = fn(*args, _stream_of(index))
-        else:
-            with _torch_module.cuda.device(index):
-                rc = fn(*args, _stream_of(index))
+            return fn(*args, _stream_of(index))
+        with _torch_module.cuda.device(index):
+            return fn(*args, _stream_of(index))
     except ctypes.ArgumentError as e:
         _bad(str(e))
-    if rc != KAVG_OK:
-        raise KavgError(rc, "%s rejected its arguments" % name if rc == KAVG_EINVAL else "HIP launch failed")
 
 
 def _images(x, name):
@@ -241,13 +242,12 @@ def _images(x, name):
     return _IMAGES.pack(x.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-def _params(p, x, name):
-    """(pointer, learner stride) of a fp32 [sets][channels] (or [channels]) tensor, None: (None, 0)."""
+def _params(p, x, shape, name):
+    """(pointer, learner stride) of a fp32 tensor of that shape, [sets][channels] or [channels]; None: (None, 0)."""
     if p is None:
         return None, 0
-    shape = x.shape
-    if p.dtype is not _torch_module.float32 or p.device != x.device or p.shape != (shape[-1:] if len(shape) == 3 else shape[::3]):
-        _bad("%s is not a float32 tensor of [%schannels] on x's device" % (name, "sets, " if len(shape) == 4 else ""))
+    if p.dtype is not _torch_module.float32 or p.device != x.device or p.shape != shape:
+        _bad("%s is not a float32 tensor of [%schannels] on x's device" % (name, "sets, " if len(shape) == 2 else ""))
     st = p.stride()
     if st[-1] != 1 and shape[-1] > 1:
         _bad("%s has a last stride of %d" % (name, st[-1]))
@@ -290,17 +290,23 @@ def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE,
     or [images, groups] in float32, which kavg_group_norm_backward wants."""
     torch = _torch_module or _torch()
     norm = _norm(x, groups, eps, activation, drop, seed, site)
-    block, at, nbytes = _workspace(norm, 0, x, weight)
     y = _output(x, out)
-    w, ws = _params(weight, x, "weight")
-    b, bs = _params(bias, x, "bias")
+    channels = x.shape[::3] if x.dim() == 4 else x.shape[-1:]
+    w, ws = _params(weight, x, channels, "weight")
+    b, bs = _params(bias, x, channels, "bias")
     mean = rstd = m = r = None
     if stats:
         shape = x.shape[:-2] + (groups,)
         mean = torch.empty(shape, dtype=torch.float32, device=x.device) if weight is None else weight.new_empty(shape)
         rstd = torch.empty_like(mean)
         m, r = mean.data_ptr(), rstd.data_ptr()
-    _call("kavg_group_norm", x, _lib.kavg_group_norm, norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), m, r, at, nbytes)
+    args = (norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), m, r)
+    rc = _launch(x, _lib.kavg_group_norm, *args, None, 0)
+    if rc == KAVG_ENOMEM:                        # (large images only: the others are spared the question and the block)
+        block, at, nbytes = _workspace(norm, 0, x, weight)
+        rc = _launch(x, _lib.kavg_group_norm, *args, at, nbytes)
+    if rc != KAVG_OK:
+        _failed("kavg_group_norm", rc)
     return (y, mean, rstd) if stats else y
 
 
@@ -318,13 +324,16 @@ def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation
             _bad("mean, rstd are not what kavg_group_norm returned")
     block, at, nbytes = _workspace(norm, 1, x, mean)
     dx = _output(x, out)
-    w, ws = _params(weight, x, "weight")
-    b, bs = _params(bias, x, "bias")
+    channels = x.shape[::3] if x.dim() == 4 else x.shape[-1:]
+    w, ws = _params(weight, x, channels, "weight")
+    b, bs = _params(bias, x, channels, "bias")
     dweight, dbias = _gradient(dweight, weight), _gradient(dbias, bias)
-    gw, gws = _params(dweight, x, "dweight")
-    gb, gbs = _params(dbias, x, "dbias")
-    _call("kavg_group_norm_backward", x, _lib.kavg_group_norm_backward, norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(),
-          rstd.data_ptr(), w, ws, b, bs, _images(dx, "out"), gw, gws, gb, gbs, at, nbytes)
+    gw, gws = _params(dweight, x, channels, "dweight")
+    gb, gbs = _params(dbias, x, channels, "dbias")
+    rc = _launch(x, _lib.kavg_group_norm_backward, norm, _images(dy, "dy"), _images(x, "x"), mean.data_ptr(), rstd.data_ptr(), w, ws, b, bs,
+                 _images(dx, "out"), gw, gws, gb, gbs, at, nbytes)
+    if rc != KAVG_OK:
+        _failed("kavg_group_norm_backward", rc)
     return dx, dweight, dbias
 
 
@@ -367,8 +376,9 @@ def kavg_dropout(x, drop, seed, site=0, residual=None, out=None):
     at = rs = None
     if residual is not None:
         at, rs = _like(residual, x, "residual").data_ptr(), _rows(residual, "residual")[2]
-    _call("kavg_dropout", x, _lib.kavg_dropout, x.data_ptr(), xs, at, rs or 0, y.data_ptr(), _rows(y, "out")[2], rows, cols, dtype, drop, seed,
-          site)
+    rc = _launch(x, _lib.kavg_dropout, x.data_ptr(), xs, at, rs or 0, y.data_ptr(), _rows(y, "out")[2], rows, cols, dtype, drop, seed, site)
+    if rc != KAVG_OK:
+        _failed("kavg_dropout", rc)
     return y
 
 
@@ -379,8 +389,9 @@ def kavg_dropout_backward(dy, drop, seed, site=0, out=None):
     _counters_ok(seed, site)
     dx = _output(dy, out)
     rows, cols, stride = _rows(dy, "dy")
-    _call("kavg_dropout_backward", dy, _lib.kavg_dropout_backward, dy.data_ptr(), stride, dx.data_ptr(), _rows(dx, "out")[2], rows, cols, dtype,
-          drop, seed, site)
+    rc = _launch(dy, _lib.kavg_dropout_backward, dy.data_ptr(), stride, dx.data_ptr(), _rows(dx, "out")[2], rows, cols, dtype, drop, seed, site)
+    if rc != KAVG_OK:
+        _failed("kavg_dropout_backward", rc)
     return dx
 
 
