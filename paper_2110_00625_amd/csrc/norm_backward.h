@@ -32,13 +32,9 @@ template <int V, bool FLAT, int GRAN> struct Channels {
 
     __device__ __forceinline__ Channels(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l) : mask(c, t, l) {
         first_group = l.groups_at(c, t);
+        lane_parameters(c, t, l, w, b, group);
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-            group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
-            mean[a] = c.mean[first_group + group[a]];
-            rstd[a] = c.rstd[first_group + group[a]];
-        }
-        lane_parameters(c, t, l, w, b);
+        for (int a = 0; a < A; ++a) { mean[a] = c.mean[first_group + group[a]]; rstd[a] = c.rstd[first_group + group[a]]; }
     }
     // the tile's weights into LDS, by the lanes of the first place
     __device__ __forceinline__ void share(const Tile& t, const Lane<V, FLAT>& l, float* lds) const {

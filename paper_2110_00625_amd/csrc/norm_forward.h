@@ -77,42 +77,52 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
     }
 }
 
-// the same of packs of which valid(k) elements are the image's; count: packs (flat: of each element)
-template <class E, int V, int NV, bool FLAT, int GRAN, class Valid>
-__device__ __forceinline__ void lane_moments(const typename Pack<E, V>::type (&xv)[NV], Valid valid, float (&mean)[V / GRAN], float (&sq)[V / GRAN],
-                                             int (&count)[FLAT ? V : 1]) {
+// The same of packs from the `first`-th on of which not all are the image's, and how many are (flat: of each element): `whole` of them, and one
+// more in some lanes (flat: or a part of one).
+template <class E, int V, int NV, bool FLAT, int GRAN>
+__device__ __forceinline__ void lane_moments(const typename Pack<E, V>::type (&xv)[NV], const Tile& t, const Lane<V, FLAT>& l, int first, float (&mean)[V / GRAN],
+                                             float (&sq)[V / GRAN], float (&count)[FLAT ? V : 1]) {
     constexpr int A = V / GRAN;
+    int whole = 0, more = 0;                         // more: elements of the pack behind the whole ones
     float sum[A];
 #pragma unroll
     for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
 #pragma unroll
-    for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] = 0;
-#pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int n = valid(k);
-        if (n == V) {
+        if (l.whole(t, first + k)) {
+            ++whole;
 #pragma unroll
             for (int a = 0; a < A; ++a) sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]);
-        } else if (FLAT && n) {
+        } else {
+            const int n = l.valid(t, first + k);
+            more |= n;                               // (no other pack has any)
+            if (FLAT) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i / GRAN] += i < n ? to_float(xv[k][i]) : 0.f;
+                for (int i = 0; i < V; ++i) sum[i / GRAN] += i < n ? to_float(xv[k][i]) : 0.f;
+            } else if (n) {
+#pragma unroll
+                for (int a = 0; a < A; ++a) sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]);
+            }
         }
-#pragma unroll
-        for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] += n > a;
     }
+    const float each = whole ? 1.f / (float)(whole * GRAN) : 0.f, each_more = 1.f / (float)((whole + 1) * GRAN);
 #pragma unroll
-    for (int a = 0; a < A; ++a) mean[a] = count[FLAT ? a : 0] ? sum[a] / (float)(count[FLAT ? a : 0] * GRAN) : 0.f;
+    for (int a = 0; a < A; ++a) mean[a] = sum[a] * ((FLAT ? a : 0) < more ? each_more : each);
+#pragma unroll
+    for (int a = 0; a < (FLAT ? V : 1); ++a) count[a] = (float)(whole + (a < more));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int n = valid(k);
         auto v = xv[k];
         keep_packed(v);
-        if (n == V) {
+        if (l.whole(t, first + k)) {
 #pragma unroll
             for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
-        } else if (FLAT && n) {
+        } else {
+            const int n = l.valid(t, first + k);
+            if (n) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) if (i < n) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
+                for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += !FLAT || i < n ? d * d : 0.f; }
+            }
         }
     }
 }
@@ -142,12 +152,6 @@ __device__ __forceinline__ void join_lanes(const NormCall& c, const Tile& t, con
                    [&](int j) { return part_mean[base + slot(j)]; }, [&](int j) { return part_sq[base + slot(j)]; }, &m, &q);
         if (lane == 0) done(unit, in, m, q);
     }
-}
-
-// group of the tile of a lane's a-th sum (of a lane without work, whose group may not exist: the first one)
-template <int V, bool FLAT, int GRAN, int A> __device__ __forceinline__ void lane_groups(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, int (&group)[A]) {
-#pragma unroll
-    for (int a = 0; a < A; ++a) group[a] = l.on ? divide(FLAT ? l.channel(c, a) : l.col * V + a * GRAN, t.by_d) : 0;
 }
 
 // weight times r; SiLU's factor into both, or drop's scale, which commutes with ReLU
@@ -197,13 +201,12 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     constexpr bool ASK = GRAN > 1 || NV <= FLAT_PACKS;      // (both ways of sixteen packs with sums per channel do not fit the registers)
     if (ASK && l.whole(t, NV - 1)) whole_moments<E, V, NV, GRAN>(xv, mean, rstd);
     else {
-        int count[FLAT ? V : 1];
-        lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, k); }, mean, rstd, count);
+        float count[FLAT ? V : 1];
+        lane_moments<E, V, NV, FLAT, GRAN>(xv, t, l, 0, mean, rstd, count);
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) keep_packed(xv[k]);
-    lane_parameters(c, t, l, w, b);                     // (on their way while the groups are joined)
-    lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
+    lane_parameters(c, t, l, w, b, group);                     // (on their way while the groups are joined)
     float* stat = lds + 2 * blockDim.x * A;          // [unit][group of the tile] mean, then rstd
     const int groups = t.units * t.groups, D = c.channels / c.groups;
     join_lanes<V, FLAT, GRAN>(c, t, l, chunk, lds, mean, rstd, [&](int unit, int in, float m, float q) {
@@ -262,11 +265,11 @@ __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
             continue;
         }
         // (the image ends in this turn or did before: the turns in front of its end were whole)
-        int count[FLAT ? V : 1];
-        lane_moments<E, V, NV, FLAT, GRAN>(xv, [&](int k) { return l.valid(t, turn + k); }, m, q, count);
+        float count[FLAT ? V : 1];
+        lane_moments<E, V, NV, FLAT, GRAN>(xv, t, l, turn, m, q, count);
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            const float n = (float)(count[FLAT ? a : 0] * GRAN), old = (float)(turn * GRAN);
+            const float n = count[FLAT ? a : 0] * GRAN, old = (float)(turn * GRAN);
             const float share = n > 0.f ? n / (n + old) : 0.f, d = m[a] - mean[a];
             mean[a] += d * share;
             sq[a] += q[a] + d * d * (old * share);
@@ -312,8 +315,7 @@ __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
     // (loads return in order: what the first pack needs is asked for before the packs)
     float mean[A], rstd[A], w[V], b[V];
     int group[A];
-    lane_parameters(c, t, l, w, b);
-    lane_groups<V, FLAT, GRAN, A>(c, t, l, group);
+    lane_parameters(c, t, l, w, b, group);
     typename Pack<E, V>::type next[NV];
     const auto packs_from = [&](int first) {
         load_packs<NV>(t, l, first, [&](int k, auto whole) { next[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.x, from, f.x_extent, first + k); });

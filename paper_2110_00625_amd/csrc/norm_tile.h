@@ -138,9 +138,16 @@ template <int V, bool FLAT> struct Lane {
             if (first_channel >= c.channels) { on = false; first_channel = 0; }
         }
     }
-    __device__ __forceinline__ int channel(const NormCall& c, int i) const {
-        const int ch = first_channel + i;
-        return FLAT && ch >= c.channels ? FLAT && V > c.channels ? ch % c.channels : ch - c.channels : ch;
+    __device__ __forceinline__ void channels(const NormCall& c, int (&ch)[V]) const {
+#pragma unroll
+        for (int i = 0; i < V; ++i) ch[i] = first_channel + i;
+        if (!FLAT) return;
+        if (V <= c.channels) {
+#pragma unroll
+            for (int i = 1; i < V; ++i) ch[i] -= ch[i] >= c.channels ? c.channels : 0;
+        } else {
+            for (int i = 1; i < V; ++i) ch[i] %= c.channels;
+        }
     }
     // where the lane's image, its learner's parameters, the tile's groups (a lane without work: groups that exist) and the first element of
     // the image's number lie
@@ -230,9 +237,15 @@ __device__ __forceinline__ typename Pack<E, V>::type tile_load(const Tile& t, co
     return v;
 }
 
-// load(k, are they whole?) of the lane's packs first .. first+NV-1, all of them in one branch or the other
+// load(k, is it whole?) of the lane's packs first .. first+NV-1; in rows all of them in one branch or the other
 template <int NV, int V, bool FLAT, class F> __device__ __forceinline__ void load_packs(const Tile& t, const Lane<V, FLAT>& l, int first, F load) {
-    if (l.whole(t, first + NV - 1)) {
+    if (FLAT) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (l.whole(t, first + k)) load(k, std::true_type());
+            else load(k, std::false_type());
+        }
+    } else if (l.whole(t, first + NV - 1)) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) load(k, std::true_type());
     } else {
@@ -272,14 +285,15 @@ __device__ __forceinline__ void tile_store(const Tile& t, const Lane<V, FLAT>& l
 static __device__ float no_weight[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, no_bias[8] = {};      // (never written; not const, for constants
                                                                                                     // lie in another kind of memory)
 template <int V, bool FLAT>
-__device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V, FLAT>& l, const float* of, int64_t at, const float* none, float (&p)[V]) {
+__device__ __forceinline__ void lane_parameters(const Lane<V, FLAT>& l, const int (&ch)[V], const float* of, int64_t at, const float* none, float (&p)[V]) {
     const float* from = of ? of + at : none;
+    const int each = of ? -1 : 0;
     if (FLAT) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = from[of ? l.channel(c, i) : 0];
+        for (int i = 0; i < V; ++i) p[i] = from[ch[i] & each];
     } else {
         constexpr int N = V < 4 ? V : 4;
-        from += of ? l.first_channel : 0;
+        from += l.first_channel & each;
 #pragma unroll
         for (int i = 0; i < V; i += N) {
             const typename Pack<float, N>::type v = pack_load<float, N>(from + i);
@@ -288,10 +302,15 @@ __device__ __forceinline__ void lane_parameters(const NormCall& c, const Lane<V,
         }
     }
 }
-template <int V, bool FLAT>
-__device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V]) {
-    lane_parameters(c, l, c.weight, l.set_at(t, c.weight_stride), no_weight, w);
-    lane_parameters(c, l, c.bias, l.set_at(t, c.bias_stride), no_bias, b);
+// the channels' weights and biases, and the groups in the tile of the lane's A sums (of a lane without work, whose group may not exist: the first)
+template <int V, bool FLAT, int A>
+__device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, float (&w)[V], float (&b)[V], int (&group)[A]) {
+    int ch[V];
+    l.channels(c, ch);
+    lane_parameters(l, ch, c.weight, l.set_at(t, c.weight_stride), no_weight, w);
+    lane_parameters(l, ch, c.bias, l.set_at(t, c.bias_stride), no_bias, b);
+#pragma unroll
+    for (int a = 0; a < A; ++a) group[a] = l.on ? divide(FLAT ? ch[a] : l.col * V + a * (V / A), t.by_d) : 0;
 }
 
 // bf16 packs stay packed between their uses (the compiler would keep their floats, twice the registers).
