@@ -20,7 +20,7 @@ namespace kavg {
 struct Tile {
     int nv, vec;             // packs per lane, elements per pack
     bool flat;
-    int gran;                // elements of a pack that always lie in one group: all, half of them, or 1
+    int gran;                // elements of a pack that always lie in one group (a power of two)
     int threads, units;      // lanes of a workgroup, images of a workgroup
     int cols, lane_rows;     // packs per row, rows that the lanes of a unit cover together
     int channels, groups;    // of a tile
@@ -75,7 +75,8 @@ template <class E, class F> hipError_t with_layout(const Tile& t, F f) {
     if (t.vec == 1) return f(one, std::false_type(), one);
     if (t.flat) return f(pack, std::true_type(), one);
     if (t.gran == V) return f(pack, std::false_type(), pack);
-    return t.gran == V / 2 ? f(pack, std::false_type(), std::integral_constant<int, V / 2>()) : f(pack, std::false_type(), one);
+    if (t.gran == V / 2) return f(pack, std::false_type(), std::integral_constant<int, V / 2>());
+    return t.gran == 2 ? f(pack, std::false_type(), std::integral_constant<int, 2>()) : f(pack, std::false_type(), one);
 }
 // f(constants: SiLU, dropout)
 template <class F> hipError_t with_options(const NormCall& c, F f) {

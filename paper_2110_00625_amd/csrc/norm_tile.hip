@@ -75,7 +75,7 @@ bool rows_tiles(const NormCall& c, int vec, int elem, bool backward, NormTiles* 
     const int64_t images = c.sets * c.images, pieces = c.channels / least;
     Tile t = {};
     t.vec = vec;
-    t.gran = D % vec == 0 ? vec : D % (vec / 2) == 0 ? vec / 2 : 1;          // (vec = 1: the first)
+    t.gran = std::gcd(D, vec);
     t.rows = (int)c.positions;
     const int most = backward ? backward_packs(t.gran, vec) : FORWARD_PACKS;
     // tiles of rows' segments of so many bytes, or of a piece if that is more
