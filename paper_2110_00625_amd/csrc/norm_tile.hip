@@ -111,9 +111,12 @@ bool rows_tiles(const NormCall& c, int vec, int elem, bool backward, NormTiles* 
         return finish(c, backward, &n->whole);
     }
     if (least / vec > LANES) return false;
-    // whole lines of a row, or, where no run of groups is made of them, longer segments (three images of 127x129, 320 channels in 32 groups,
-    // bf16, backward: segments of 80 bytes 52 us, 160 47, 320 44, 640 53; two of 256x256x128, forward: 128 bytes 27 us, 256 31)
-    cut(128);
+    // Whole lines of a row (forward: two of 256x256x128 in bf16 128 bytes 24 us, 256 25).  Longer segments where no run of groups is made of lines
+    // (backward: three images of 127x129, 320 channels in 32 groups, bf16: 80 bytes 52 us, 160 47, 320 44, 640 53), and in the backward pass where
+    // a workgroup has many turns to go (128 bytes / 512: nineteen turns, nine images of 8964 positions, 512 channels in fp32, 183 / 167;
+    // fourteen, three of 19162, 1024 in bf16, 127 / 120; eight, sixteen of 4096, 512 in bf16, 70 / 68; but four, four of 16384, 256, 34 / 37).
+    const int64_t turns = images * c.positions * c.channels / vec / (SUM_GROUPS * LANES * GRAD_PACKS);
+    cut(backward && turns >= 6 ? 512 : 128);
     if ((int64_t)t.channels * elem % 128) cut(512);
     t.lane_rows = std::max(1, LANES / t.cols);
     return twice(c, backward, t, c.positions, n);
