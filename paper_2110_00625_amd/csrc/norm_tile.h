@@ -1,7 +1,7 @@
 // Group norm in tiles that stay in registers: what the forward and the backward kernels share.
 //
-// A tile is some channels (whole groups) of a run of an image's positions.  A lane owns packs of V elements (16 bytes; one element
-// where no pack fits), NV of them: always the same V channels, at positions `lane_rows` apart, so that parameters and sums of a channel
+// A tile is some channels (whole groups) of a run of an image's positions.  A lane owns packs of V elements (16 bytes, or 8 of
+// bf16; one element where no pack fits), NV of them: always the same V channels, at positions `lane_rows` apart, so that parameters and sums of a channel
 // stay in the lane's registers, and a wavefront reads and writes whole segments of rows.
 //
 //   rows   V divides the channels: a row is a position, a pack never leaves it.
@@ -68,15 +68,18 @@ template <class E> hipError_t tiled_forward(const NormCall& c, const NormTiles& 
 template <class E> hipError_t tiled_backward(const NormCall& c, const NormTiles& t, void* workspace, hipStream_t st);
 
 // f(constants: elements of a pack, flat, elements of it in one group) of a tile
-template <class E, class F> hipError_t with_layout(const Tile& t, F f) {
-    constexpr int V = 16 / (int)sizeof(E);
+template <int V, class F> hipError_t with_granules(const Tile& t, F f) {
     constexpr std::integral_constant<int, V> pack = {};
-    constexpr std::integral_constant<int, 1> one = {};
-    if (t.vec == 1) return f(one, std::false_type(), one);
-    if (t.flat) return f(pack, std::true_type(), one);
     if (t.gran == V) return f(pack, std::false_type(), pack);
     if (t.gran == V / 2) return f(pack, std::false_type(), std::integral_constant<int, V / 2>());
-    return t.gran == 2 ? f(pack, std::false_type(), std::integral_constant<int, 2>()) : f(pack, std::false_type(), one);
+    return t.gran == 2 ? f(pack, std::false_type(), std::integral_constant<int, 2>()) : f(pack, std::false_type(), std::integral_constant<int, 1>());
+}
+template <class E, class F> hipError_t with_layout(const Tile& t, F f) {
+    constexpr int V = 16 / (int)sizeof(E);
+    constexpr std::integral_constant<int, 1> one = {};
+    if (t.vec == 1) return f(one, std::false_type(), one);
+    if (t.flat) return f(std::integral_constant<int, V>(), std::true_type(), one);
+    return t.vec == V ? with_granules<V>(t, f) : with_granules<4>(t, f);
 }
 // f(constants: SiLU, dropout)
 template <class F> hipError_t with_options(const NormCall& c, F f) {
@@ -316,8 +319,8 @@ __device__ __forceinline__ void lane_parameters(const NormCall& c, const Tile& t
 
 // bf16 packs stay packed between their uses (the compiler would keep their floats, twice the registers).
 template <class P> __device__ __forceinline__ void keep_packed(P& v) {
-    if constexpr (sizeof(P) == 16 && sizeof(v[0]) == 2) {
-        typedef int words __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(P) >= 8 && sizeof(v[0]) == 2) {
+        typedef int words __attribute__((ext_vector_type(sizeof(P) / 4)));
         words w = __builtin_bit_cast(words, v);
         asm volatile("" : "+v"(w));
         v = __builtin_bit_cast(P, w);

@@ -154,6 +154,9 @@ bool flat_tiles(const NormCall& c, int vec, int most, bool backward, NormTiles* 
 bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t) {
     const int elem = c.dtype == KAVG_BF16 ? 2 : 4, vec = 16 / elem;
     if (c.channels % vec == 0) return rows_tiles(c, vec, elem, backward, t);
+    // packs of half the bytes rather than flat (3680 images of 85 positions, 380 channels in bf16, forward 133 us / 244; 64 of 1024, 100 channels 12.5 / 25.5,
+    // backward 20 / 32; 4080 of 180, 12 channels, backward 22 / 33)
+    if (c.channels % 4 == 0 && rows_tiles(c, 4, elem, backward, t)) return true;
     if (contiguous && flat_tiles(c, vec, backward ? backward_packs(1, vec) : FLAT_PACKS, backward, t)) return true;
     return rows_tiles(c, 1, elem, backward, t);
 }
