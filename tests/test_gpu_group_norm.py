@@ -91,7 +91,8 @@ def test_against_64_bits(shape, dtype):
 @pytest.mark.parametrize("shape", [(1, 1, 20000, 64, 64), (1, 1, 20000, 33, 33), (2, 3, 50, 40, 10), (1, 1, 20000, 40, 10), (1, 3, 784, 40, 5), (1, 1, 5000, 320, 32),
                                    (1, 1, 2048, 32, 4), (1, 1, 2049, 32, 4), (2, 300, 2, 16, 2), (1, 9, 1, 8, 8), (1, 2, 3, 8192, 1),
                                    (1, 3, 2, 16400, 1), (2, 2, 5, 9001, 1), (1, 2, 40, 1031, 1), (2, 3, 1, 12297, 3), (1, 1, 20000, 20, 5),
-                                   (2, 3, 50, 36, 18), (1, 2, 300, 60, 12), (1, 1, 5000, 60, 12), (1, 3, 40, 380, 38), (3, 5, 16, 4, 2)], ids=lambda s: "-".join(map(str, s)))
+                                   (2, 3, 50, 36, 18), (1, 2, 300, 60, 12), (1, 1, 5000, 60, 12), (1, 3, 40, 380, 38), (3, 5, 16, 4, 2),
+                                   (2, 3, 51, 22, 11), (1, 2, 300, 54, 2), (1, 1, 20001, 10, 5), (1, 1, 5000, 70, 14), (1, 40, 3, 2, 1)], ids=lambda s: "-".join(map(str, s)))
 def test_edges_of_the_tiles(shape, dtype):
     for k, (act, drop) in enumerate(((kavg.KAVG_ACT_SILU, 0.1), (kavg.KAVG_ACT_RELU, 0.0))):
         x, dy, w, b = _inputs(shape, dtype, 31 * k + shape[2])
@@ -99,7 +100,7 @@ def test_edges_of_the_tiles(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
-@pytest.mark.parametrize("shape", [(2, 3, 31, 24, 3), (1, 2, 1030, 64, 8), (2, 2, 20, 21, 3), (2, 2, 33, 20, 5)], ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("shape", [(2, 3, 31, 24, 3), (1, 2, 1030, 64, 8), (2, 2, 20, 21, 3), (2, 2, 33, 20, 5), (2, 2, 33, 14, 7)], ids=lambda s: "-".join(map(str, s)))
 @pytest.mark.parametrize("pad,first", [(8, 0), (8, 8), (3, 1), (1, 0)])
 def test_channels_of_a_wider_tensor(shape, dtype, pad, first):
     """x, dy and the output are channel slices of longer rows, whose other values stay what they are; images and sets lie apart."""
