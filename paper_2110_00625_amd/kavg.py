@@ -259,9 +259,17 @@ def _norm(x, groups, eps, activation, drop, seed, site):
     if len(shape) != 3 and len(shape) != 4:
         _bad("x has %d dimensions: [sets, images, positions, channels] or [images, positions, channels] is wanted" % len(shape))
     try:
+        if groups < 1 or shape[-1] % groups:             # (before the statistics are allocated)
+            _bad("%d groups of %d channels" % (groups, shape[-1]))
         return _NORM.pack(code, activation, shape[0] if len(shape) == 4 else 1, shape[-3], shape[-2], shape[-1], groups, eps, 0, drop, seed, site)
-    except struct.error as e:
+    except (struct.error, TypeError) as e:
         _bad(str(e))
+
+
+def _shapes(x, groups):
+    """Shapes of the parameters and of the statistics (plain tuples: slices of a torch.Size take longer)."""
+    shape = x.shape
+    return ((shape[0], shape[3]), (shape[0], shape[1], groups)) if len(shape) == 4 else ((shape[2],), (shape[0], groups))
 
 
 def _workspace(norm, backward, x, like):
@@ -291,13 +299,12 @@ def kavg_group_norm(x, weight, bias, groups, eps=1e-5, activation=KAVG_ACT_NONE,
     torch = _torch_module or _torch()
     norm = _norm(x, groups, eps, activation, drop, seed, site)
     y = _output(x, out)
-    channels = x.shape[::3] if x.dim() == 4 else x.shape[-1:]
+    channels, statistics = _shapes(x, groups)
     w, ws = _params(weight, x, channels, "weight")
     b, bs = _params(bias, x, channels, "bias")
     mean = rstd = m = r = None
     if stats:
-        shape = x.shape[:-2] + (groups,)
-        mean = torch.empty(shape, dtype=torch.float32, device=x.device) if weight is None else weight.new_empty(shape)
+        mean = torch.empty(statistics, dtype=torch.float32, device=x.device) if weight is None else weight.new_empty(statistics)
         rstd = torch.empty_like(mean)
         m, r = mean.data_ptr(), rstd.data_ptr()
     args = (norm, _images(x, "x"), w, ws, b, bs, _images(y, "out"), m, r)
@@ -318,13 +325,12 @@ def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation
     torch = _torch_module or _torch()
     norm = _norm(x, groups, 1.0, activation, drop, seed, site)       # (eps went into rstd)
     _like(dy, x, "dy")
-    shape = x.shape[:-2] + (groups,)
+    channels, statistics = _shapes(x, groups)
     for t in (mean, rstd):
-        if t.shape != shape or t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous():
+        if t.shape != statistics or t.dtype is not torch.float32 or t.device != x.device or not t.is_contiguous():
             _bad("mean, rstd are not what kavg_group_norm returned")
     block, at, nbytes = _workspace(norm, 1, x, mean)
     dx = _output(x, out)
-    channels = x.shape[::3] if x.dim() == 4 else x.shape[-1:]
     w, ws = _params(weight, x, channels, "weight")
     b, bs = _params(bias, x, channels, "bias")
     dweight, dbias = _gradient(dweight, weight), _gradient(dbias, bias)

@@ -128,7 +128,7 @@ def test_binding_refuses_what_does_not_fit(lib):
     f, g = kavg.kavg_group_norm, kavg.kavg_group_norm_backward
     nchw = torch.zeros(2, 3, 8, 5, device=d).transpose(2, 3)
     calls = [
-        lambda: f(nchw, w, b, 2), lambda: f(x.half(), w, b, 2), lambda: f(x[0, 0], w[0], b[0], 2), lambda: f(x, w, b, 3), lambda: f(x, w, b, 0),
+        lambda: f(nchw, w, b, 2), lambda: f(x.half(), w, b, 2), lambda: f(x[0, 0], w[0], b[0], 2), lambda: f(x, w, b, 3), lambda: f(x, w, b, 0), lambda: f(x, w, b, -1, stats=True), lambda: f(x, w, b, 16, stats=True), lambda: f(x, w, b, None),
         lambda: f(x, w, b, 2, eps=0.0), lambda: f(x, w, b, 2, activation=9), lambda: f(x, w, b, 2, drop=1.5), lambda: f(x, w, b, 2, seed=-1),
         lambda: f(x, w, b, 2, site=1 << 24), lambda: f(x, w[0], b, 2), lambda: f(x, w.bfloat16(), b, 2), lambda: f(x, w.cpu(), b, 2),
         lambda: f(x, w.t().contiguous().t(), b, 2), lambda: f(x, w, b, 2, out=x.bfloat16()), lambda: f(x, w, b, 2, out=x[:1]),
