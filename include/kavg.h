@@ -360,7 +360,8 @@ typedef struct {
     uint64_t seed, site;
 } kavg_norm;
 
-/* Bytes of device workspace a call wants (may be 0); 16-byte aligned. */
+/* Bytes of device workspace a call wants (may be 0); 16-byte aligned.  A call that is given fewer than it needs says so
+ * (KAVG_ENOMEM) before it launches anything. */
 int kavg_group_norm_workspace(const kavg_norm* norm, int backward, size_t* bytes);
 
 /* weight, bias: learner j's [channels] at weight + j*weight_stride; NULL = ones / zeros.  mean, rstd: [sets][images]
@@ -387,8 +388,8 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
  * site: the place in the model and the step (a number of the caller's, < 2^24), so that one seed serves them all.
  * The backward call with the same drop, seed and site applies the same mask to dy (the residual's gradient is dy itself).
  * y may be x or residual, dx may be dy (same strides).
- * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, 2^30 columns or more in rows that lie apart, drop outside [0, 1], site >= 2^24, unknown dtype, null pointers,
- * an output whose rows overlap. */
+ * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, 2^30 columns or more in rows that lie apart, drop outside
+ * [0, 1], site >= 2^24, unknown dtype, null pointers, an output whose rows overlap. */
 int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
                  int64_t rows, int64_t cols, int dtype, double drop, uint64_t seed, uint64_t site, void* hip_stream);
 int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int64_t rows, int64_t cols,

@@ -99,8 +99,8 @@ bool rows_tiles(const NormCall& c, int vec, int elem, bool backward, NormTiles* 
         t.nv = fit(MOST_LANES);
     }
     // Else segments of 128 bytes, or of 64 or 32 where only these bring an image into a workgroup of 512 lanes, so that two share a compute
-    // unit (one of 1024 lanes: 32x32x64 in bf16 with twice the segment, backward 138 us against 122; forward, 128 channels, a workgroup of 1024
-    // lanes with eight packs each against one of 512 with sixteen 222 against 143).
+    // unit (32x32x64 in bf16, backward: twice the segment for 1024 lanes 124 us against 112; 32x32x128, forward: half the segment for 256 lanes 129
+    // against 111).
     for (const int lanes : {LANES, MOST_LANES})
         for (int64_t segment = 128; segment >= 32 && !t.nv; segment /= 2) { cut(segment); t.nv = fit(lanes); }
     if (t.nv) {
