@@ -100,9 +100,11 @@ bool rows_tiles(const NormCall& c, int vec, int elem, bool backward, NormTiles* 
     }
     // Else segments of 128 bytes, or of 64 or 32 where only these bring an image into a workgroup of 512 lanes, so that two share a compute
     // unit (32x32x64 in bf16, backward: twice the segment for 1024 lanes 124 us against 112; 32x32x128, forward: half the segment for 256 lanes 129
-    // against 111).
+    // against 111).  Then the same for 1024 lanes, but no 32 bytes: those cost more than reading the image twice (1225 positions, 64 channels in
+    // groups of four, bf16, backward, us, whole / twice: 80 images 30 / 24, 1024 227 / 164; but in 64 bytes, 64 images of 1000, 256 channels,
+    // 35 / 37, in 128, 64 of 2000, 512 channels, forward 73 / 90, 256 of 500, backward 119 / 141).
     for (const int lanes : {LANES, MOST_LANES})
-        for (int64_t segment = 128; segment >= 32 && !t.nv; segment /= 2) { cut(segment); t.nv = fit(lanes); }
+        for (int64_t segment = 128; segment >= (lanes == LANES ? 32 : 64) && !t.nv; segment /= 2) { cut(segment); t.nv = fit(lanes); }
     if (t.nv) {
         t.lane_rows = (int)up(c.positions, t.nv);
         t.chunks = 1;
@@ -136,6 +138,7 @@ bool flat_tiles(const NormCall& c, int vec, int most, bool backward, NormTiles* 
     t.blocks = 1;
     t.lane_rows = 1;
     const auto lanes = [&](int nv) { return up(up(packs, nv), period) * period; };
+    // (1024 lanes rather than two readings: 256 images of 784 positions, 45 channels in bf16, forward 21 us / 34; of 361, 33, backward 18.5 / 24)
     t.nv = packs_per_lane(most, LANES, images, lanes);
     if (!t.nv) t.nv = packs_per_lane(most, MOST_LANES, images, lanes);
     t.cols = (int)(t.nv ? lanes(t.nv) : LANES / period * period);
