@@ -100,7 +100,7 @@ def test_edges_of_the_tiles(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
-@pytest.mark.parametrize("shape", [(2, 3, 31, 24, 3), (1, 2, 1030, 64, 8), (2, 2, 20, 21, 3), (2, 2, 33, 20, 5), (2, 2, 33, 14, 7)], ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("shape", [(2, 3, 31, 24, 3), (1, 2, 1030, 64, 8), (2, 2, 20, 21, 3), (2, 2, 33, 20, 5), (2, 2, 33, 14, 7), (2, 2, 20, 1031, 1)], ids=lambda s: "-".join(map(str, s)))
 @pytest.mark.parametrize("pad,first", [(8, 0), (8, 8), (3, 1), (1, 0)])
 def test_channels_of_a_wider_tensor(shape, dtype, pad, first):
     """x, dy and the output are channel slices of longer rows, whose other values stay what they are; images and sets lie apart."""
@@ -149,7 +149,7 @@ def test_parameters_inside_replicas():
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
-@pytest.mark.parametrize("shape", [(2, 2, 9, 16, 4), (1, 1, 3000, 64, 8)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 2, 9, 16, 4), (1, 1, 3000, 64, 8), (2, 1, 12, 1031, 1)], ids=str)
 def test_without_parameters_and_one_set(shape, dtype):
     J, I, S, C, G = shape
     x, dy, _, _ = _inputs(shape, dtype, 7)
@@ -168,7 +168,7 @@ def test_without_parameters_and_one_set(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
-@pytest.mark.parametrize("shape", [(1, 3, 40, 24, 3), (1, 2, 5000, 64, 8), (1, 1, 70, 21, 7)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 3, 40, 24, 3), (1, 2, 5000, 64, 8), (1, 1, 70, 21, 7), (1, 2, 90, 1031, 1)], ids=str)
 def test_in_place(shape, dtype):
     x, dy, w, b = _inputs(shape, dtype, 8)
     opt = dict(activation=kavg.KAVG_ACT_SILU, drop=0.1, seed=5)
@@ -194,7 +194,7 @@ def test_gradient_of_a_sum_is_a_broadcast_input():
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=("f32", "bf16"))
-@pytest.mark.parametrize("shape", [(1, 3, 40, 20, 5), (1, 3, 1500, 64, 8), (1, 2, 35, 21, 7), (1, 3, 9000, 24, 4)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 3, 40, 20, 5), (1, 3, 1500, 64, 8), (1, 2, 35, 21, 7), (1, 3, 9000, 24, 4), (1, 3, 20, 2062, 2)], ids=str)
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
 def test_one_value_that_is_no_number_stays_in_its_group(shape, dtype, value):
     _, I, S, C, G = shape
