@@ -316,8 +316,7 @@ template <class E>
 hipError_t backward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
     if (!c.sets) return hipSuccess;
     NormTiles t;
-    const bool contiguous = c.xs.row == c.channels && c.dys.row == c.channels && c.outs.row == c.channels;
-    const bool tiled = c.images && c.positions && norm_tiles(c, contiguous, true, &t);
+    const bool tiled = c.images && c.positions && call_tiles(c, true, &t);
     const hipError_t e = check(tiled ? norm_workspace(c, t, true) : wide_workspace(c), workspace, bytes);
     if (e != hipSuccess) return e;
     if (tiled) return tiled_backward<E>(c, t, workspace, st);
@@ -328,8 +327,7 @@ template <class E>
 hipError_t forward(const NormCall& c, void* workspace, size_t bytes, hipStream_t st) {
     if (!(c.sets * c.images)) return hipSuccess;
     NormTiles t;
-    const bool contiguous = c.xs.row == c.channels && c.outs.row == c.channels;
-    const bool tiled = c.positions && norm_tiles(c, contiguous, false, &t);
+    const bool tiled = c.positions && call_tiles(c, false, &t);
     const hipError_t e = check(tiled ? norm_workspace(c, t, false) : wide_workspace(c), workspace, bytes);
     if (e != hipSuccess) return e;
     return tiled ? tiled_forward<E>(c, t, workspace, st) : wide_forward<E>(c, (float*)workspace, st);

@@ -53,6 +53,9 @@ inline int64_t extent_of(const NormCall& c, const Strides& s) {
 
 // false: no tile fits (groups too wide for a workgroup)
 bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t);
+// The same of a call with its operands: flat only where the positions of each lie end to end and what is read holds a pack at least.  (A pack
+// at the end of a tensor is moved to end with it, see tile_load; images that share memory make a tensor shorter than its elements are many.)
+bool call_tiles(const NormCall& c, bool backward, NormTiles* t);
 size_t norm_workspace(const NormCall& c, const NormTiles& t, bool backward);
 // values of a group in a whole chunk, in positions
 inline int64_t chunk_positions(const NormCall& c, const Tile& t) { return (int64_t)t.nv * (t.flat ? (int64_t)t.cols * t.vec / c.channels : t.lane_rows); }

@@ -164,6 +164,12 @@ bool norm_tiles(const NormCall& c, bool contiguous, bool backward, NormTiles* t)
     return rows_tiles(c, 1, elem, backward, t);
 }
 
+bool call_tiles(const NormCall& c, bool backward, NormTiles* t) {
+    const int vec = c.dtype == KAVG_BF16 ? 8 : 4;
+    const auto read_flat = [&](const Strides& s) { return s.row == c.channels && extent_of(c, s) >= vec; };
+    return norm_tiles(c, read_flat(c.xs) && (!backward || read_flat(c.dys)) && c.outs.row == c.channels, backward, t);
+}
+
 size_t norm_workspace(const NormCall& c, const NormTiles& t, bool backward) {
     const size_t images = (size_t)(c.sets * c.images), groups = images * c.groups, chunks = t.whole.nv ? 1 : t.sums.chunks;
     if (!backward) return t.whole.nv ? 0 : (2 * groups * chunks + 2 * groups) * sizeof(float);
