@@ -38,7 +38,7 @@ class _Dropout(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         dx = kavg.kavg_dropout_backward(dy.contiguous(), **ctx.options) if ctx.needs_input_grad[0] else None
-        return dx, dy, None
+        return dx, dy if ctx.needs_input_grad[1] else None, None
 
 
 def group_norm(x, weight, bias, groups, eps=1e-5, activation=None, drop=0.0, seed=0, site=0):
