@@ -53,19 +53,24 @@ template <int V, bool FLAT, int GRAN> struct Channels {
             if (SILU) { w[i] *= SILU_SCALE; b[i] *= SILU_SCALE; }
         }
     }
-    // what dx takes of its group: r A - m r^2 B and r^2 B
-    __device__ __forceinline__ void group_part(int a, float sum, float sum_xh, float (&rest)[A], float (&rrB)[A]) const {
+    // what dx takes of its group: r A and r^2 B
+    __device__ __forceinline__ void group_part(int a, float sum, float sum_xh, float (&rA)[A], float (&rrB)[A]) const {
         rrB[a] = rstd[a] * rstd[a] * sum_xh;
-        rest[a] = rstd[a] * sum - mean[a] * rrB[a];
+        rA[a] = rstd[a] * sum;
+    }
+    // of a pack: x - m
+    template <class P> __device__ __forceinline__ void distances(const P& x, float (&d)[V]) const {
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = to_float(x[i]) - mean[i / GRAN];
     }
     // of pack k: x - m, and dz without drop's scale
     template <class E, bool SILU, bool DROP>
     __device__ __forceinline__ void gradient(const NormCall& c, int k, const typename Pack<E, V>::type& x, typename Pack<E, V>::type dy, float (&d)[V], float (&g)[V]) const {
         if (DROP) mask.template drop<E>(c.drop, k, dy);
         float z[V];
+        distances(x, d);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            d[i] = to_float(x[i]) - mean[i / GRAN];
             z[i] = d[i] * w[i] + b[i];
             g[i] = to_float(dy[i]);
         }
@@ -186,14 +191,14 @@ template <int V, bool FLAT> __device__ __forceinline__ void group_means(const No
     }
 }
 
-// dx of pack k from dz (without scale) and x: r weight_c dz - x r^2 B - (r A - m r^2 B).  (m r^2 B on its own is off by m r 2^-24 of r B, as is
-// what m's own rounding does to it.)
-template <bool SILU, class E, int V, bool FLAT, int GRAN>
+// dx of pack k from dz (without scale) and x - m: r weight_c dz - ((x - m) r^2 B + r A).  (x r^2 B less a constant of the group m r^2 B would be an
+// instruction per element less and no faster, and off by m r 2^-24 of r B: a mean of ten thousand spreads in fp32, by 9e-4 of dx.)
+template <class E, bool SILU, int V, bool FLAT, int GRAN>
 __device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const Lane<V, FLAT>& l, const Channels<V, FLAT, GRAN>& h, const Place<V, FLAT>& to, int k,
-                                         const typename Pack<E, V>::type& x, float (&g)[V], const float (&rest)[V / GRAN], const float (&rrB)[V / GRAN]) {
+                                         const float (&d)[V], float (&g)[V], const float (&rA)[V / GRAN], const float (&rrB)[V / GRAN]) {
     const float scale = c.drop.scale * (SILU ? SILU_BACK : 1.f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) g[i] = __builtin_fmaf(g[i], h.w[i] * scale, -__builtin_fmaf(to_float(x[i]), rrB[i / GRAN], rest[i / GRAN]));
+    for (int i = 0; i < V; ++i) g[i] = __builtin_fmaf(g[i], h.w[i] * scale, -__builtin_fmaf(d[i], rrB[i / GRAN], rA[i / GRAN]));
     tile_store<E, V, FLAT>(t, l, (E*)c.out, to, k, packed<E, V>(g));
 }
 
@@ -239,13 +244,15 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     __syncthreads();
     group_means(c, t, l, s);
     __syncthreads();
-    float rest[A], rrB[A];
+    float rA[A], rrB[A];
 #pragma unroll
-    for (int a = 0; a < A; ++a) h.group_part(a, s.g0[l.unit * t.groups + h.group[a]], s.g0[(t.units + l.unit) * t.groups + h.group[a]], rest, rrB);
+    for (int a = 0; a < A; ++a) h.group_part(a, s.g0[l.unit * t.groups + h.group[a]], s.g0[(t.units + l.unit) * t.groups + h.group[a]], rA, rrB);
     const Place<V, FLAT> to(c, t, l, c.outs);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        write_dx<SILU, E, V, FLAT, GRAN>(c, t, l, h, to, k, xv[k], dz[k], rest, rrB);
+        float d[V];
+        h.distances(xv[k], d);
+        write_dx<E, SILU>(c, t, l, h, to, k, d, dz[k], rA, rrB);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -333,7 +340,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
             gn[k] = tile_load<E, V, FLAT, whole.value>(t, l, (const E*)c.dy, at, f.dy_extent, first + k);
         });
     };
-    float rest[A], rrB[A];
+    float rA[A], rrB[A];
     if (f.group_sums) {
         float gA[A], gB[A];
 #pragma unroll
@@ -341,7 +348,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
         packs_from(t.nv - NV);
         h.template scale<SILU>();
 #pragma unroll
-        for (int a = 0; a < A; ++a) h.group_part(a, gA[a], gB[a], rest, rrB);
+        for (int a = 0; a < A; ++a) h.group_part(a, gA[a], gB[a], rA, rrB);
     } else {
         // every workgroup adds up the chunks of its channels, JOINED_PARTS of them per lane at most
         const SumSpace s(lds, 0, t.channels, t.groups, blockDim.x);
@@ -374,7 +381,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
         group_means(c, t, l, s);
         __syncthreads();
 #pragma unroll
-        for (int a = 0; a < A; ++a) h.group_part(a, s.g0[h.group[a]], s.g0[t.groups + h.group[a]], rest, rrB);
+        for (int a = 0; a < A; ++a) h.group_part(a, s.g0[h.group[a]], s.g0[t.groups + h.group[a]], rA, rrB);
     }
     for (int turn = t.nv - NV; turn >= 0; turn -= NV) {
         typename Pack<E, V>::type xv[NV], gv[NV];
@@ -385,7 +392,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
         for (int k = 0; k < NV; ++k) {
             float d[V], g[V];
             h.template gradient<E, SILU, DROP>(c, turn + k, xv[k], gv[k], d, g);
-            write_dx<SILU, E, V, FLAT, GRAN>(c, t, l, h, to, turn + k, xv[k], g, rest, rrB);
+            write_dx<E, SILU>(c, t, l, h, to, turn + k, d, g, rA, rrB);
         }
     }
 }
