@@ -37,28 +37,28 @@ template <class E, int V, int NV, int GRAN>
 __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&xv)[NV], float (&mean)[V / GRAN], float (&sq)[V / GRAN]) {
     constexpr int A = V / GRAN;
     float sum[A];
+    bool lost[A];
 #pragma unroll
-    for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
+    for (int a = 0; a < A; ++a) { sum[a] = sq[a] = 0.f; lost[a] = true; }
     if constexpr (sizeof(E) == 2 && GRAN > 1) {
         // bf16: sums of values and of squares by dot products (half an instruction per element each; a mean and distances from it are four).
-        // n v = sum x^2 - n m^2 cancels where the mean is large against the spread: a wavefront that loses more than two bits in any lane
-        // takes the distances after all.
+        // n v = sum x^2 - n m^2 cancels where the mean is large against the spread: a sum that loses more than two bits is taken of the
+        // distances after all, each for itself, so that no group's result depends on another one's values.
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
             for (int a = 0; a < A; ++a) { sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]); sq[a] = pack_squares<GRAN>(xv[k], a * GRAN, sq[a]); }
         }
-        bool lost = false;
+        bool any = false;
 #pragma unroll
         for (int a = 0; a < A; ++a) {
             mean[a] = sum[a] * (1.f / (NV * GRAN));
             const float all = sq[a];
             sq[a] = all - sum[a] * mean[a];
-            lost |= !(sq[a] >= 0.25f * all);
+            lost[a] = !(sq[a] >= 0.25f * all);
+            any |= lost[a];
         }
-        if (!__any(lost)) return;
-#pragma unroll
-        for (int a = 0; a < A; ++a) sq[a] = 0.f;
+        if (!__any(any)) return;
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -68,13 +68,18 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
 #pragma unroll
         for (int a = 0; a < A; ++a) mean[a] = sum[a] * (1.f / (NV * GRAN));
     }
+    float far[A];
+#pragma unroll
+    for (int a = 0; a < A; ++a) far[a] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         auto v = xv[k];
         keep_packed(v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; sq[i / GRAN] += d * d; }
+        for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; far[i / GRAN] += d * d; }
     }
+#pragma unroll
+    for (int a = 0; a < A; ++a) sq[a] = lost[a] ? far[a] : sq[a];
 }
 
 // The same of packs from the `first`-th on of which not all are the image's, and how many are (flat: of each element): `whole` of them, and one
