@@ -55,7 +55,7 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
             mean[a] = sum[a] * (1.f / (NV * GRAN));
             const float all = sq[a];
             sq[a] = all - sum[a] * mean[a];
-            lost[a] = !(sq[a] >= 0.25f * all);
+            lost[a] = !(__builtin_fmaf(-0.25f, all, sq[a]) >= 0.f);         // (squares whose sum overflows: NaN, and lost)
             any |= lost[a];
         }
         if (!__any(any)) return;
