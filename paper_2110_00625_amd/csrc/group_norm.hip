@@ -4,7 +4,8 @@
 // Backward, with dz = act'(z) drop(dy) and h = weight_c dz:
 //     dbias_c = sum dz,  dweight_c = sum dz xh  (over a learner's images and positions),
 //     dx = r (h - mean h - xh mean(h xh))       (means over the group).
-// Statistics and sums are fp32; the variance is taken about the mean, in a second sum.
+// Statistics are fp32; the variance is taken about the mean, in a second sum.  Sums of any number of terms are 64 bits wide, of up to some
+// hundred fp32.
 //
 // Most calls run on tiles in registers (norm_tile.h).  What no tile takes, groups wider than 8192 channels (fp32: 4096), odd ones of more than
 // some hundred, and counts of tiles past 2^30, runs on the kernels here: a lane per channel goes along its chunk of the positions, sums per channel
@@ -77,14 +78,15 @@ template <class F> __device__ __forceinline__ void for_rows(int64_t rows, F f) {
     for (; s < rows; ++s) f(s, std::integral_constant<int, 1>());
 }
 
-// mean and squared distances from it of a channel in a chunk, eight values at a time, joined as means of parts
+// mean and squared distances from it of a channel in a chunk, eight values at a time, joined as means of parts (in 64 bits: a chunk may be the whole
+// image, of any length)
 template <class E>
 __global__ void __launch_bounds__(T) norm_wide_moments_kernel(WideCall f) {
     for (int64_t image = blockIdx.z; image < f.n.sets * f.n.images; image += gridDim.z) {
         const WidePlace l(f, image);
         if (!l.on) continue;
         const E* x = l.at<const E>(f.n.x, f.n.xs);
-        float mean = 0.f, sq = 0.f;
+        double mean = 0., sq = 0.;
         for_rows(l.rows, [&](int64_t s, auto some) {
             constexpr int K = some.value;
             float v[K], sum = 0.f, q = 0.f;
@@ -95,13 +97,13 @@ __global__ void __launch_bounds__(T) norm_wide_moments_kernel(WideCall f) {
             const float m = sum * (1.f / K);
 #pragma unroll
             for (int i = 0; i < K; ++i) q += (v[i] - m) * (v[i] - m);
-            const float d = m - mean, share = (float)K / (float)(s + K);
+            const float d = (float)(m - mean), share = (float)K / (float)(s + K);
             mean += d * share;
             sq += q + d * d * ((float)s * share);
         });
         float* to = l.parts(f);
-        to[0] = mean;
-        to[f.n.channels] = sq;
+        to[0] = (float)mean;
+        to[f.n.channels] = (float)sq;
     }
 }
 
@@ -138,16 +140,17 @@ __global__ void __launch_bounds__(JOIN) norm_wide_join_kernel(WideCall f) {
     for (int64_t g = blockIdx.x; g < c.sets * c.images * c.groups; g += gridDim.x) {
         const int64_t image = g / c.groups;
         const int first = (int)(g - image * c.groups) * D;
-        float mean = 0.f, sum = 0.f;
+        float mean = 0.f, var = 0.f;
         if (f.chunks) {
+            double sum = 0.;
             for_parts(f, image, first, [&](int j, int, float m, float) { sum += (j < f.chunks - 1 ? whole : last) * m; });
-            mean = block_sum(sum, lds) / n;
-            sum = 0.f;
+            mean = block_sum((float)sum, lds) / n;
+            sum = 0.;
             for_parts(f, image, first, [&](int j, int, float m, float q) { sum += q + (j < f.chunks - 1 ? whole : last) * (m - mean) * (m - mean); });
-            sum = block_sum(sum, lds) / n;
+            var = block_sum((float)sum, lds) / n;
         }
         if (threadIdx.x == 0) {
-            const float r = 1.f / sqrtf(sum + c.eps);
+            const float r = 1.f / sqrtf(var + c.eps);
             f.mean[g] = mean;
             f.rstd[g] = r;
             if (c.mean) { c.mean[g] = mean; c.rstd[g] = r; }
@@ -165,15 +168,14 @@ __global__ void __launch_bounds__(JOIN) norm_wide_group_kernel(WideCall f, float
         const int64_t image = g / c.groups;
         const int first = (int)(g - image * c.groups) * D;
         const float* w = c.weight ? c.weight + (uint32_t)image / (uint32_t)c.images * c.weight_stride + first : nullptr;
-        float a = 0.f, b = 0.f;
+        double a = 0., b = 0.;
         for_parts(f, image, first, [&](int, int d, float dz, float dzx) {
             const float wd = w ? w[d] : 1.f;
             a += wd * dz;
             b += wd * dzx;
         });
-        a = block_sum(a, lds);
-        b = block_sum(b, lds);
-        if (threadIdx.x == 0) { group_sums[2 * g] = a / n; group_sums[2 * g + 1] = b / n; }
+        const float A = block_sum((float)a, lds) / n, B = block_sum((float)b, lds) / n;
+        if (threadIdx.x == 0) { group_sums[2 * g] = A; group_sums[2 * g + 1] = B; }
     }
 }
 
@@ -204,9 +206,9 @@ __global__ void __launch_bounds__(T) norm_wide_apply_kernel(WideCall f) {
     }
 }
 
-// f(position in the chunk, dz, x - m) of a lane's channel
-template <class E, bool SILU, class F>
-__device__ __forceinline__ void for_gradients(const NormCall& c, const WidePlace& l, float w, float mean, float rstd, F f) {
+// f(position in the chunk, dz, x - m) of a lane's channel, and after() behind every ROWS of them, or one
+template <class E, bool SILU, class F, class After>
+__device__ __forceinline__ void for_gradients(const NormCall& c, const WidePlace& l, float w, float mean, float rstd, F f, After after) {
     const E* x = l.at<const E>(c.x, c.xs);
     const E* dy = l.at<const E>(c.dy, c.dys);
     const float b = c.bias ? c.bias[l.set * c.bias_stride + l.ch] : 0.f;
@@ -222,6 +224,7 @@ __device__ __forceinline__ void for_gradients(const NormCall& c, const WidePlace
             if (c.drop.threshold) g[i] = drop_keeps(c.drop, number + (uint64_t)(s + i) * c.channels) ? g[i] * c.drop.scale : 0.f;
             f(s + i, through_slope<SILU>(g[i], SILU ? SILU_SCALE * z : z, c.floor), d);
         }
+        after();
     });
 }
 
@@ -232,11 +235,13 @@ __global__ void __launch_bounds__(T) norm_wide_sums_kernel(WideCall f) {
         const WidePlace l(f, image);
         if (!l.on) continue;
         const float mean = c.mean[l.image * c.groups + l.group], rstd = c.rstd[l.image * c.groups + l.group];
-        float a = 0.f, b = 0.f;
-        for_gradients<E, SILU>(c, l, c.weight ? c.weight[l.set * c.weight_stride + l.ch] : 1.f, mean, rstd, [&](int64_t, float dz, float d) { a += dz; b += dz * d; });
+        double a = 0., b = 0.;
+        float some = 0.f, some_d = 0.f;
+        for_gradients<E, SILU>(c, l, c.weight ? c.weight[l.set * c.weight_stride + l.ch] : 1.f, mean, rstd,
+                               [&](int64_t, float dz, float d) { some += dz; some_d += dz * d; }, [&] { a += some; b += some_d; some = some_d = 0.f; });
         float* to = l.parts(f);
-        to[0] = a;
-        to[c.channels] = b * rstd;
+        to[0] = (float)a;
+        to[c.channels] = (float)b * rstd;
     }
 }
 
@@ -249,7 +254,8 @@ __global__ void __launch_bounds__(T) norm_wide_dx_kernel(WideCall f) {
         const int64_t g = l.image * c.groups + l.group;
         const float w = c.weight ? c.weight[l.set * c.weight_stride + l.ch] : 1.f, mean = c.mean[g], rstd = c.rstd[g], A = f.group_sums[2 * g], B = f.group_sums[2 * g + 1];
         E* dx = l.at<E>(c.out, c.outs);
-        for_gradients<E, SILU>(c, l, w, mean, rstd, [&](int64_t s, float dz, float d) { dx[s * c.outs.row] = from_float<E>(rstd * (w * dz - A - d * rstd * B)); });
+        for_gradients<E, SILU>(c, l, w, mean, rstd,
+                               [&](int64_t s, float dz, float d) { dx[s * c.outs.row] = from_float<E>(rstd * (w * dz - A - d * rstd * B)); }, [] {});
     }
 }
 

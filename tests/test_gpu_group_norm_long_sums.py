@@ -43,3 +43,9 @@ def _x(shape, dtype):
 @pytest.mark.parametrize("shape", [(1, 200000, 1, 64, 8), (1, 300000, 2, 24, 3), (1, 100000, 1, 65, 5), (1, 30000, 5, 513, 1)], ids=lambda s: "-".join(map(str, s)))
 def test_many_images(shape, dtype):
     _check(_x(shape[:4], dtype), shape[4], 0.1)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("images,positions", [(342, 4096), (350, 10007)])
+def test_long_images_of_groups_that_no_tile_takes(images, positions, dtype):
+    _check(_x((1, 1, positions, 513), dtype).expand(1, images, positions, 513), 1, 0.1)
