@@ -277,10 +277,21 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     };
     packs_from(0);
     h.template scale<SILU>();
+    // SUM_RUN packs are added up one after the other, and so are their sums, which wait in the lane's place of the LDS
+    const SumSpace s(lds, blockDim.x * V, t.channels, t.groups, blockDim.x);
+    float *const before0 = s.p0 + threadIdx.x * V, *const before1 = s.p1 + threadIdx.x * V;
     float s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.f;
     for (int turn = 0; turn < t.nv; turn += NV) {
+        if (turn && turn % SUM_RUN == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                before0[i] = turn > SUM_RUN ? before0[i] + s0[i] : s0[i];
+                before1[i] = turn > SUM_RUN ? before1[i] + s1[i] : s1[i];
+                s0[i] = s1[i] = 0.f;
+            }
+        }
         typename Pack<E, V>::type xv[NV], gv[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) { xv[k] = xn[k]; gv[k] = gn[k]; }
@@ -292,7 +303,11 @@ __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
             add_pack<V, FLAT>(l.valid(t, turn + k), d, g, s0, s1);
         }
     }
-    channel_sums(f, l, h, SumSpace(lds, blockDim.x * V, t.channels, t.groups, blockDim.x), s0, s1);
+    if (t.nv > SUM_RUN) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { s0[i] += before0[i]; s1[i] += before1[i]; }
+    }
+    channel_sums(f, l, h, s, s0, s1);
 }
 
 // dweight and dbias: a learner's sums over its images and their chunks.  A workgroup (the largest power of two of its lanes): `wide`
@@ -417,7 +432,7 @@ __global__ void __launch_bounds__(T) norm_group_kernel(BackwardCall f, float* gr
         const int D = c.channels / c.groups, first = (int)(g - image * c.groups) * D;
         const float* p = f.parts + (int64_t)image * f.chunks * 2 * c.channels + first;
         const float* w = c.weight ? c.weight + set * c.weight_stride + first : nullptr;
-        float a = 0.f, b = 0.f;
+        double a = 0., b = 0.;                       // (chunks of any number)
         for (int r = threadIdx.x / D, i = threadIdx.x - r * D; r < f.chunks;) {
             const float wi = w ? w[i] : 1.f;
             a += wi * p[(int64_t)r * 2 * c.channels + i];
@@ -425,9 +440,8 @@ __global__ void __launch_bounds__(T) norm_group_kernel(BackwardCall f, float* gr
             i += T;
             if (i >= D) { const int over = i / D; r += over; i -= over * D; }
         }
-        a = team_sum(a, 64);
-        b = team_sum(b, 64);
-        if (threadIdx.x % 64 == 0) { lds[threadIdx.x / 64] = a; lds[4 + threadIdx.x / 64] = b; }
+        const float wa = team_sum((float)a, 64), wb = team_sum((float)b, 64);
+        if (threadIdx.x % 64 == 0) { lds[threadIdx.x / 64] = wa; lds[4 + threadIdx.x / 64] = wb; }
         __syncthreads();
         if (threadIdx.x < 2) {
             const float* q = lds + 4 * threadIdx.x;

@@ -42,6 +42,7 @@ constexpr int backward_packs(int gran, int vec) { return vec == 8 ? gran == 1 ? 
 constexpr int SUM_PACKS = 4;       // of a turn of the forward sums, which holds two turns
 constexpr int GRAD_PACKS = 2;      // of a turn of the backward sums
 constexpr int APPLY_PACKS = 4;
+constexpr int SUM_RUN = 128;       // packs of the backward sums that are added up in one go (a chunk of 1 MB; images of 4 GB and more have some thousand)
 
 constexpr int JOINED_PARTS = 4;    // chunks per lane that the workgroups of the results join themselves
 constexpr size_t LDS_PLAIN = 64 * 1024;      // more than that has to be asked for

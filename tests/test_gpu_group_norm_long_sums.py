@@ -1,6 +1,6 @@
-"""Sums of many terms: the parameters' gradients of many images, and of images that one lane goes through for long.  The terms are all of
-one sign and size, so that a running fp32 sum loses the same way at every step: the error of n additions one after the other is up to
-n 2^-25 of the sum, against K of layers_reference.py, which allows for 256 of them."""
+"""Sums of many terms: statistics of long images, gradients of the parameters of many images and of images that one lane goes through for
+long.  The gradient's terms are of one sign and size, so that a running fp32 sum loses the same way at every step: the error of n
+additions one after the other is up to n 2^-25 of the sum, against K of layers_reference.py, which allows for 256 of them."""
 import pytest
 import torch
 
@@ -24,7 +24,11 @@ def _check(x, groups, value):
     size = torch.zeros_like(xh)
     for i in range(0, 1 if each else I, 4096):
         k = min(4096, I - i) if not each else 1
-        v = x[0, i:i + k].double().view(k, S, groups, -1) - mean[0, i:i + k].double()[:, None, :, None]
+        v = x[0, i:i + k].double().view(k, S, groups, -1)
+        var, m = torch.var_mean(v, (1, 3), correction=0)
+        assert ((mean[0, i:i + k].double() - m).abs() <= R.K * v.abs().amax((1, 3))).all()
+        assert ((rstd[0, i:i + k].double() * (var + 1e-5).sqrt() - 1).abs() <= R.K).all()
+        v = v - mean[0, i:i + k].double()[:, None, :, None]
         v = (v * rstd[0, i:i + k].double()[:, None, :, None]).view(-1, C)
         xh += v.sum(0)
         size += v.abs().sum(0)
@@ -49,3 +53,9 @@ def test_many_images(shape, dtype):
 @pytest.mark.parametrize("images,positions", [(342, 4096), (350, 10007)])
 def test_long_images_of_groups_that_no_tile_takes(images, positions, dtype):
     _check(_x((1, 1, positions, 513), dtype).expand(1, images, positions, 513), 1, 0.1)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=("f32", "bf16"))
+@pytest.mark.parametrize("images,positions,channels,groups", [(512, 65536, 64, 8), (1100, 40000, 33, 3)])
+def test_long_images_on_tiles(images, positions, channels, groups, dtype):
+    _check(_x((1, 1, positions, channels), dtype).expand(1, images, positions, channels), groups, 0.12850189)
