@@ -386,6 +386,9 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
  * T = floor(65536*drop + 1/2); so p = T/65536 (at most 2^-17 from drop), and 1/(1-p) is that of the p in force, so that
  * the expectation of y is x.  A dropped element gives zero whatever x holds, infinities and NaN among it.
  * site: the place in the model and the step (a number of the caller's, < 2^24), so that one seed serves them all.
+ * That seed should not be a context's index_seed: the minibatch indices are drawn by the same generator (learner j's are
+ * its outputs from number 1 + j*2^40 on), so that the masks of site j and the indices of learner j would come from the
+ * same words.
  * The backward call with the same drop, seed and site applies the same mask to dy (the residual's gradient is dy itself).
  * y may be x or residual, dx may be dy (same strides).
  * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, 2^30 columns or more in rows that lie apart, drop outside

@@ -373,7 +373,8 @@ def _counters_ok(seed, site):
 def kavg_dropout(x, drop, seed, site=0, residual=None, out=None):
     """Dropout of a float32 or bfloat16 tensor in evenly spaced rows (contiguous, or slices of the last dimension), plus a
     residual of the same shape.  The mask is that of (drop, seed, site) and of an element's number in row-major order; it is
-    not stored.  out: x or the residual among others."""
+    not stored.  seed: not the index_seed of a context, whose minibatch indices come from the same generator.  out: x or the
+    residual among others."""
     _torch_module or _torch()
     dtype = _dtype(x, "x")
     _counters_ok(seed, site)

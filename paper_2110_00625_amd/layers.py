@@ -1,7 +1,8 @@
 """Group norm and dropout as differentiable torch functions: kavg_group_norm and kavg_dropout of the library with their backward
 passes.  What autograd keeps of a group norm is its input and two statistics per group, of a dropout nothing: the mask is drawn
-again from (drop, seed, site).  A program that writes its own backward pass calls `kavg` instead, which can also write into given
-tensors (a learner's gradient vector, x itself)."""
+again from (drop, seed, site), where seed is not the index_seed of a context (its minibatch indices come from the same generator).
+A program that writes its own backward pass calls `kavg` instead, which can also write into given tensors (a learner's gradient
+vector, x itself)."""
 import torch
 from torch.autograd.function import once_differentiable
 
