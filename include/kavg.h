@@ -349,7 +349,9 @@ typedef struct {
  *   z = weight_c (x - m) / sqrt(v + eps) + bias_c,   y = activation(z),
  * and where drop > 0, y is then dropped as by kavg_dropout (element numbers of the whole [sets][images][positions]
  * [channels] tensor).  sets: learners, each with its own weight and bias.  Any size may be 0 but channels and groups.
- * Limits: fewer than 2^42 elements, eps > 0, 0 <= drop <= 1, site < 2^24. */
+ * Limits: fewer than 2^42 elements, 2^31 groups (sets * images * groups) and 2^31 channels (sets * channels), a size of 0
+ * counted as one; strides of images, of rows and of parameters at most 2^46 over the size of their dimension (where that is
+ * more than one); 0 < eps < infinity, 0 <= drop <= 1, site < 2^24. */
 typedef struct {
     int dtype, activation;
     int64_t sets, images, positions;
@@ -391,8 +393,9 @@ int kavg_group_norm_backward(const kavg_norm* norm, const kavg_images* dy, const
  * same words.
  * The backward call with the same drop, seed and site applies the same mask to dy (the residual's gradient is dy itself).
  * y may be x or residual, dx may be dy (same strides).
- * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, 2^30 columns or more in rows that lie apart, drop outside
- * [0, 1], site >= 2^24, unknown dtype, null pointers, an output whose rows overlap. */
+ * KAVG_EINVAL: rows < 0, cols < 1, 2^42 elements or more, 2^30 columns or more in rows that lie apart, a stride (of more
+ * than one row) below 0 or above 2^46 / rows, drop outside [0, 1], site >= 2^24, unknown dtype, pointers that are null or
+ * not aligned to an element, an output whose rows overlap. */
 int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
                  int64_t rows, int64_t cols, int dtype, double drop, uint64_t seed, uint64_t site, void* hip_stream);
 int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int64_t rows, int64_t cols,
