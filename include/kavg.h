@@ -338,7 +338,8 @@ int kavg_meta_update_flat(float* w_tilde_dev, float* v_dev, float* replicas_dev,
 #define KAVG_ACT_SILU 2                  /* z / (1 + exp(-z)) */
 
 /* Images of all learners: element (j, i, s, c) at data[j*set_stride + i*image_stride + s*row_stride + c], in elements.
- * Strides of inputs may be anything from 0 on; rows, images and sets of an output may not overlap. */
+ * Strides of inputs may be anything from 0 on; of an output, the dimensions may lie in any order, but each has to step
+ * over all that the denser ones span. */
 typedef struct {
     void* data;                          /* dev */
     int64_t set_stride, image_stride, row_stride;

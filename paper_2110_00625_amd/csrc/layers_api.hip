@@ -1,5 +1,6 @@
 // C entries of the layers: argument checks, then a launcher.  No state, no allocation, nothing that throws.
 #include "layers.h"
+#include <algorithm>
 #include <cmath>
 
 namespace {
@@ -36,12 +37,18 @@ bool images_ok(const kavg_norm* n, const kavg_images* x, bool written) {
     if (!x) return false;
     if (empty(n)) return true;
     if (!x->data || ((uintptr_t)x->data & (n->dtype == KAVG_BF16 ? 1 : 3))) return false;
-    int64_t run = n->channels;                              // elements from an image's, a set's first to its last
-    const int64_t sizes[3] = {n->positions, n->images, n->sets}, strides[3] = {x->row_stride, x->image_stride, x->set_stride};
-    for (int i = 0; i < 3; ++i) {
-        if (sizes[i] < 2) continue;
-        if (strides[i] < (written ? run : 0) || strides[i] > ((int64_t)1 << 46) / sizes[i]) return false;
-        run += (sizes[i] - 1) * strides[i];
+    struct { int64_t stride, size; } d[3] = {{x->row_stride, n->positions}, {x->image_stride, n->images}, {x->set_stride, n->sets}};
+    for (auto& i : d) {
+        if (i.size < 2) i = {0, 1};                         // (its stride says nothing)
+        if (i.stride < 0 || i.stride > ((int64_t)1 << 46) / i.size) return false;
+    }
+    if (!written) return true;
+    // from the densest dimension on, each has to step over what the ones before it span (a dimension of one is no step)
+    std::sort(d, d + 3, [](const auto& a, const auto& b) { return a.stride < b.stride; });
+    int64_t run = n->channels;
+    for (const auto& i : d) {
+        if (i.size > 1 && i.stride < run) return false;
+        run += (i.size - 1) * i.stride;
     }
     return true;
 }
