@@ -262,7 +262,7 @@ def _norm(x, groups, eps, activation, drop, seed, site):
         if groups < 1 or shape[-1] % groups:             # (before the statistics are allocated)
             _bad("%d groups of %d channels" % (groups, shape[-1]))
         return _NORM.pack(code, activation, shape[0] if len(shape) == 4 else 1, shape[-3], shape[-2], shape[-1], groups, eps, 0, drop, seed, site)
-    except (struct.error, TypeError) as e:
+    except (struct.error, TypeError, OverflowError) as e:
         _bad(str(e))
 
 
@@ -366,8 +366,12 @@ def _rows(x, name):
 
 
 def _counters_ok(seed, site):
-    if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 24:           # (ctypes would wrap them)
-        _bad("seed %d, site %d" % (seed, site))
+    try:
+        if 0 <= seed < 1 << 64 and 0 <= site < 1 << 24:              # (ctypes would wrap them)
+            return
+    except TypeError:
+        pass
+    _bad("seed %r, site %r" % (seed, site))
 
 
 def kavg_dropout(x, drop, seed, site=0, residual=None, out=None):
