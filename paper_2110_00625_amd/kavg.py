@@ -285,6 +285,8 @@ def _workspace(norm, backward, x, like):
 
 
 def _gradient(given, of):
+    if given is False:
+        return None
     if given is not None or of is None:
         return given
     return _torch_module.empty_like(of) if of.is_contiguous() else of.new_empty(of.shape)
@@ -321,7 +323,7 @@ def kavg_group_norm_backward(dy, x, mean, rstd, weight, bias, groups, activation
                              out=None, dweight=None, dbias=None):
     """Gradients of kavg_group_norm (same options; mean, rstd as it returned them): dx (out, if given: dy itself among
     others), dweight, dbias (float32, [sets, channels] or [channels]; written into the tensors given, which may lie in a
-    learner's gradient vector; None where weight, bias are None)."""
+    learner's gradient vector; False: not wanted; None where that is said or weight, bias are None)."""
     torch = _torch_module or _torch()
     norm = _norm(x, groups, 1.0, activation, drop, seed, site)       # (eps went into rstd)
     _like(dy, x, "dy")

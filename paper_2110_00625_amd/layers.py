@@ -25,8 +25,10 @@ class _GroupNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         # (a gradient can have any strides, that of a sum for example zeros)
-        dx, dweight, dbias = kavg.kavg_group_norm_backward(dy.contiguous(), *ctx.saved_tensors, ctx.groups, **ctx.options)
-        return dx, dweight, dbias, None, None, None
+        wanted = ctx.needs_input_grad
+        dx, dweight, dbias = kavg.kavg_group_norm_backward(dy.contiguous(), *ctx.saved_tensors, ctx.groups, dweight=None if wanted[1] else False,
+                                                           dbias=None if wanted[2] else False, **ctx.options)
+        return dx if wanted[0] else None, dweight, dbias, None, None, None
 
 
 class _Dropout(torch.autograd.Function):
