@@ -351,8 +351,8 @@ typedef struct {
  * and where drop > 0, y is then dropped as by kavg_dropout (element numbers of the whole [sets][images][positions]
  * [channels] tensor).  sets: learners, each with its own weight and bias.  Any size may be 0 but channels and groups.
  * Limits: fewer than 2^42 elements, 2^31 groups (sets * images * groups) and 2^31 channels (sets * channels), a size of 0
- * counted as one; strides of images, of rows and of parameters at most 2^46 over the size of their dimension (where that is
- * more than one); 0 < eps < infinity, 0 <= drop <= 1, site < 2^24. */
+ * counted as one, and at most 2^31 - 2^16 channels of an image; strides of images, of rows and of parameters at most
+ * 2^46 over the size of their dimension (where that is more than one); 0 < eps < infinity, 0 <= drop <= 1, site < 2^24. */
 typedef struct {
     int dtype, activation;
     int64_t sets, images, positions;

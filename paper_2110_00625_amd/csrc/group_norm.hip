@@ -127,7 +127,7 @@ template <class F> __device__ __forceinline__ void for_parts(const WideCall& f, 
     const float* parts = f.parts + image * f.chunks * 2 * channels + first;
     for (int j = 0; j < f.chunks; ++j, parts += 2 * (int64_t)channels) {
 #pragma unroll 8
-        for (int d = threadIdx.x; d < D; d += JOIN) of(j, d, parts[d], parts[channels + d]);
+        for (int d = threadIdx.x; d < D; d += JOIN) of(j, d, parts[d], (parts + channels)[d]);
     }
 }
 

@@ -8,6 +8,7 @@ namespace {
 using namespace kavg;
 
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 42;
+constexpr int MOST_CHANNELS = INT32_MAX - 65535;            // (counted in 32 bits by lanes, the last of which lie behind them)
 
 // a * b * c * d below the limit, each factor from 0 on (a size of 0 leaves the others alone)
 bool product_ok(int64_t a, int64_t b, int64_t c, int64_t d, int64_t below) {
@@ -25,7 +26,7 @@ bool drop_ok(double drop, uint64_t site) { return drop >= 0. && drop <= 1. && si
 bool norm_ok(const kavg_norm* n) {
     if (!n || n->reserved || (n->dtype != KAVG_FP32 && n->dtype != KAVG_BF16)) return false;
     if (n->activation < KAVG_ACT_NONE || n->activation > KAVG_ACT_SILU) return false;
-    if (n->channels < 1 || n->groups < 1 || n->channels % n->groups) return false;
+    if (n->channels < 1 || n->channels > MOST_CHANNELS || n->groups < 1 || n->channels % n->groups) return false;
     if (!product_ok(n->sets, n->images, n->positions, n->channels, MOST_ELEMENTS)) return false;
     if (!product_ok(n->sets, n->images, n->groups, 1, (int64_t)1 << 31) || !product_ok(n->sets, n->channels, 1, 1, (int64_t)1 << 31)) return false;
     return n->eps > 0.f && std::isfinite(n->eps) && drop_ok(n->drop, n->site);

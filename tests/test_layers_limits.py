@@ -50,3 +50,14 @@ def test_strides_of_dropout(lib):  # noqa: F811
         return lib.kavg_dropout(AT, xs, AT, rs, AT, ys, rows, cols, 0, 0.5, 1, 0, None)
     for kw in (dict(xs=(1 << 44) + 1), dict(rs=(1 << 44) + 1), dict(ys=(1 << 44) + 1), dict(cols=1 << 30, xs=0, rs=0, ys=1 << 30)):
         assert drop(**kw) == kavg.KAVG_EINVAL, kw
+
+
+def test_channels(lib):  # noqa: F811
+    """Channels are counted in 32 bits by workgroups that go a little past the last one."""
+    for sets, groups in ((1, 1), (1, 1 << 10), (0, 1)):
+        most = (1 << 31) - (1 << 16)
+        assert _accepted(lib, sets=sets, images=1, positions=1, channels=most, groups=groups)
+        for over in (most + (1 << 10), (1 << 31) - (1 << 10)):
+            kw = dict(sets=sets, images=1, positions=1, channels=over, groups=groups)
+            assert not _accepted(lib, **kw)
+            assert forward(lib, norm(**kw)) == kavg.KAVG_EINVAL and backward(lib, norm(**kw)) == kavg.KAVG_EINVAL
