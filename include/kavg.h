@@ -328,8 +328,8 @@ int kavg_meta_update_flat(float* w_tilde_dev, float* v_dev, float* replicas_dev,
  * Stateless calls on caller arrays for learners whose local steps the caller writes (F is any model, the meta step is
  * kavg_meta_update_flat's).  The activations of all learners are one tensor, channels last, and every learner has its
  * own parameters, which may lie inside its replica.  dtype is that of the activations (KAVG_FP32 or KAVG_BF16);
- * parameters, statistics, every sum and their gradients are fp32, and a result is rounded once (bf16: nearest, ties to
- * even).  All calls are asynchronous on hip_stream (NULL = the default stream), work on the current device, hold nothing
+ * parameters, statistics and gradients of parameters are fp32, every sum fp32 or wider, and a result is rounded once
+ * (bf16: nearest, ties to even).  All calls are asynchronous on hip_stream (NULL = the default stream), work on the current device, hold nothing
  * between calls, and may be recorded into a graph.
  * Errors: KAVG_EINVAL for what a call says it wants and does not get (checked before any device call), KAVG_ENOMEM
  * (workspace too small), KAVG_EDEVICE (a launch failed). */

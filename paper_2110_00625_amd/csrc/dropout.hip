@@ -2,8 +2,8 @@
 // (counter_stream.h), so the backward pass draws it again and nothing is stored.  An element is read and written once, and a draw of
 // 64 bits, some thirty instructions, serves four of them: bound by memory.  A pack per lane (four per lane, their loads in flight together, were
 // the same within 4 % either way).  67M elements in bf16 40 us, 6.6 TB/s, part of it in the 256 MB cache behind the L2, 47 us out of memory; 2048 rows
-// of 4096 in bf16 with a residual 9.0 us, 5.6 TB/s; 4999 rows of 1001 in fp32 7.6 us, 5.3 TB/s; 192 rows of 256 2.4 us of a call
-// of 7.5, which is the host's time.
+// of 4096 in bf16 with a residual 9.0 us, 5.6 TB/s; 4999 rows of 1001 in fp32 7.9 us, 5.1 TB/s; 192 rows of 256 2.4 us of a call
+// of 7.8, which is the host's time.
 #include "layers.h"
 #include <algorithm>
 #include <cmath>

@@ -11,8 +11,8 @@
 // some hundred, and counts of tiles past 2^30, runs on the kernels here: a lane per channel goes along its chunk of the positions, sums per channel
 // and chunk go through memory to the groups, and the image is read again for the results.  They are right for any size, load an element at a
 // time (128 bytes of bf16 a wavefront, eight rows of them in flight), and are bound by that and by their launches' latencies: 8 images of 1000
-// positions, 1031 channels in one group, in bf16, backward 50 us (a workgroup per group, for whom there are eight: 2475); 64 vectors of 16384
-// forward 24, backward 34 (17 and 26).
+// positions, 1031 channels in one group, in bf16, backward 53 us (a workgroup per group, for whom there are eight: 2475); 64 vectors of 16384
+// forward 23, backward 33 (17 and 26).
 #include "norm_backward.h"
 #include "norm_forward.h"
 #include "wave_sum.h"
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(T) norm_wide_dx_kernel(WideCall f) {
 }
 
 // channels, chunks, images of a launch: some thousand workgroups, and images one after the other where there are more (1024 vectors of 16384
-// channels, backward: 188 us, a workgroup for every one of them 281)
+// channels, backward: 191 us, a workgroup for every one of them 281)
 dim3 wide_grid(const NormCall& c, int chunks) {
     const int64_t blocks = (c.channels + T - 1) / T, most = std::max<int64_t>(1, MOST_GROUPS / (blocks * chunks));
     return dim3((unsigned)blocks, (unsigned)chunks, (unsigned)std::min({c.sets * c.images, most, (int64_t)65535}));

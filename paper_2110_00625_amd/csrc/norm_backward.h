@@ -204,9 +204,9 @@ __device__ __forceinline__ void write_dx(const NormCall& c, const Tile& t, const
 
 // Images that a workgroup holds: x and dy read once, x kept as it came and dz in fp32 from the sums to dx (a rounded dz would be another
 // gradient, a second mask and sigmoid half the instructions again).  So four packs of bf16 per lane, 112 registers, two workgroups of 512 lanes per
-// compute unit.  1024 images of 32x32x64 in bf16 with SiLU and dropout: 112 us, 3.6 TB/s of the 403 MB; 37 vector instructions per element keep
-// the vector units busy for two thirds of it, what is left is the two workgroups' waiting for loads and for each other's lanes.  In fp32
-// with SiLU, 256 images of 28x28x40: 21.6 us, 4.5 TB/s (one workgroup per compute unit, and nothing to fill its waits).
+// compute unit.  1024 images of 32x32x64 in bf16 with SiLU and dropout: 112 us, 3.6 TB/s of the 403 MB; 39 vector instructions per element keep
+// the vector units busy for seven tenths of it, what is left is the two workgroups' waiting for loads and for each other's lanes.  In fp32
+// with SiLU, 256 images of 28x28x40: 21.9 us, 4.4 TB/s (one workgroup per compute unit, and nothing to fill its waits).
 template <class E, int V, int NV, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
     constexpr int A = V / GRAN;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(BackwardCall f) {
 }
 
 // Sums of a chunk per channel, in turns of GRAD_PACKS packs per lane, the next turn's on their way.  63 MB (x and dy of three images of
-// 127x129x320 in bf16, SiLU) in 18.2 us, 3.5 TB/s.
+// 127x129x320 in bf16, SiLU) in 18.0 us, 3.5 TB/s.
 template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_sums_kernel(BackwardCall f) {
     constexpr int NV = GRAD_PACKS;
@@ -346,7 +346,7 @@ int64_t r = share;
 }
 
 // dx of an image read again, by the workgroups that read the same tiles for the sums, on the same XCD and the last first: those are what
-// its cache still holds.  Behind the tiles, the parameters.  Those 63 MB again and 31 MB written in 17.6 us, 5.4 TB/s.
+// its cache still holds.  Behind the tiles, the parameters.  Those 63 MB again and 31 MB written in 17.2 us, 5.5 TB/s.
 template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
     constexpr int A = V / GRAN, NV = GRAD_PACKS;
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(512) norm_dx_kernel(BackwardCall f) {
     }
 }
 
-// A and B of a group from the sums of its image's chunks: a workgroup per group, a launch and its latency (4 us).
+// A and B of a group from the sums of its image's chunks: a workgroup per group, a launch and its latency (4 to 5 us).
 template <int T>
 __global__ void __launch_bounds__(T) norm_group_kernel(BackwardCall f, float* group_sums) {
     __shared__ float lds[8];                         // (T = 256: four wavefronts)
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(T) norm_group_kernel(BackwardCall f, float* gr
     }
 }
 
-// The parameters' gradients behind norm_backward_kernel, whose sums per image it adds: a launch of its own, 4 us, for an order of the sums that
+// The parameters' gradients behind norm_backward_kernel, whose sums per image it adds: a launch of its own, 4 to 5 us, for an order of the sums that
 // does not depend on which workgroup ends first (atomics would).
 template <int T>
 __global__ void __launch_bounds__(T) norm_param_kernel(BackwardCall f) {

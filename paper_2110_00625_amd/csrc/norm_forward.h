@@ -190,7 +190,7 @@ __device__ __forceinline__ void write_result(const NormCall& c, const Tile& t, c
 // Images that a workgroup holds: read once, statistics, result, written once.  Up to sixteen packs per lane, so that two workgroups of 512 lanes
 // with 64 KB of x each share a compute unit and one loads while the other computes or writes.  Bound by memory where there is much: 1024 images of
 // 32x32x128 in bf16 with ReLU and dropout 111 us, 4.8 TB/s (a copy of that size 5.1), 15 vector instructions per element, half of them the
-// draws'.  A thousand vectors of 1024 in fp32: 7.4 us, a launch and its latencies.
+// draws'.  A thousand vectors of 1024 in fp32: 7.0 us, a launch and its latencies.
 template <class E, int V, int NV, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
     constexpr int A = V / GRAN;
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(1024) norm_forward_kernel(ForwardCall f) {
 }
 
 // Moments of a chunk, in turns of SUM_PACKS packs per lane, the next turn's on their way; a lane joins its turns as means of parts.  Bound by
-// latency: of 33 MB (two images of 256x256x128 in bf16) 11.5 us, 2.9 TB/s, a load, two turns and the join of the lanes.
+// latency: of 33 MB (two images of 256x256x128 in bf16) 11.0 us, 3.0 TB/s, a load, two turns and the join of the lanes.
 template <class E, int V, bool FLAT, int GRAN>
 __global__ void __launch_bounds__(512) norm_moments_kernel(ForwardCall f) {
     constexpr int A = V / GRAN, NV = SUM_PACKS;
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(T) norm_join_kernel(ForwardCall f, int64_t gro
 }
 
 // Results of an image read again, by the workgroups that read the same tiles for the sums, on the same XCD and the last first: those are
-// what its cache still holds.  Those 33 MB read and written in 14.2 us, 4.7 TB/s.  (Images kept on chip from the sums to the results would want
+// what its cache still holds.  Those 33 MB read and written in 14.8 us, 4.5 TB/s.  (Images kept on chip from the sums to the results would want
 // workgroups that wait for each other, which a caller's other work on the device could keep from running.)
 template <class E, int V, bool FLAT, int GRAN, bool SILU, bool DROP>
 __global__ void __launch_bounds__(512) norm_apply_kernel(ForwardCall f) {
