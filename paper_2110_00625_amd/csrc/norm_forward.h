@@ -37,9 +37,17 @@ template <class E, int V, int NV, int GRAN>
 __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&xv)[NV], float (&mean)[V / GRAN], float (&sq)[V / GRAN]) {
     constexpr int A = V / GRAN;
     float sum[A];
-    bool lost[A];
 #pragma unroll
-    for (int a = 0; a < A; ++a) { sum[a] = sq[a] = 0.f; lost[a] = true; }
+    for (int a = 0; a < A; ++a) sum[a] = sq[a] = 0.f;
+    const auto add_distances = [&](float (&to)[A]) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            auto v = xv[k];
+            keep_packed(v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; to[i / GRAN] += d * d; }
+        }
+    };
     if constexpr (sizeof(E) == 2 && GRAN > 1) {
         // bf16: sums of values and of squares by dot products (half an instruction per element each; a mean and distances from it are four).
         // n v = sum x^2 - n m^2 cancels where the mean is large against the spread: a sum that loses more than two bits is taken of the
@@ -49,7 +57,7 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
 #pragma unroll
             for (int a = 0; a < A; ++a) { sum[a] = pack_sum<GRAN>(xv[k], a * GRAN, sum[a]); sq[a] = pack_squares<GRAN>(xv[k], a * GRAN, sq[a]); }
         }
-        bool any = false;
+        bool lost[A], any = false;
 #pragma unroll
         for (int a = 0; a < A; ++a) {
             mean[a] = sum[a] * (1.f / (NV * GRAN));
@@ -59,6 +67,12 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
             any |= lost[a];
         }
         if (!__any(any)) return;
+        float far[A];
+#pragma unroll
+        for (int a = 0; a < A; ++a) far[a] = 0.f;
+        add_distances(far);
+#pragma unroll
+        for (int a = 0; a < A; ++a) sq[a] = lost[a] ? far[a] : sq[a];
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -67,19 +81,8 @@ __device__ __forceinline__ void whole_moments(const typename Pack<E, V>::type (&
         }
 #pragma unroll
         for (int a = 0; a < A; ++a) mean[a] = sum[a] * (1.f / (NV * GRAN));
+        add_distances(sq);
     }
-    float far[A];
-#pragma unroll
-    for (int a = 0; a < A; ++a) far[a] = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        auto v = xv[k];
-        keep_packed(v);
-#pragma unroll
-        for (int i = 0; i < V; ++i) { const float d = to_float(v[i]) - mean[i / GRAN]; far[i / GRAN] += d * d; }
-    }
-#pragma unroll
-    for (int a = 0; a < A; ++a) sq[a] = lost[a] ? far[a] : sq[a];
 }
 
 // The same of packs from the `first`-th on of which not all are the image's, and how many are (flat: of each element): `whole` of them, and one
