@@ -402,6 +402,104 @@ int kavg_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
 int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int64_t rows, int64_t cols,
                           int dtype, double drop, uint64_t seed, uint64_t site, void* hip_stream);
 
+/* ---- Products of a learner's layer ------------------------------------------------------------------------------------
+ * Matrix products with bias, activation and residual in their epilogue, for all learners at once, and their gradients; caller
+ * arrays, conventions and errors as for the layers above.  dtype is that of x, the weights, y and their like (KAVG_FP32 or
+ * KAVG_BF16; a learner's bf16 weights are the copy that kavg_adamw or the shadow that kavg_meta_update_flat writes); biases and
+ * gradients of weights and biases are fp32.  Sums are fp32, a result is rounded once.
+ *   z = x W^T + b,   y = residual + activation(z)                                             (kavg_linear)
+ *   from dz, the gradient of z:  dx = (dz W) * slope(pre),  dW = dz^T x,  db = sum of dz's rows   (kavg_linear_backward)
+ * In a net of several layers x is the activation of the layer below: `activation` of the backward call is that layer's and `pre` its
+ * z, so that dx is the gradient of that z, which that layer's backward call wants (KAVG_ACT_NONE: dx is the gradient of x; pre NULL).  ReLU's
+ * slope at 0 is 0; for ReLU, pre may also be x itself.
+ * Order of a call's sums, and so its bits, depend on the sizes, strides and alignment alone.
+ * Limits: sizes at most 2^31 - 2^16, fewer than 2^42 elements in any matrix, strides at most 2^46 over the size of their dimension
+ * (the stride of a dimension of one says nothing); inputs, outputs >= 1; sets or rows may be 0 (dW, db are zeros then). */
+typedef struct {
+    int dtype, activation;
+    int64_t sets, rows, inputs, outputs;
+} kavg_product;
+
+/* [sets][rows][columns]: element (j, r, c) at data[j*set_stride + r*row_stride + c].  Strides of inputs may be anything from 0 on; of
+ * an output, no element twice. */
+typedef struct {
+    void* data;                          /* dev */
+    int64_t set_stride, row_stride;
+} kavg_rows;
+
+/* Weights or their gradient: element (j, o, i) at data[j*set_stride + o*output_stride + i*input_stride]; one of the last two is 1. */
+typedef struct {
+    void* data;                          /* dev */
+    int64_t set_stride, output_stride, input_stride;
+} kavg_weights;
+
+/* Bytes of device workspace a call wants (may be 0); 16-byte aligned.  A call that is given fewer than it needs says so
+ * (KAVG_ENOMEM) before it launches anything. */
+int kavg_linear_workspace(const kavg_product* product, int backward, size_t* bytes);
+
+/* bias: learner j's [outputs] at bias + j*bias_stride; NULL = zeros.  residual, pre: NULL = none, not wanted (pre receives z).  y may be
+ * the residual (same strides); no other array that is written may overlap another of the call. */
+int kavg_linear(const kavg_product* product, const kavg_rows* x, const kavg_weights* weight, const float* bias, int64_t bias_stride,
+                const kavg_rows* residual, const kavg_rows* y, const kavg_rows* pre, void* workspace, size_t workspace_bytes,
+                void* hip_stream);
+
+/* dx, dweight, dbias: NULL = not wanted (weight and pre are not needed without dx, x not without dweight); written, not added to.
+ * dweight: fp32, in either order.  dx may be pre (same strides) or x; no other array that is written may overlap another of the call. */
+int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const kavg_rows* x, const kavg_weights* weight,
+                         const kavg_rows* pre, const kavg_rows* dx, const kavg_weights* dweight, float* dbias, int64_t dbias_stride,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Step of a learner: AdamW ------------------------------------------------------------------------------------
+ * One step over many tensors at once, in place, for learners whose local steps the caller writes (parameters that lie in
+ * rows of the replicas: a tensor's rows are the learners).  With g = grad_scale * gradient, t = step,
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ * in fp32, every operation of the first line rounded by itself; copy, where there is one, gets p as bf16 (nearest, ties
+ * away from zero, as kavg_meta_update_flat's shadow).
+ *
+ * bits 32: m and v are fp32.  bits 8: m and the root r = sqrt(v) are e4m3 (no infinities, 448 the largest), one byte per
+ * value, times a scale, a power of two in fp32, for every 256 values of a row: the scale is 2^(k-8) where
+ * 2^(k-1) c <= the block's largest finite magnitude < 2^k c, c = 1.7320508 (0x3FDDB3D7), and 2^-126 at least.  m is rounded to nearest
+ * (ties to even).  r is rounded down or up at random, up with its distance from the lower neighbour in units of theirs
+ * (a root rounded to nearest could not decay: a step changes it by less than half a unit), never to zero unless it is
+ * zero.  The draw for element number e = row * cols + col of tensor i of the call: the 16 bits at 16*(e mod 4) of SplitMix64
+ * output number 1 + i*2^40 + floor(e/4), seeded with seed + step (see kavg_dropout, also for the choice of a seed), plus a
+ * half, over 65536.  The step itself uses m and v before they are rounded.  A value that is not finite is kept as NaN and
+ * leaves the others of its block alone.
+ *
+ * Rows of a tensor: rows x cols elements; parameters, gradients and copies with row strides (in elements), states without
+ * gaps ([rows][cols], scales [rows][ceil(cols/256)]).  No two pieces of memory that the call writes may overlap, or overlap one it reads. */
+typedef struct {
+    float* param;                        /* dev, as are all of them */
+    const void* grad;                    /* of options.grad_dtype                    */
+    void* m;
+    void* v;
+    float* m_scale;                      /* bits 8, else NULL                        */
+    float* v_scale;
+    uint16_t* copy;                      /* or NULL                                  */
+    int64_t rows, cols, param_stride, grad_stride, copy_stride;
+    float weight_decay;
+    int reserved;                        /* 0 */
+} kavg_adamw_tensor;
+
+/* step_dev, lr_dev, grad_scale_dev: NULL, or a number in device memory that takes the place of the host's when the kernels
+ * run (so that a recorded graph can be replayed with others; a step below 1 counts as 1). */
+typedef struct {
+    int bits, grad_dtype;
+    double lr, beta1, beta2, eps, grad_scale;
+    uint64_t step, seed;
+    const int64_t* step_dev;
+    const float* lr_dev;
+    const float* grad_scale_dev;
+} kavg_adamw_options;
+
+/* The step on `count` tensors (host arrays; tensors of no elements are left out).  Asynchronous on hip_stream, may be recorded
+ * into a graph, holds nothing between calls.
+ * KAVG_EINVAL: bits other than 8 and 32, unknown dtype, lr, eps or weight_decay below 0, a beta outside [0, 1), numbers that are
+ * not finite, step 0 (without step_dev), count < 0 or (bits 8) of 2^24 or more, rows or cols < 0, 2^40 elements or more of a tensor,
+ * 2^31 rows or more, a stride (of more than one row) below cols or (gradients) below 0, or above 2^46 / rows, pointers that are null or not aligned to an element. */
+int kavg_adamw(const kavg_adamw_options* options, const kavg_adamw_tensor* tensors, int count, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,118 @@
+// Launch interface of the products (kavg_linear, kavg_linear_backward) and what their kernels share.  The boundary (learner_api.hip)
+// has checked every argument.
+//
+// All three products of a layer are  O[r][c] = sum_k R(r,k) C(c,k)  per learner:
+//   forward          r = row,     c = output, k = input     R = x,           C = W
+//   data gradient    r = row,     c = input,  k = output    R = dz,          C = W turned
+//   weight gradient  r = output,  c = input,  k = row       R = dz turned,   C = x turned
+// (of weights that lie as [inputs][outputs] the other way round: C = W turned, C = W, and R = x turned, C = dz turned).
+#pragma once
+#include "kavg_internal.h"
+#include "layers.h"
+
+namespace kavg {
+
+// Element (x, k) of a learner's matrix: base[set * set_stride + x * stride + k], or of a turned one base[.. + k * stride + x].
+struct Matrix { const void* base; int64_t set_stride, stride; };
+
+// What becomes of a product's values v(r, c).  Pointers that are null are left out, in this order:
+//   v += bias[c];  kept[r][c] = v;  v = act(v);  v *= slope(before[r][c]);  v += residual[r][c];  out[r][c] = v
+struct Finish {
+    const float* bias; int64_t bias_set;
+    void* kept; int64_t kept_set, kept_row;
+    bool silu; float floor;                      // act: see layers.h
+    const void* before; int64_t before_set, before_row;
+    bool slope_silu;
+    const void* residual; int64_t residual_set, residual_row;
+    void* out; int64_t out_set, out_row;         // of the operands' type, of a weight gradient fp32
+};
+
+struct ProductCall {
+    int dtype;
+    int64_t sets;
+    int nR, nC, nK;
+    Matrix R, C;
+    bool r_turned, c_turned;                     // (r_turned: a weight gradient, c_turned too)
+    Finish finish;
+    // sums over k of R (side 1) or C (side 2), of a weight gradient: those of dz are the bias's gradient
+    int side; float* sums; int64_t sums_set;
+};
+
+// How a product is cut: the tile (linear_tile.h), and between how many workgroups a tile's contraction is split.  Their partial results, [split]
+// [set][r][c] in fp32 with rows of `pitch`, and sums lie in the workspace; the launch that joins them finishes the values.
+struct Plan {
+    int tile, splits, pitch;
+    size_t bytes;                                // of workspace
+};
+Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient);
+// hipErrorOutOfMemory, hipErrorInvalidValue: a workspace too small, misaligned or not there, before anything is launched
+hipError_t launch_product(const ProductCall& c, void* workspace, size_t bytes, hipStream_t st);
+
+#if defined(__HIPCC__)
+template <class E, int V> __device__ __forceinline__ void load_some(const E* p, int n, float (&v)[V]) {
+    if (n >= V) {
+#pragma unroll
+        for (int i = 0; i < V; i += 16 / sizeof(E) < V ? 16 / sizeof(E) : V) {
+            constexpr int W = 16 / sizeof(E) < V ? 16 / sizeof(E) : V;
+            const auto q = pack_load<E, W>(p + i);
+#pragma unroll
+            for (int k = 0; k < W; ++k) v[i + k] = to_float(q[k]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = k < n ? to_float(p[k]) : 0.f;
+    }
+}
+template <class E, int V> __device__ __forceinline__ void store_some(E* p, int n, const float (&v)[V]) {
+    if (n >= V) {
+        constexpr int W = 16 / sizeof(E) < V ? 16 / sizeof(E) : V;
+#pragma unroll
+        for (int i = 0; i < V; i += W) {
+            typename Pack<E, W>::type q;
+#pragma unroll
+            for (int k = 0; k < W; ++k) q[k] = from_float<E>(v[i + k]);
+            pack_store<E, W>(p + i, q);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) if (k < n) p[k] = from_float<E>(v[k]);
+    }
+}
+
+// n <= V values of row r from column c on.  E: type of the operands, O: of the result.
+template <class E, class O, int V>
+__device__ __forceinline__ void finish_values(const Finish& f, int64_t set, int64_t r, int c, int n, float (&v)[V]) {
+    float t[V];
+    if (f.bias) {
+        load_some<float, V>(f.bias + set * f.bias_set + c, n, t);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += t[k];
+    }
+    if (f.kept) store_some<E, V>((E*)f.kept + set * f.kept_set + r * f.kept_row + c, n, v);
+    if (f.silu) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] *= sigmoid_of(v[k] * SILU_SCALE);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = __builtin_elementwise_maximum(v[k], f.floor);
+    }
+    if (f.before) {
+        load_some<E, V>((const E*)f.before + set * f.before_set + r * f.before_row + c, n, t);
+        if (f.slope_silu) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = through_slope<true>(v[k], t[k] * SILU_SCALE, 0.f);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = through_slope<false>(v[k], t[k], 0.f);
+        }
+    }
+    if (f.residual) {
+        load_some<E, V>((const E*)f.residual + set * f.residual_set + r * f.residual_row + c, n, t);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += t[k];
+    }
+    store_some<O, V>((O*)f.out + set * f.out_set + r * f.out_row + c, n, v);
+}
+#endif
+
+}  // namespace kavg

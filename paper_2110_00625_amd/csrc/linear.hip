@@ -1,0 +1,168 @@
+// Products of learners' layers: which tile a call takes, whether its contraction is split, and the launch that joins the parts.
+#include "linear_tile.h"
+#include <algorithm>
+
+namespace kavg {
+
+hipError_t start_bf16_plain(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+hipError_t start_bf16_turned(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+hipError_t start_bf16_gradient(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+hipError_t start_f32_plain(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+hipError_t start_f32_turned(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+hipError_t start_f32_gradient(int tile, bool direct, const ProductArgs& a, hipStream_t st);
+
+namespace {
+
+constexpr int CUS = 256;
+constexpr int T = 256;
+constexpr int64_t MOST_TILES = 1 << 22;          // of a launch (fewer than 2^32 lanes)
+
+struct Size { int r, c; };
+constexpr Size tile_size(int tile) {
+#define TILE(NUMBER, TR, TC, WR, WC, WK) if (tile == NUMBER) return {TR, TC};
+    KAVG_TILES(TILE)
+#undef TILE
+    return {0, 0};
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int64_t tiles_of(int tile, int64_t sets, int nR, int nC) {
+    const Size s = tile_size(tile);
+    return sets * up(nR, s.r) * std::max<int64_t>(1, up(nC, s.c));
+}
+
+// A lane adds up the parts of eight columns of a row, in order, and finishes them; the sums follow after the last row.
+template <class E, bool GRADIENT>
+__global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, uint32_t per_row, Divisor by_row) {
+    const uint64_t first = (uint64_t)blockIdx.x * T;
+    if (first < packs) {
+        // (a row has fewer than 2^28 packs, so that what is divided stays below 2^30)
+        const uint64_t row0 = first / per_row;
+        const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, down = divide(at, by_row);
+        if (first + threadIdx.x >= packs) return;
+        const uint64_t row = row0 + down;
+        const int c = (int)(at - down * per_row) * 8;
+        const float* p = a.partial + row * a.pitch + c;
+        float v[8] = {};
+        for (int s = 0; s < a.splits; ++s) {
+            float t[8];
+            load_some<float, 8>(p + s * a.partial_split, 8, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += t[k];
+        }
+        const int64_t set = (int64_t)(row / (uint64_t)a.nR), r = (int64_t)(row - (uint64_t)set * a.nR);
+        if constexpr (GRADIENT) store_some<float, 8>((float*)a.finish.out + set * a.finish.out_set + r * a.finish.out_row + c, a.nC - c, v);
+        else finish_values<E, E, 8>(a.finish, set, r, c, a.nC - c, v);
+    }
+}
+
+struct SumsArgs { const float* parts; float* sums; int64_t split, from_set, to_set; int n, splits; int64_t sets; };
+
+__global__ void __launch_bounds__(T) join_sums_kernel(SumsArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * T + threadIdx.x, set = i / a.n, x = i - set * a.n;
+    if (set >= a.sets) return;
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += a.parts[s * a.split + set * a.from_set + x];
+    a.sums[set * a.to_set + x] = v;
+}
+
+bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem) {
+    const int chunk = 16 / elem;
+    return !((uintptr_t)m.base & 15) && extent % chunk == 0 && (sets < 2 || m.set_stride % chunk == 0) && (lines < 2 || m.stride % chunk == 0);
+}
+
+}  // namespace
+
+Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient) {
+    const int bk = dtype == KAVG_BF16 ? Kind<__bf16>::BK : Kind<float>::BK;
+    const int64_t slices = up(nK, bk);
+    Plan p = {};
+    p.pitch = (int)up(nC, 8) * 8;
+    if (nC <= 32) p.tile = TILE_TALL;
+    else if (nR <= 32) p.tile = TILE_WIDE;
+    else p.tile = tiles_of(TILE_LARGE, sets, nR, nC) >= CUS ? TILE_LARGE : tiles_of(TILE_MIDDLE, sets, nR, nC) >= CUS ? TILE_MIDDLE : TILE_SMALL;
+    const int64_t tiles = tiles_of(p.tile, sets, nR, nC);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slices / 8, 2 * CUS / tiles));
+    p.splits = slices ? (int)up(slices, up(slices, p.splits)) : 1;        // (none without a slice)
+    if (p.splits > 1) p.bytes = (size_t)p.splits * sets * ((size_t)nR * p.pitch + (weight_gradient ? std::max(nR, nC) : 0)) * sizeof(float);
+    return p;
+}
+
+hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes, hipStream_t st) {
+    const bool bf16 = call.dtype == KAVG_BF16;
+    const int elem = bf16 ? 2 : 4, bk = bf16 ? Kind<__bf16>::BK : Kind<float>::BK;
+    const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
+    if (plan.splits > 1) {
+        if (bytes < plan.bytes) return hipErrorOutOfMemory;
+        if (!workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;
+    }
+    const bool direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
+                        aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
+    const int tile = plan.tile == TILE_LARGE && !direct ? TILE_MIDDLE : plan.tile;
+    const Size size = tile_size(tile);
+    const int64_t slices = up(call.nK, bk);
+
+    ProductArgs a = {};
+    a.nC = call.nC; a.nK = call.nK;
+    a.tiles_c = (int)std::max<int64_t>(1, up(call.nC, size.c));
+    a.splits = plan.splits;
+    a.per_split = (int)up(slices, plan.splits);
+    a.finish = call.finish;
+    a.side = call.side;
+    a.sums = call.sums; a.sums_set = call.sums_set;
+    // as many learners and rows at once as a launch takes (all of them, but for results of some hundred gigabytes)
+    const int64_t of_row = (int64_t)a.tiles_c * a.splits, rows_at_once = std::min<int64_t>(call.nR, std::max<int64_t>(1, MOST_TILES / of_row) * size.r);
+    const int64_t sets_at_once = rows_at_once < call.nR ? 1 : std::max<int64_t>(1, MOST_TILES / (of_row * up(call.nR, size.r)));
+    if (of_row > MOST_TILES || (plan.splits > 1 && (rows_at_once < call.nR || sets_at_once < call.sets))) return hipErrorInvalidValue;
+    for (int64_t set = 0; set < call.sets; set += sets_at_once)
+        for (int64_t r = 0; r < call.nR; r += rows_at_once) {
+            const int64_t sets = std::min(sets_at_once, call.sets - set);
+            auto moved = [&](const void* p, int64_t elements, int size) { return p ? (void*)((char*)p + elements * size) : nullptr; };
+            a.nR = (int)std::min(rows_at_once, call.nR - r);
+            a.R = call.R; a.C = call.C;
+            a.R.base = moved(call.R.base, set * call.R.set_stride + (call.r_turned ? r : r * call.R.stride), elem);
+            a.C.base = moved(call.C.base, set * call.C.set_stride, elem);
+            Finish& f = a.finish;
+            f.bias = (const float*)moved(call.finish.bias, set * f.bias_set, 4);
+            f.kept = moved(call.finish.kept, set * f.kept_set + r * f.kept_row, elem);
+            f.before = moved(call.finish.before, set * f.before_set + r * f.before_row, elem);
+            f.residual = moved(call.finish.residual, set * f.residual_set + r * f.residual_row, elem);
+            f.out = moved(call.finish.out, set * f.out_set + r * f.out_row, call.r_turned ? 4 : elem);
+            if (call.side) a.sums = call.sums + set * call.sums_set + (call.side == 1 ? r : 0);
+            a.tiles_r = (int)up(a.nR, size.r);
+            a.total = (uint32_t)(sets * a.splits * a.tiles_r * a.tiles_c);
+            a.per_xcd = (uint32_t)up(a.total, 8);
+            SumsArgs sums = {};
+            if (plan.splits > 1) {
+                a.partial = (float*)workspace;
+                a.pitch = plan.pitch;
+                a.partial_split = sets * (int64_t)a.nR * a.pitch;
+                if (call.side) {
+                    sums = {a.partial + plan.splits * a.partial_split, a.sums, 0, call.side == 1 ? a.nR : a.nC, call.sums_set, call.side == 1 ? a.nR : a.nC, plan.splits, sets};
+                    sums.split = sets * sums.n;
+                    a.sums = (float*)sums.parts; a.sums_set = sums.from_set; a.sums_split = sums.split;
+                }
+            }
+            const auto start = call.r_turned ? (bf16 ? start_bf16_gradient : start_f32_gradient)
+                                             : call.c_turned ? (bf16 ? start_bf16_turned : start_f32_turned) : (bf16 ? start_bf16_plain : start_f32_plain);
+            hipError_t e = start(tile, direct, a, st);
+            if (e != hipSuccess) return e;
+            if (plan.splits > 1) {
+                const uint32_t per_row = (uint32_t)plan.pitch / 8;
+                const uint64_t packs = (uint64_t)sets * a.nR * per_row;
+                if (packs) {
+                    const dim3 grid((unsigned)up(packs, T)), lanes(T);
+                    if (call.r_turned) join_kernel<float, true><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
+                    else if (bf16) join_kernel<__bf16, false><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
+                    else join_kernel<float, false><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
+                }
+                if (call.side) join_sums_kernel<<<dim3((unsigned)up(sets * sums.n, T)), dim3(T), 0, st>>>(sums);
+                e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+        }
+    return hipSuccess;
+}
+
+}  // namespace kavg

@@ -1,0 +1,8 @@
+// Tiles of the products of bf16 operands, C turned (linear_tile.h).
+#include "linear_tile.h"
+
+namespace kavg {
+
+hipError_t start_bf16_turned(int tile, bool direct, const ProductArgs& a, hipStream_t st) { return start_kind<__bf16, false, true>(tile, direct, a, st); }
+
+}  // namespace kavg

@@ -1,0 +1,8 @@
+// Tiles of the products of f32 operands, both turned (linear_tile.h).
+#include "linear_tile.h"
+
+namespace kavg {
+
+hipError_t start_f32_gradient(int tile, bool direct, const ProductArgs& a, hipStream_t st) { return start_kind<float, true, true>(tile, direct, a, st); }
+
+}  // namespace kavg

@@ -1,0 +1,371 @@
+// Tiles of the products (linear.h) on the matrix cores: bf16 operands with v_mfma_f32_32x32x16_bf16, fp32 ones with v_mfma_f32_32x32x2_f32,
+// sums in fp32.
+//
+// A workgroup owns a TR x TC tile of one learner's result, its WR x WC wavefronts MR x MC blocks of 32 x 32 of it each.  The contraction
+// goes by slices of 128 bytes (BK = 64 or 32 elements), which lie in LDS in 16-byte chunks:
+//   an operand whose contraction index is contiguous in memory as rows [x][128 bytes], chunk c of row x at c ^ (x/2 mod 8), so that the
+//     sixteen lanes that read together find sixteen different banks' groups;
+//   a turned operand as it lies in memory, [k][TX], its fragments taken by transposing reads (bf16) or single words (fp32); in bf16 the
+//     chunks of row k are exchanged too, by blocks of four, with k mod 4 (rows of 256 bytes and more), so that four rows of a block of 32 lie in different banks.
+// The lanes own slots of that layout in order, which is what loads from memory into LDS want; where an operand is not aligned to 16 bytes
+// or its contiguous extent is no multiple of a chunk, a slice comes through registers into the same slots.  A slice is in flight while the one
+// before it is multiplied (two LDS buffers).  Elements past the contraction are zeros; rows past an operand's extent are anything that can be read,
+// they reach only results that are not stored.
+//
+// The matrix instruction's row index runs along c, so that a lane owns four consecutive columns of a row of the result, after an exchange between
+// the halves of the wavefront eight.
+#pragma once
+#include "linear.h"
+
+namespace kavg {
+
+struct ProductArgs {
+    Matrix R, C;
+    int nR, nC, nK;
+    int tiles_r, tiles_c, splits, per_split;         // per_split: slices of a split
+    uint32_t total, per_xcd;                         // workgroups, and of each of the 8 XCDs
+    Finish finish;
+    float* partial; int pitch; int64_t partial_split;    // or null: nothing is split
+    int side; float* sums; int64_t sums_set, sums_split;
+};
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <class E> struct Kind;
+template <> struct Kind<__bf16> { typedef bf16x8 chunk; static constexpr int V = 8, BK = 64; };
+template <> struct Kind<float> { typedef f32x4 chunk; static constexpr int V = 4, BK = 32; };
+constexpr int SLICE_BYTES = 128, CHUNKS = 8;         // of a row
+
+// which chunk of its row a slot holds
+template <class E, int TX, bool TURNED> __device__ __forceinline__ int swizzle(int row) {
+    if (!TURNED) return (row >> 1) & 7;
+    return sizeof(E) == 2 && TX >= 128 ? (row & 3) * 4 : sizeof(E) == 2 && TX == 64 ? (row >> 1 & 1) * 4 : 0;
+}
+
+// Loads of one operand's slices; every lane owns N chunks of a slice.
+template <class E, int TX, bool TURNED, int NT> struct Loader {
+    static constexpr int V = Kind<E>::V, BK = Kind<E>::BK, N = TX * CHUNKS / NT, PER_ROW = TURNED ? TX / V : CHUNKS;
+    static_assert(N * NT == TX * CHUNKS, "whole chunks per lane");
+    const E* at[N];                 // of the present slice
+    const E* end;                   // behind the operand's last element
+    int k[N];                       // of the chunk's first element in a slice
+    int x[N];                       // turned: of the chunk's first element
+    int slot0;                      // of the wavefront's first chunk
+    int64_t step, stride;
+
+    __device__ __forceinline__ void init(const Matrix& m, int64_t set, int x0, int nX, int k0, int nK, int tid) {
+        const E* base = (const E*)m.base + set * m.set_stride;
+        stride = m.stride;
+        step = TURNED ? BK * stride : BK;
+        end = base + (TURNED ? (int64_t)(nK - 1) * stride + nX : (int64_t)(nX - 1) * stride + nK);
+        slot0 = __builtin_amdgcn_readfirstlane(tid >> 6) * N * 64;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int slot = slot0 + i * 64 + (tid & 63), row = slot / PER_ROW, chunk = (slot % PER_ROW) ^ swizzle<E, TX, TURNED>(row);
+            if (TURNED) {
+                k[i] = row;
+                x[i] = x0 + chunk * V < nX ? x0 + chunk * V : max(nX - V, 0);          // (past the extent: the last chunk)
+                at[i] = base + (int64_t)(k0 + row) * stride + x[i];
+            } else {
+                k[i] = chunk * V;
+                at[i] = base + (int64_t)min(x0 + row, nX - 1) * stride + k0 + k[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] += step;
+    }
+    // straight into LDS; left: elements of the contraction from this slice on.  What lies past it is loaded from before its end, and zeroed by
+    // fix() once it has landed.
+    __device__ __forceinline__ void load(char* tile, int left) const {
+        typedef __attribute__((address_space(3))) void* lds_p;
+        typedef const __attribute__((address_space(1))) void* glb_p;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const E* p = at[i];
+            if (left < BK) {
+                const int over = TURNED ? k[i] - left + 1 : k[i] + V - left;
+                if (over > 0) p -= TURNED ? over * stride : (int64_t)over;
+            }
+            __builtin_amdgcn_global_load_lds((glb_p)p, (lds_p)(tile + (slot0 + i * 64) * 16), 16, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void fix(char* tile, int left, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (k[i] >= left) *(u32x4*)(tile + (slot0 + i * 64 + (tid & 63)) * 16) = (u32x4){0u, 0u, 0u, 0u};
+    }
+    // Through registers, at any alignment and length.  (A turned operand's last chunk of a row may be read into what follows, as far as the operand
+    // reaches in memory.)
+    __device__ __forceinline__ void fetch(u32x4 (&r)[N], int left, int nX) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int there = TURNED ? nX - x[i] : left - k[i];
+            const int whole = !TURNED ? there : k[i] >= left ? 0 : there > 0 && end - at[i] >= V ? V : there;
+            if (whole >= V) r[i] = __builtin_bit_cast(u32x4, pack_load<E, V>(at[i]));
+            else {
+                typename Kind<E>::chunk c;
+#pragma unroll
+                for (int e = 0; e < V; ++e) c[e] = e < whole ? at[i][e] : (E)0.f;
+                r[i] = __builtin_bit_cast(u32x4, c);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(const u32x4 (&r)[N], char* tile, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(u32x4*)(tile + (slot0 + i * 64 + (tid & 63)) * 16) = r[i];
+    }
+};
+
+// The operand of a matrix instruction: slab kk (two chunks) of the 32 rows from x0 on.
+template <class E, int TX, bool TURNED> __device__ __forceinline__ typename Kind<E>::chunk fragment(const char* tile, int x0, int kk, int lane) {
+    const int half = lane >> 5;
+    if constexpr (!TURNED) {
+        const int x = x0 + (lane & 31);
+        return *(const typename Kind<E>::chunk*)(tile + x * SLICE_BYTES + ((kk * 2 + half) ^ swizzle<E, TX, false>(x)) * 16);
+    } else if constexpr (sizeof(E) == 2) {
+        // in a group of 16 lanes, lane 4a + b fetches x = 4b .. 4b+3 of row a and receives the four rows of x = 4a + b
+        const int t = lane & 15, group = lane >> 4, row = kk * 16 + (group >> 1) * 8 + (t >> 2);
+        const int chunk = (x0 / 8 + (group & 1) * 2 + ((t & 3) >> 1)) ^ swizzle<E, TX, true>(row);
+        const char* p = tile + row * (TX * 2) + chunk * 16 + (t & 1) * 8;
+        typedef bf16x4 __attribute__((address_space(3))) * lds_ptr;
+        const char* q = tile + (row + 4) * (TX * 2) + ((x0 / 8 + (group & 1) * 2 + ((t & 3) >> 1)) ^ swizzle<E, TX, true>(row + 4)) * 16 + (t & 1) * 8;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)q);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+        f32x4 v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] = *(const float*)(tile + (kk * 8 + half * 4 + t) * (TX * 4) + (x0 + (lane & 31)) * 4);
+        return v;
+    }
+}
+
+__device__ __forceinline__ f32x16 multiply(const bf16x8& c, const bf16x8& r, f32x16 acc) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, r, acc, 0, 0, 0); }
+__device__ __forceinline__ f32x16 multiply(const f32x4& c, const f32x4& r, f32x16 acc) {
+    // (element t of both chunks: k = t of the lower lanes' chunk and of the upper lanes')
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(c[t], r[t], acc, 0, 0, 0);
+    return acc;
+}
+__device__ __forceinline__ void add_up(const bf16x8& f, float (&s)[4]) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    const pair ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_fdot2_f32_bf16((pair){f[2 * i], f[2 * i + 1]}, ones, s[i], false);
+}
+__device__ __forceinline__ void add_up(const f32x4& f, float (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += f[i];
+}
+
+template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT> struct ProductTile {
+    static constexpr int NT = 64 * WR * WC * WK, MR = TR / (32 * WR), MC = TC / (32 * WC);
+    static constexpr int BUFFER = (TR + TC) * SLICE_BYTES;
+    static constexpr int JOIN = WK > 1 ? WR * WC * MR * MC * 16 * 64 * 4 : 0;            // a k group's sums
+    static constexpr int LDS = 2 * BUFFER > JOIN ? 2 * BUFFER : JOIN;
+};
+
+template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT>
+__global__ void __launch_bounds__(64 * WR * WC * WK) product_kernel(ProductArgs a) {
+    typedef ProductTile<E, TR, TC, WR, WC, WK, RT, CT, DIRECT> P;
+    typedef typename Kind<E>::chunk chunk;
+    constexpr int NT = P::NT, MR = P::MR, MC = P::MC, BK = Kind<E>::BK, SLABS = 4 / WK;
+    static_assert(!RT || WK == 1, "sums of an operand are those of one group of wavefronts");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wk = wave / (WR * WC), wr = wave % (WR * WC) / WC, wc = wave % WC;
+
+    // Workgroups go round the 8 XCDs in launch order; each XCD takes a run of tiles, which share operands in its L2, eight rows of tiles at a time.
+    const uint32_t number = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (number >= a.total) return;
+    const uint32_t tiles = (uint32_t)a.tiles_r * a.tiles_c, which = number / tiles, tile = number - which * tiles;
+    const int64_t set = which / (uint32_t)a.splits;
+    const int split = (int)(which % (uint32_t)a.splits);
+    const uint32_t band = tile / (8u * a.tiles_c), in_band = tile - band * 8u * a.tiles_c, height = min(8u, (uint32_t)a.tiles_r - band * 8u);
+    const int tile_c = (int)(in_band / height), tile_r = (int)(band * 8 + in_band % height);
+    const int r0 = tile_r * TR, c0 = tile_c * TC;
+    const int slice0 = split * a.per_split, slices = min(a.per_split, (a.nK + BK - 1) / BK - slice0);
+    int left = a.nK - slice0 * BK;
+
+    Loader<E, TR, RT, NT> rl;
+    Loader<E, TC, CT, NT> cl;
+    rl.init(a.R, set, r0, a.nR, slice0 * BK, a.nK, tid);
+    cl.init(a.C, set, c0, a.nC, slice0 * BK, a.nK, tid);
+
+    f32x16 acc[MR][MC];
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+        for (int j = 0; j < MC; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    constexpr int MS = MR > MC ? MR : MC;
+    float sums[RT ? MS : 1][4] = {};
+    const bool sum_r = RT && a.side == 1 && tile_c == 0 && wc == 0, sum_c = RT && a.side == 2 && tile_r == 0 && wr == 0;
+
+    auto multiply_slice = [&](const char* buffer) {
+        const char *rt = buffer, *ct = buffer + TR * SLICE_BYTES;
+        chunk rf[2][MR], cf[2][MC];
+        auto take = [&](int to, int s) {
+            const int kk = wk * SLABS + s;
+#pragma unroll
+            for (int j = 0; j < MC; ++j) cf[to][j] = fragment<E, TC, CT>(ct, (wc * MC + j) * 32, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MR; ++i) rf[to][i] = fragment<E, TR, RT>(rt, (wr * MR + i) * 32, kk, lane);
+        };
+        take(0, 0);
+#pragma unroll
+        for (int s = 0; s < SLABS; ++s) {
+            if (s + 1 < SLABS) take((s + 1) & 1, s + 1);
+#pragma unroll
+            for (int i = 0; i < MR; ++i)
+#pragma unroll
+                for (int j = 0; j < MC; ++j) acc[i][j] = multiply(cf[s & 1][j], rf[s & 1][i], acc[i][j]);
+            if (sum_r) {
+#pragma unroll
+                for (int i = 0; i < MR; ++i) add_up(rf[s & 1][i], sums[RT ? i : 0]);
+            }
+            if (sum_c) {
+#pragma unroll
+                for (int j = 0; j < MC; ++j) add_up(cf[s & 1][j], sums[RT ? j : 0]);
+            }
+        }
+    };
+
+    if constexpr (DIRECT) {
+        rl.load(lds, left);
+        cl.load(lds + TR * SLICE_BYTES, left);
+        for (int s = 0; s < slices; ++s, left -= BK) {
+            char* now = lds + (s & 1) * P::BUFFER;
+            char* next = lds + (~s & 1) * P::BUFFER;
+            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0): this wavefront's part of the slice has landed
+            if (left < BK) {
+                rl.fix(now, left, tid);
+                cl.fix(now + TR * SLICE_BYTES, left, tid);
+            }
+            __syncthreads();                                 // everyone's has, and the other buffer is no longer read
+            if (s + 1 < slices) {
+                rl.advance();
+                cl.advance();
+                rl.load(next, left - BK);
+                cl.load(next + TR * SLICE_BYTES, left - BK);
+            }
+            multiply_slice(now);
+        }
+    } else {
+        u32x4 rr[rl.N], cr[cl.N];
+        rl.fetch(rr, left, a.nR);
+        cl.fetch(cr, left, a.nC);
+        for (int s = 0; s < slices; ++s, left -= BK) {
+            char* now = lds + (s & 1) * P::BUFFER;
+            rl.put(rr, now, tid);
+            cl.put(cr, now + TR * SLICE_BYTES, tid);
+            __syncthreads();                                 // (the buffer's last reads lie before the last barrier)
+            if (s + 1 < slices) {
+                rl.advance();
+                cl.advance();
+                rl.fetch(rr, left - BK, a.nR);
+                cl.fetch(cr, left - BK, a.nC);
+            }
+            multiply_slice(now);
+        }
+    }
+
+    if constexpr (WK > 1) {                                  // the k groups' sums, in order
+        float* join = (float*)lds + (wave % (WR * WC)) * MR * MC * 16 * 64 + lane;
+        for (int g = 1; g < WK; ++g) {
+            __syncthreads();
+            if (wk == g) {
+#pragma unroll
+                for (int i = 0; i < MR; ++i)
+#pragma unroll
+                    for (int j = 0; j < MC; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) join[((i * MC + j) * 16 + e) * 64] = acc[i][j][e];
+            }
+            __syncthreads();
+            if (wk == 0) {
+#pragma unroll
+                for (int i = 0; i < MR; ++i)
+#pragma unroll
+                    for (int j = 0; j < MC; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[i][j][e] += join[((i * MC + j) * 16 + e) * 64];
+            }
+        }
+        if (wk) return;
+    }
+
+    if (RT && (sum_r || sum_c)) {
+        float* to = a.sums + set * a.sums_set + split * a.sums_split;
+        const int first = sum_r ? r0 + wr * MR * 32 : c0 + wc * MC * 32, n = sum_r ? a.nR : a.nC;
+#pragma unroll
+        for (int i = 0; i < MS; ++i) {
+            if (i >= (sum_r ? MR : MC)) break;
+            const float half = (sums[RT ? i : 0][0] + sums[RT ? i : 0][1]) + (sums[RT ? i : 0][2] + sums[RT ? i : 0][3]);
+            const float sum = half + __shfl_xor(half, 32);
+            const int x = first + i * 32 + lane;
+            if (lane < 32 && x < n) to[x] = sum;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MR; ++i) {
+        const int r = r0 + (wr * MR + i) * 32 + (lane & 31);
+#pragma unroll
+        for (int j = 0; j < MC; ++j) {
+#pragma unroll
+            for (int q = 0; q < 4; q += 2) {
+                // columns 8q + 4 half .. of two groups of eight: the lower half of the wavefront takes the first, the upper half the second
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float lower = acc[i][j][q * 4 + e], upper = acc[i][j][q * 4 + 4 + e];      // (__builtin_bit_cast of a vector's element takes its first)
+                    const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lower), __builtin_bit_cast(uint32_t, upper), false, false);
+                    v[e] = __builtin_bit_cast(float, (uint32_t)p[0]);
+                    v[4 + e] = __builtin_bit_cast(float, (uint32_t)p[1]);
+                }
+                const int c = c0 + (wc * MC + j) * 32 + (q + (lane >> 5)) * 8, n = a.nC - c;
+                if (r >= a.nR || n <= 0) continue;
+                if (a.partial) store_some<float, 8>(a.partial + split * a.partial_split + (set * a.nR + r) * a.pitch + c, 8, v);
+                else if constexpr (RT) store_some<float, 8>((float*)a.finish.out + set * a.finish.out_set + r * a.finish.out_row + c, n, v);
+                else finish_values<E, E, 8>(a.finish, set, r, c, n, v);
+            }
+        }
+    }
+}
+
+// Tiles: rows, columns, wavefronts along rows, columns and the contraction.  The first two are those of large results, the third of small
+// ones, the others of results that are narrow one way.
+#define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4, 1) TILE(1, 128, 128, 2, 2, 1) TILE(2, 64, 64, 2, 2, 1) TILE(3, 128, 32, 4, 1, 1) TILE(4, 32, 128, 1, 4, 1)
+enum { TILE_LARGE = 0, TILE_MIDDLE = 1, TILE_SMALL = 2, TILE_TALL = 3, TILE_WIDE = 4, TILE_KINDS = 5 };
+
+// DIRECT wants operands whose chunks are aligned and whole; the largest tile is for such operands only
+template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT>
+hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
+    typedef ProductTile<E, TR, TC, WR, WC, WK, RT, CT, DIRECT> P;
+    const auto kernel = product_kernel<E, TR, TC, WR, WC, WK, RT, CT, DIRECT>;
+    if (P::LDS > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<dim3(8 * a.per_xcd), dim3(P::NT), P::LDS, st>>>(a);
+    return hipGetLastError();
+}
+
+template <class E, bool RT, bool CT> hipError_t start_kind(int tile, bool direct, const ProductArgs& a, hipStream_t st) {
+#define TILE(NUMBER, TR, TC, WR, WC, WK) \
+    case NUMBER: \
+        if (direct) return start_tile<E, TR, TC, WR, WC, WK, RT, CT, true>(a, st); \
+        if constexpr (TR * TC < 256 * 256) return start_tile<E, TR, TC, WR, WC, WK, RT, CT, false>(a, st); \
+        break;
+    switch (tile) { KAVG_TILES(TILE) }
+#undef TILE
+    return hipErrorInvalidValue;
+}
+
+}  // namespace kavg

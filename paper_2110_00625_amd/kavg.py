@@ -25,6 +25,7 @@ EXPORTS = [
     "kavg_velocity_bytes", "kavg_set_learner_momentum", "kavg_velocity", "kavg_graph", "kavg_init_static", "kavg_probe", "kavg_refresh_bytes", "kavg_set_refresh",
     "kavg_num_params_conv", "kavg_workspace_bytes_conv", "kavg_init_conv", "kavg_fused", "kavg_set_fused", "kavg_set_wait_limit",
     "kavg_group_norm_workspace", "kavg_group_norm", "kavg_group_norm_backward", "kavg_dropout", "kavg_dropout_backward",
+    "kavg_linear_workspace", "kavg_linear", "kavg_linear_backward", "kavg_adamw",
 ]
 STATIC_WORKSPACE_BYTES = 32 << 20
 CLASS_NAMES = ["index", "forward", "loss", "backward", "update", "meta", "head", "correction"]
@@ -105,6 +106,10 @@ def load_library():
                          ctypes.c_uint64, c_vp],
         "kavg_dropout_backward": [c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_int, ctypes.c_double, ctypes.c_uint64,
                                   ctypes.c_uint64, c_vp],
+        "kavg_linear_workspace": [ctypes.c_char_p, c_int, ctypes.POINTER(c_sz)],
+        "kavg_linear": [ctypes.c_char_p] * 3 + [c_vp, c_i64] + [ctypes.c_char_p] * 3 + [c_vp, c_sz, c_vp],
+        "kavg_linear_backward": [ctypes.c_char_p] * 7 + [c_vp, c_i64, c_vp, c_sz, c_vp],
+        "kavg_adamw": [ctypes.c_char_p, c_vp, c_int, c_vp],
         "kavg_probe": [c_int, c_vp, c_vp, c_sz, c_int, c_vp, c_vp, ctypes.POINTER(ctypes.c_double)],
     }.items():
         fn = getattr(lib, name)
@@ -406,6 +411,288 @@ def kavg_dropout_backward(dy, drop, seed, site=0, out=None):
     if rc != KAVG_OK:
         _failed("kavg_dropout_backward", rc)
     return dx
+
+
+# -- products of a learner's layer ----------------------------------------------------------------------------------------
+
+_PRODUCT = struct.Struct("=iiqqqq")           # kavg_product
+_MATRIX = struct.Struct("=Qqq")               # kavg_rows
+_WEIGHTS = struct.Struct("=Qqqq")             # kavg_weights
+
+
+def _sides(x, weight):
+    """(leading dimensions, rows, inputs, outputs) of x [sets, rows, inputs] and weight [sets, outputs, inputs], or both without sets."""
+    _dtype(x, "x")
+    shape, of = x.shape, weight.shape
+    if len(shape) not in (2, 3) or len(of) != len(shape) or of[-1] != shape[-1] or of[:-2] != shape[:-2]:
+        _bad("x of %s and weights of %s: [sets, rows, inputs] and [sets, outputs, inputs] or [rows, inputs] and [outputs, inputs] are wanted" % (tuple(shape), tuple(of)))
+    if weight.dtype is not x.dtype or weight.device != x.device:
+        _bad("weight is not of x's type and device")
+    return tuple(shape[:-2]), shape[-2], shape[-1], of[-2]
+
+
+def _product(x, activation, lead, rows, inputs, outputs):
+    try:
+        return _PRODUCT.pack(_DTYPES[x.dtype], activation, lead[0] if lead else 1, rows, inputs, outputs)
+    except (struct.error, TypeError, OverflowError) as e:
+        _bad(str(e))
+
+
+def _matrix(t, x, shape, name):
+    """kavg_rows of a tensor of that shape and of x's type and device."""
+    if t.dtype is not x.dtype or t.device != x.device or t.shape != shape:
+        _bad("%s is not a tensor of %s of x's type and device" % (name, list(shape)))
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        _bad("%s has a last stride of %d" % (name, st[-1]))
+    return _MATRIX.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
+
+
+def _weights(t, name):
+    """kavg_weights of [sets, outputs, inputs] or [outputs, inputs], in either order in memory."""
+    st, shape = t.stride(), t.shape
+    if st[-1] != 1 and st[-2] != 1 and shape[-1] > 1 and shape[-2] > 1:
+        _bad("%s has strides of %s: outputs or inputs have to lie together" % (name, list(st)))
+    return _WEIGHTS.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2], st[-1])
+
+
+def _product_workspace(product, backward, x):
+    n = ctypes.c_size_t(0)
+    if _lib.kavg_linear_workspace(product, backward, ctypes.byref(n)) != KAVG_OK:
+        _bad("kavg_linear rejected its sizes or options")
+    if not n.value:
+        return None, None, 0
+    block = _torch_module.empty(n.value, dtype=_torch_module.uint8, device=x.device)
+    return block, block.data_ptr(), n.value
+
+
+def kavg_linear(x, weight, bias=None, activation=KAVG_ACT_NONE, residual=None, pre=False, out=None):
+    """residual + activation(x W^T + bias) of all learners: x [sets, rows, inputs] with weight [sets, outputs, inputs], or [rows, inputs]
+    with [outputs, inputs]; float32 or bfloat16, x with any strides but a last one of 1, weights in either order (a transposed
+    view will do); bias [sets, outputs] or [outputs] in float32, or None; residual like the result, or None.  Returns y (out, if
+    given: the residual among others), or with pre=True or a tensor to write to (y, pre), pre being x W^T + bias, which
+    kavg_linear_backward of the layer above wants."""
+    torch = _torch_module or _torch()
+    if not isinstance(weight, torch.Tensor):
+        _bad("weight is no tensor")
+    lead, rows, inputs, outputs = _sides(x, weight)
+    product = _product(x, activation, lead, rows, inputs, outputs)
+    shape = lead + (rows, outputs)
+    b, bs = None, 0
+    if bias is not None:
+        if bias.dtype is not torch.float32 or bias.device != x.device or bias.shape != lead + (outputs,):
+            _bad("bias is not a float32 tensor of %s on x's device" % list(lead + (outputs,)))
+        b, st = bias.data_ptr(), bias.stride()
+        bs = st[0] if lead else 0
+        if st[-1] != 1 and outputs > 1:
+            _bad("bias has a last stride of %d" % st[-1])
+    block, at, nbytes = _product_workspace(product, 0, x)
+    y = x.new_empty(shape) if out is None else out
+    kept = None if pre is False or pre is None else x.new_empty(shape) if pre is True else pre
+    rc = _launch(x, _lib.kavg_linear, product, _matrix(x, x, x.shape, "x"), _weights(weight, "weight"), b, bs,
+                 None if residual is None else _matrix(residual, x, shape, "residual"), _matrix(y, x, shape, "out"),
+                 None if kept is None else _matrix(kept, x, shape, "pre"), at, nbytes)
+    if rc != KAVG_OK:
+        _failed("kavg_linear", rc)
+    return y if kept is None else (y, kept)
+
+
+def _fp32(given, x, shape, name):
+    """The gradient to write: the tensor given, a new one for None, None for False."""
+    if given is False:
+        return None
+    if given is None:
+        return _torch_module.empty(shape, dtype=_torch_module.float32, device=x.device)
+    if given.dtype is not _torch_module.float32 or given.device != x.device or given.shape != shape:
+        _bad("%s is not a float32 tensor of %s on x's device" % (name, list(shape)))
+    return given
+
+
+def kavg_linear_backward(dz, x, weight, activation=KAVG_ACT_NONE, pre=None, out=None, dweight=None, dbias=None):
+    """Gradients of kavg_linear from dz [sets, rows, outputs] (or [rows, outputs]), the gradient of x W^T + bias: (dx, dweight, dbias).
+    With an activation, the one that x came from, dx is the gradient of that activation's input, `pre`.  Each gradient goes into the
+    tensor given (out for dx: pre or x among others; dweight float32 like weight, in either order; dbias float32), into a new one for
+    None (dweight in weight's order), and is left out, and None, for False."""
+    torch = _torch_module or _torch()
+    if not isinstance(weight, torch.Tensor):
+        _bad("weight is no tensor")
+    lead, rows, inputs, outputs = _sides(x, weight)
+    product = _product(x, activation, lead, rows, inputs, outputs)
+    z = _matrix(dz, x, lead + (rows, outputs), "dz")
+    block, at, nbytes = _product_workspace(product, 1, x)
+    dx = None if out is False else torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    d = p = None
+    if dx is not None:
+        d = _matrix(dx, x, x.shape, "out")
+        if activation != KAVG_ACT_NONE:
+            if pre is None:
+                _bad("the slope of an activation wants pre")
+            p = _matrix(pre, x, x.shape, "pre")
+    if dweight is None and weight.stride(-1) != 1 and inputs > 1:
+        dweight = torch.empty(lead + (inputs, outputs), dtype=torch.float32, device=x.device).transpose(-1, -2)
+    dw, db = _fp32(dweight, x, weight.shape, "dweight"), _fp32(dbias, x, lead + (outputs,), "dbias")
+    b = bs = 0
+    if db is not None:
+        b, st = db.data_ptr(), db.stride()
+        bs = st[0] if lead else 0
+        if st[-1] != 1 and outputs > 1:
+            _bad("dbias has a last stride of %d" % st[-1])
+    rc = _launch(x, _lib.kavg_linear_backward, product, z, _matrix(x, x, x.shape, "x"), _weights(weight, "weight"), p, d,
+                 None if dw is None else _weights(dw, "dweight"), b or None, bs, at, nbytes)
+    if rc != KAVG_OK:
+        _failed("kavg_linear_backward", rc)
+    return dx, dw, db
+
+
+# -- step of a learner ------------------------------------------------------------------------------------------------------
+
+_TENSOR = struct.Struct("=7Q5qfi")            # kavg_adamw_tensor
+_GRAD = struct.Struct("=Q")                   # its gradient (at 8), the gradient's stride (at 80), its weight decay (at 96)
+_STRIDE = struct.Struct("=q")
+_DECAY = struct.Struct("=f")
+_STEP = struct.Struct("=iidddddQQQQQ")        # kavg_adamw_options
+_BLOCK = 256                                  # values of an 8-bit state that share a scale
+
+
+def _run(x, name, rows=None):
+    """(rows, columns, row stride) of a tensor: trailing dimensions without gaps are the columns, the others evenly spaced rows.  rows: as
+    many are wanted (a tensor without gaps can have any number of them)."""
+    n = x.numel()
+    if x.is_contiguous():
+        r = rows or 1
+        if n % r:
+            _bad("%s does not lie in %d rows" % (name, r))
+        return r, n // r, n // r
+    shape, st = x.shape, x.stride()
+    cols, d = 1, x.dim() - 1
+    while d >= 0 and (shape[d] == 1 or st[d] == cols):
+        cols *= shape[d]
+        d -= 1
+    r, stride = 1, 0
+    for d in range(d, -1, -1):
+        if shape[d] == 1:
+            continue
+        if r == 1:
+            stride = st[d]
+        elif st[d] != stride * r:
+            _bad("%s does not lie in evenly spaced rows" % name)
+        r *= shape[d]
+    if rows is not None and r != rows:
+        _bad("%s does not lie in %d rows" % (name, rows))
+    return r, cols, stride
+
+
+class AdamW:
+    """AdamW steps over many tensors at once (kavg_adamw): a table of parameters (float32 on one device, whose trailing dimensions lie
+    together: whole tensors, or views [P, ..] of the learners' rows of the replicas), their states, and bfloat16 copies of
+    the parameters if wanted (a list like params, with None where there is none).
+
+    states: per parameter (m, v) of 32 bits, float32 and like the parameter without gaps, or (m, v, m_scale, v_scale) of 8 bits, float8_e4m3fn
+    and float32 [rows, blocks of 256 of a row]; v of 8 bits holds the root of the second moment.  Made by `zeros` if not given, of
+    `bits`, with a row per learner where the parameter lies in rows.  They are `self.states`, written by every step."""
+
+    def __init__(self, params, states=None, copies=None, bits=32):
+        torch = _torch_module or _torch()
+        self.params, self.copies = list(params), list(copies) if copies is not None else [None] * len(params)
+        if bits not in (8, 32):
+            _bad("states of %r bits" % (bits,))
+        if states is None:
+            states = [self.zeros(p, bits) for p in self.params]
+        self.states = [tuple(s) for s in states]
+        if len(self.states) != len(self.params) or len(self.copies) != len(self.params) or len({len(s) for s in self.states}) > 1:
+            _bad("%d parameters, %d states, %d copies" % (len(self.params), len(self.states), len(self.copies)))
+        self.bits = bits if not self.states else 32 if len(self.states[0]) == 2 else 8
+        self.device = self.params[0].device if self.params else None
+        self._table = ctypes.create_string_buffer(_TENSOR.size * max(1, len(self.params)))
+        self._rows, self._decay, written = [], None, set()
+        for i, (p, state, copy) in enumerate(zip(self.params, self.states, self.copies)):
+            name = "params[%d]" % i
+            _dtype(p, name)
+            if p.dtype is not torch.float32 or p.device != self.device:
+                _bad("%s is not a float32 tensor on the device of the others" % name)
+            self._check_state(torch, p, state, "states[%d]" % i)
+            rows = state[2].shape[0] if self.bits == 8 else None
+            rows, cols, stride = _run(p, name, rows)
+            if self.bits == 8 and p.numel() and state[2].shape[1] != (cols + _BLOCK - 1) // _BLOCK:
+                _bad("states[%d] has scales for %s blocks of %d columns" % (i, tuple(state[2].shape), cols))
+            at, cs = 0, 0
+            if copy is not None:
+                if copy.dtype is not torch.bfloat16 or copy.shape != p.shape or copy.device != p.device:
+                    _bad("copies[%d] is not a bfloat16 tensor like the parameter" % i)
+                at, cs = copy.data_ptr(), _run(copy, "copies[%d]" % i, rows)[2]
+            pointers = [p.data_ptr(), 0, state[0].data_ptr(), state[1].data_ptr()] + ([s.data_ptr() for s in state[2:]] if self.bits == 8 else [0, 0]) + [at]
+            for a in pointers if p.numel() else ():
+                if a and a in written:
+                    _bad("%s, its state or its copy is given twice" % name)
+                written.add(a)
+            _TENSOR.pack_into(self._table, i * _TENSOR.size, *pointers, rows, cols, stride, cols, cs, 0.0, 0)
+            self._rows.append((p.shape, rows, cols))
+
+    @staticmethod
+    def zeros(p, bits=32):
+        """The states of a parameter in front of its first step."""
+        torch = _torch_module or _torch()
+        _dtype(p, "a parameter")
+        if bits == 32:
+            return tuple(torch.zeros(p.shape, dtype=torch.float32, device=p.device) for _ in "mv")
+        rows, cols, _ = _run(p, "a parameter")
+        codes = [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for _ in "mv"]
+        # (the scale of a block of zeros)
+        return (*codes, *(torch.full((rows, (cols + _BLOCK - 1) // _BLOCK), 2.0 ** -126, device=p.device) for _ in "mv"))
+
+    @staticmethod
+    def _check_state(torch, p, state, name):
+        of = (torch.float32,) * 2 if len(state) == 2 else (torch.float8_e4m3fn,) * 2 + (torch.float32,) * 2
+        if len(state) not in (2, 4) or any(s.dtype is not t or s.device != p.device or not s.is_contiguous() for s, t in zip(state, of)):
+            _bad("%s is neither (m, v) nor (m, v, m_scale, v_scale) without gaps on the parameter's device" % name)
+        if state[0].shape != p.shape or state[1].shape != p.shape:
+            _bad("%s is not of the parameter's shape" % name)
+        if len(state) == 4 and (state[2].dim() != 2 or state[2].shape != state[3].shape or not state[2].shape[0]):
+            _bad("%s has scales of %s and %s" % (name, tuple(state[2].shape), tuple(state[3].shape)))
+
+    def _device_number(self, value, dtype, name):
+        """(number, address) of a host's number or of a tensor of one element."""
+        if not isinstance(value, _torch_module.Tensor):
+            return value, 0
+        if value.dtype is not dtype or value.numel() != 1 or value.device != self.device:
+            _bad("%s is neither a number nor one %s on the parameters' device" % (name, dtype))
+        return None, value.data_ptr()
+
+    def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, seed=0):
+        """Step number `step` (from 1 on) with gradients like the parameters, all float32 or all bfloat16, in whole or evenly spaced rows; in place.
+        weight_decay: a number, or one per parameter.  step, lr, grad_scale may be tensors of one element on the device (int64, float32,
+        float32), which are read when the kernels run: a recorded graph goes on with what they hold then.  seed: of the roundings of
+        8-bit states, with the step added to it; not the index_seed of a context."""
+        torch, table, size = _torch_module, self._table, _TENSOR.size
+        if len(grads) != len(self.params):
+            _bad("%d gradients of %d parameters" % (len(grads), len(self.params)))
+        if not self.params:
+            return
+        if self._decay != weight_decay:
+            each = [float(weight_decay)] * len(self.params) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+            if len(each) != len(self.params):
+                _bad("%d weight decays of %d parameters" % (len(each), len(self.params)))
+            for i, w in enumerate(each):
+                _DECAY.pack_into(table, i * size + 96, w)
+            self._decay = weight_decay if isinstance(weight_decay, (int, float)) else None
+        code, of, device, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, 8
+        for g, (shape, rows, cols) in zip(grads, self._rows):
+            if g.dtype is not of or g.shape != shape or g.device != device:
+                _bad("gradients are not of one type, or not of the parameters' shapes and device")
+            _GRAD.pack_into(table, at, g.data_ptr())
+            _STRIDE.pack_into(table, at + 72, cols if g.is_contiguous() else _run(g, "a gradient", rows)[2])
+            at += size
+        number, step_at = self._device_number(step, torch.int64, "step")
+        rate, lr_at = self._device_number(lr, torch.float32, "lr")
+        scale, scale_at = self._device_number(grad_scale, torch.float32, "grad_scale")
+        try:
+            options = _STEP.pack(self.bits, code, 0.0 if rate is None else rate, beta1, beta2, eps, 1.0 if scale is None else scale,
+                                 1 if number is None else number, seed, step_at, lr_at, scale_at)
+        except (struct.error, TypeError, OverflowError) as e:
+            _bad(str(e))
+        rc = _launch(self.params[0], _lib.kavg_adamw, options, ctypes.addressof(table), len(self.params))
+        if rc != KAVG_OK:
+            _failed("kavg_adamw", rc)
 
 
 class MAvg:
