@@ -148,6 +148,7 @@ int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const
         c.dtype = p->dtype; c.sets = p->sets;
         c.nK = (int)p->rows;
         c.r_turned = c.c_turned = true;
+        c.finish.floor = -INFINITY;
         c.sums = dbias; c.sums_set = p->sets > 1 ? dbias_stride : 0;
         const Matrix of_dz = matrix_of(p, dz, p->outputs);
         const bool other = dweight && turned(p, dweight);                // dW lies as [inputs][outputs]

@@ -79,40 +79,63 @@ template <class E, int V> __device__ __forceinline__ void store_some(E* p, int n
     }
 }
 
-// n <= V values of row r from column c on.  E: type of the operands, O: of the result.
-template <class E, class O, int V>
-__device__ __forceinline__ void finish_values(const Finish& f, int64_t set, int64_t r, int c, int n, float (&v)[V]) {
-    float t[V];
-    if (f.bias) {
-        load_some<float, V>(f.bias + set * f.bias_set + c, n, t);
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += t[k];
+// What the values of N rows want from memory, all asked for before the first is used (a store in between could not be passed by a load).
+// E: type of the operands, O: of the result.  Columns c .. c+7 of rows r, r + step, ..; n of the columns are there, all eight if WHOLE.
+template <class E, class O, int N, bool WHOLE> struct Finisher {
+    const Finish& f;
+    int64_t set;
+    int c, n;
+    float bias[8];
+
+    __device__ __forceinline__ Finisher(const Finish& f, int64_t set, int c, int left) : f(f), set(set), c(c), n(WHOLE ? 8 : left) {
+        if (f.bias) load_some<float, 8>(f.bias + set * f.bias_set + c, n, bias);
     }
-    if (f.kept) store_some<E, V>((E*)f.kept + set * f.kept_set + r * f.kept_row + c, n, v);
-    if (f.silu) {
+    // value(u, v): the eight values of row r + u * step; rows from `end` on are left out
+    template <class Value> __device__ __forceinline__ void operator()(int64_t r, int step, int64_t end, Value value) const {
+        if (!WHOLE && n <= 0) return;
+        float before[N][8], residual[N][8];
+        if (f.before) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] *= sigmoid_of(v[k] * SILU_SCALE);
-    } else {
+            for (int u = 0; u < N; ++u) if (r + u * step < end) load_some<E, 8>((const E*)f.before + set * f.before_set + (r + u * step) * f.before_row + c, n, before[u]);
+        }
+        if (f.residual) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = __builtin_elementwise_maximum(v[k], f.floor);
-    }
-    if (f.before) {
-        load_some<E, V>((const E*)f.before + set * f.before_set + r * f.before_row + c, n, t);
-        if (f.slope_silu) {
+            for (int u = 0; u < N; ++u) if (r + u * step < end) load_some<E, 8>((const E*)f.residual + set * f.residual_set + (r + u * step) * f.residual_row + c, n, residual[u]);
+        }
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = through_slope<true>(v[k], t[k] * SILU_SCALE, 0.f);
-        } else {
+        for (int u = 0; u < N; ++u) {
+            if (r + u * step >= end) break;
+            float v[8];
+            value(u, v);
+            if (f.bias) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = through_slope<false>(v[k], t[k], 0.f);
+                for (int k = 0; k < 8; ++k) v[k] += bias[k];
+            }
+            if (f.kept) store_some<E, 8>((E*)f.kept + set * f.kept_set + (r + u * step) * f.kept_row + c, n, v);
+            if (f.silu) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= sigmoid_of(v[k] * SILU_SCALE);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __builtin_elementwise_maximum(v[k], f.floor);
+            }
+            if (f.before) {
+                if (f.slope_silu) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = through_slope<true>(v[k], before[u][k] * SILU_SCALE, 0.f);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = through_slope<false>(v[k], before[u][k], 0.f);
+                }
+            }
+            if (f.residual) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] += residual[u][k];
+            }
+            store_some<O, 8>((O*)f.out + set * f.out_set + (r + u * step) * f.out_row + c, n, v);
         }
     }
-    if (f.residual) {
-        load_some<E, V>((const E*)f.residual + set * f.residual_set + r * f.residual_row + c, n, t);
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] += t[k];
-    }
-    store_some<O, V>((O*)f.out + set * f.out_set + r * f.out_row + c, n, v);
-}
+};
 #endif
 
 }  // namespace kavg

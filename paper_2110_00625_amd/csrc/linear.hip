@@ -19,7 +19,7 @@ constexpr int64_t MOST_TILES = 1 << 22;          // of a launch (fewer than 2^32
 
 struct Size { int r, c; };
 constexpr Size tile_size(int tile) {
-#define TILE(NUMBER, TR, TC, WR, WC, WK) if (tile == NUMBER) return {TR, TC};
+#define TILE(NUMBER, TR, TC, WR, WC) if (tile == NUMBER) return {TR, TC};
     KAVG_TILES(TILE)
 #undef TILE
     return {0, 0};
@@ -33,7 +33,7 @@ int64_t tiles_of(int tile, int64_t sets, int nR, int nC) {
 }
 
 // A lane adds up the parts of eight columns of a row, in order, and finishes them; the sums follow after the last row.
-template <class E, bool GRADIENT>
+template <class E>
 __global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, uint32_t per_row, Divisor by_row) {
     const uint64_t first = (uint64_t)blockIdx.x * T;
     if (first < packs) {
@@ -52,8 +52,11 @@ __global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, 
             for (int k = 0; k < 8; ++k) v[k] += t[k];
         }
         const int64_t set = (int64_t)(row / (uint64_t)a.nR), r = (int64_t)(row - (uint64_t)set * a.nR);
-        if constexpr (GRADIENT) store_some<float, 8>((float*)a.finish.out + set * a.finish.out_set + r * a.finish.out_row + c, a.nC - c, v);
-        else finish_values<E, E, 8>(a.finish, set, r, c, a.nC - c, v);
+        const Finisher<E, E, 1, false> finish(a.finish, set, c, a.nC - c);
+        finish(r, 1, a.nR, [&](int, float (&to)[8]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) to[k] = v[k];
+        });
     }
 }
 
@@ -153,9 +156,8 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
                 const uint64_t packs = (uint64_t)sets * a.nR * per_row;
                 if (packs) {
                     const dim3 grid((unsigned)up(packs, T)), lanes(T);
-                    if (call.r_turned) join_kernel<float, true><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
-                    else if (bf16) join_kernel<__bf16, false><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
-                    else join_kernel<float, false><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
+                    if (bf16 && !call.r_turned) join_kernel<__bf16><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
+                    else join_kernel<float><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
                 }
                 if (call.side) join_sums_kernel<<<dim3((unsigned)up(sets * sums.n, T)), dim3(T), 0, st>>>(sums);
                 e = hipGetLastError();

@@ -12,10 +12,10 @@
 // before it is multiplied (two LDS buffers).  Elements past the contraction are zeros; rows past an operand's extent are anything that can be read,
 // they reach only results that are not stored.
 //
-// The matrix instruction's row index runs along c, so that a lane owns four consecutive columns of a row of the result, after an exchange between
-// the halves of the wavefront eight.
+// The matrix instruction's row index runs along c, so that a lane owns four consecutive columns of a row of the result.
 #pragma once
 #include "linear.h"
+#include <type_traits>
 
 namespace kavg {
 
@@ -80,15 +80,15 @@ template <class E, int TX, bool TURNED, int NT> struct Loader {
 #pragma unroll
         for (int i = 0; i < N; ++i) at[i] += step;
     }
-    // straight into LDS; left: elements of the contraction from this slice on.  What lies past it is loaded from before its end, and zeroed by
-    // fix() once it has landed.
-    __device__ __forceinline__ void load(char* tile, int left) const {
+    // Straight into LDS; left: elements of the contraction from this slice on.  What lies past it (not WHOLE) is loaded from before its end, and
+    // zeroed by fix() once it has landed.
+    template <bool WHOLE> __device__ __forceinline__ void load(char* tile, int left) const {
         typedef __attribute__((address_space(3))) void* lds_p;
         typedef const __attribute__((address_space(1))) void* glb_p;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const E* p = at[i];
-            if (left < BK) {
+            if (!WHOLE) {
                 const int over = TURNED ? k[i] - left + 1 : k[i] + V - left;
                 if (over > 0) p -= TURNED ? over * stride : (int64_t)over;
             }
@@ -163,22 +163,21 @@ __device__ __forceinline__ void add_up(const f32x4& f, float (&s)[4]) {
     for (int i = 0; i < 4; ++i) s[i] += f[i];
 }
 
-template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT> struct ProductTile {
-    static constexpr int NT = 64 * WR * WC * WK, MR = TR / (32 * WR), MC = TC / (32 * WC);
+template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT> struct ProductTile {
+    static constexpr int NT = 64 * WR * WC, MR = TR / (32 * WR), MC = TC / (32 * WC);
     static constexpr int BUFFER = (TR + TC) * SLICE_BYTES;
-    static constexpr int JOIN = WK > 1 ? WR * WC * MR * MC * 16 * 64 * 4 : 0;            // a k group's sums
-    static constexpr int LDS = 2 * BUFFER > JOIN ? 2 * BUFFER : JOIN;
+    static constexpr int PITCH = MC * 32 + 4, STAGE = WR * WC * 32 * PITCH * 4;            // rows of results on their way out
+    static constexpr int LDS = 2 * BUFFER > STAGE ? 2 * BUFFER : STAGE;
 };
 
-template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT>
-__global__ void __launch_bounds__(64 * WR * WC * WK) product_kernel(ProductArgs a) {
-    typedef ProductTile<E, TR, TC, WR, WC, WK, RT, CT, DIRECT> P;
+template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT>
+__global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
+    typedef ProductTile<E, TR, TC, WR, WC, RT, CT, DIRECT> P;
     typedef typename Kind<E>::chunk chunk;
-    constexpr int NT = P::NT, MR = P::MR, MC = P::MC, BK = Kind<E>::BK, SLABS = 4 / WK;
-    static_assert(!RT || WK == 1, "sums of an operand are those of one group of wavefronts");
+    constexpr int NT = P::NT, MR = P::MR, MC = P::MC, BK = Kind<E>::BK, SLABS = 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wk = wave / (WR * WC), wr = wave % (WR * WC) / WC, wc = wave % WC;
+    const int wr = wave / WC, wc = wave % WC;
 
     // Workgroups go round the 8 XCDs in launch order; each XCD takes a run of tiles, which share operands in its L2, eight rows of tiles at a time.
     const uint32_t number = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
@@ -208,54 +207,99 @@ __global__ void __launch_bounds__(64 * WR * WC * WK) product_kernel(ProductArgs 
     float sums[RT ? MS : 1][4] = {};
     const bool sum_r = RT && a.side == 1 && tile_c == 0 && wc == 0, sum_c = RT && a.side == 2 && tile_r == 0 && wr == 0;
 
-    auto multiply_slice = [&](const char* buffer) {
-        const char *rt = buffer, *ct = buffer + TR * SLICE_BYTES;
-        chunk rf[2][MR], cf[2][MC];
-        auto take = [&](int to, int s) {
-            const int kk = wk * SLABS + s;
+    // Fragments of a slab are asked for while the one before it is multiplied: two sets of registers.
+    chunk rf[2][MR], cf[2][MC];
+    auto take = [&](int to, const char* buffer, int slab) {
 #pragma unroll
-            for (int j = 0; j < MC; ++j) cf[to][j] = fragment<E, TC, CT>(ct, (wc * MC + j) * 32, kk, lane);
+        for (int j = 0; j < MC; ++j) cf[to][j] = fragment<E, TC, CT>(buffer + TR * SLICE_BYTES, (wc * MC + j) * 32, slab, lane);
 #pragma unroll
-            for (int i = 0; i < MR; ++i) rf[to][i] = fragment<E, TR, RT>(rt, (wr * MR + i) * 32, kk, lane);
-        };
-        take(0, 0);
+        for (int i = 0; i < MR; ++i) rf[to][i] = fragment<E, TR, RT>(buffer, (wr * MR + i) * 32, slab, lane);
+    };
+    auto multiply_slab = [&](int from) {
 #pragma unroll
-        for (int s = 0; s < SLABS; ++s) {
-            if (s + 1 < SLABS) take((s + 1) & 1, s + 1);
+        for (int i = 0; i < MR; ++i)
 #pragma unroll
-            for (int i = 0; i < MR; ++i)
+            for (int j = 0; j < MC; ++j) acc[i][j] = multiply(cf[from][j], rf[from][i], acc[i][j]);
+        if (sum_r) {
 #pragma unroll
-                for (int j = 0; j < MC; ++j) acc[i][j] = multiply(cf[s & 1][j], rf[s & 1][i], acc[i][j]);
-            if (sum_r) {
+            for (int i = 0; i < MR; ++i) add_up(rf[from][i], sums[RT ? i : 0]);
+        }
+        if (sum_c) {
 #pragma unroll
-                for (int i = 0; i < MR; ++i) add_up(rf[s & 1][i], sums[RT ? i : 0]);
-            }
-            if (sum_c) {
+            for (int j = 0; j < MC; ++j) add_up(cf[from][j], sums[RT ? j : 0]);
+        }
+    };
+
+    // The order for the scheduler (which would fold the two sets into one): an LDS read or two behind every product, and loads of a slice as many.
+    auto interleave = [&](auto loads) {
+        constexpr int READS = MC * (!CT ? 1 : sizeof(E) == 2 ? 2 : 4) + MR * (!RT ? 1 : sizeof(E) == 2 ? 2 : 4), PRODUCTS = MR * MC * (sizeof(E) == 2 ? 1 : 4);
+        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
 #pragma unroll
-                for (int j = 0; j < MC; ++j) add_up(cf[s & 1][j], sums[RT ? j : 0]);
-            }
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            if (loads.value && i < loads.value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         }
     };
 
     if constexpr (DIRECT) {
-        rl.load(lds, left);
-        cl.load(lds + TR * SLICE_BYTES, left);
-        for (int s = 0; s < slices; ++s, left -= BK) {
-            char* now = lds + (s & 1) * P::BUFFER;
-            char* next = lds + (~s & 1) * P::BUFFER;
-            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0): this wavefront's part of the slice has landed
-            if (left < BK) {
-                rl.fix(now, left, tid);
-                cl.fix(now + TR * SLICE_BYTES, left, tid);
+        // The barrier of a slice lies before its last slab is multiplied: by then every wavefront has that slab in registers, so that the buffer takes
+        // the slice after the next, and the next slice's first slab is read under those products.
+        constexpr int LOADS = rl.N + cl.N;
+        auto load = [&](auto whole, char* to, int rest) {
+            rl.template load<whole.value>(to, rest);
+            cl.template load<whole.value>(to + TR * SLICE_BYTES, rest);
+            rl.advance();
+            cl.advance();
+        };
+        auto mend = [&](char* slice, int rest) {
+            if (rest < BK) {
+                rl.fix(slice, rest, tid);
+                cl.fix(slice + TR * SLICE_BYTES, rest, tid);
             }
-            __syncthreads();                                 // everyone's has, and the other buffer is no longer read
+        };
+        constexpr std::true_type whole = {};
+        constexpr std::false_type cut = {};
+        load(cut, lds, left);
+        if (slices > 1) {
+            load(cut, lds + P::BUFFER, left - BK);
+            __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 0x0F70);      // vmcnt(LOADS)
+        } else __builtin_amdgcn_s_waitcnt(0x0F70);
+        mend(lds, left);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                 // (no fence, which would wait for the second slice)
+        take(0, lds, 0);
+        char *now = lds, *next = lds + P::BUFFER;
+        auto first_slabs = [&] {
+#pragma unroll
+            for (int slab = 0; slab + 1 < SLABS; ++slab) {
+                take(~slab & 1, now, slab + 1);
+                multiply_slab(slab & 1);
+                interleave(std::integral_constant<int, 0>());
+            }
+        };
+        auto turn = [&] { char* t = now; now = next; next = t; };
+        int s = 0;
+        for (const int full = min(left / BK, slices); s + 2 < full; ++s, left -= BK) {   // the slices that this loop loads are whole ones
+            first_slabs();
+            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0): this wavefront's part of the next slice has landed
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            load(whole, now, left);
+            take(0, next, 0);
+            multiply_slab((SLABS - 1) & 1);
+            interleave(std::integral_constant<int, LOADS>());
+            turn();
+        }
+        for (; s < slices; ++s, left -= BK) {
+            first_slabs();
             if (s + 1 < slices) {
-                rl.advance();
-                cl.advance();
-                rl.load(next, left - BK);
-                cl.load(next + TR * SLICE_BYTES, left - BK);
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                mend(next, left - BK);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if (s + 2 < slices) load(cut, now, left - 2 * BK);
+                take(0, next, 0);
             }
-            multiply_slice(now);
+            multiply_slab((SLABS - 1) & 1);
+            turn();
         }
     } else {
         u32x4 rr[rl.N], cr[cl.N];
@@ -272,33 +316,13 @@ __global__ void __launch_bounds__(64 * WR * WC * WK) product_kernel(ProductArgs 
                 rl.fetch(rr, left - BK, a.nR);
                 cl.fetch(cr, left - BK, a.nC);
             }
-            multiply_slice(now);
-        }
-    }
-
-    if constexpr (WK > 1) {                                  // the k groups' sums, in order
-        float* join = (float*)lds + (wave % (WR * WC)) * MR * MC * 16 * 64 + lane;
-        for (int g = 1; g < WK; ++g) {
-            __syncthreads();
-            if (wk == g) {
+            take(0, now, 0);
 #pragma unroll
-                for (int i = 0; i < MR; ++i)
-#pragma unroll
-                    for (int j = 0; j < MC; ++j)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) join[((i * MC + j) * 16 + e) * 64] = acc[i][j][e];
-            }
-            __syncthreads();
-            if (wk == 0) {
-#pragma unroll
-                for (int i = 0; i < MR; ++i)
-#pragma unroll
-                    for (int j = 0; j < MC; ++j)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[i][j][e] += join[((i * MC + j) * 16 + e) * 64];
+            for (int slab = 0; slab < SLABS; ++slab) {
+                if (slab + 1 < SLABS) take(~slab & 1, now, slab + 1);
+                multiply_slab(slab & 1);
             }
         }
-        if (wk) return;
     }
 
     if (RT && (sum_r || sum_c)) {
@@ -313,42 +337,47 @@ __global__ void __launch_bounds__(64 * WR * WC * WK) product_kernel(ProductArgs 
             if (lane < 32 && x < n) to[x] = sum;
         }
     }
+    // Results leave through LDS, by wavefront: 32 rows of its columns at a time, so that the lanes of a row write whole lines (and the code is there once
+    // for eight columns of a lane, not for every register).
+    constexpr int WTC = MC * 32, PITCH = P::PITCH, ROW_LANES = WTC / 8, ROWS = 64 / ROW_LANES, TURNS = 32 / ROWS;
+    __syncthreads();
+    float* stage = (float*)lds + wave * 32 * PITCH;
+    const int c = c0 + wc * WTC + (lane % ROW_LANES) * 8, down = lane / ROW_LANES;
+    auto emit = [&](const auto& finish) {
 #pragma unroll
-    for (int i = 0; i < MR; ++i) {
-        const int r = r0 + (wr * MR + i) * 32 + (lane & 31);
+        for (int i = 0; i < MR; ++i) {
 #pragma unroll
-        for (int j = 0; j < MC; ++j) {
+            for (int j = 0; j < MC; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; q += 2) {
-                // columns 8q + 4 half .. of two groups of eight: the lower half of the wavefront takes the first, the upper half the second
-                float v[8];
+                for (int q = 0; q < 4; ++q) *(f32x4*)(stage + (lane & 31) * PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = (f32x4){acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+            finish(r0 + (wr * MR + i) * 32 + down, ROWS, a.nR, [&](int u, float (&v)[8]) {
+                const float* from = stage + (down + u * ROWS) * PITCH + (lane % ROW_LANES) * 8;
+                const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float lower = acc[i][j][q * 4 + e], upper = acc[i][j][q * 4 + 4 + e];      // (__builtin_bit_cast of a vector's element takes its first)
-                    const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lower), __builtin_bit_cast(uint32_t, upper), false, false);
-                    v[e] = __builtin_bit_cast(float, (uint32_t)p[0]);
-                    v[4 + e] = __builtin_bit_cast(float, (uint32_t)p[1]);
-                }
-                const int c = c0 + (wc * MC + j) * 32 + (q + (lane >> 5)) * 8, n = a.nC - c;
-                if (r >= a.nR || n <= 0) continue;
-                if (a.partial) store_some<float, 8>(a.partial + split * a.partial_split + (set * a.nR + r) * a.pitch + c, 8, v);
-                else if constexpr (RT) store_some<float, 8>((float*)a.finish.out + set * a.finish.out_set + r * a.finish.out_row + c, n, v);
-                else finish_values<E, E, 8>(a.finish, set, r, c, n, v);
-            }
+                for (int k = 0; k < 4; ++k) { v[k] = lo[k]; v[4 + k] = hi[k]; }
+            });
         }
-    }
+    };
+    typedef typename std::conditional<RT, float, E>::type O;
+    if (a.partial) {
+        Finish parts = {};
+        parts.floor = -INFINITY;
+        parts.out = a.partial + split * a.partial_split; parts.out_set = (int64_t)a.nR * a.pitch; parts.out_row = a.pitch;
+        emit(Finisher<E, float, TURNS, false>(parts, set, c, a.nC > c ? 8 : 0));          // (rows are padded to whole eights)
+    } else if (c0 + TC <= a.nC) emit(Finisher<E, O, TURNS, true>(a.finish, set, c, 8));
+    else emit(Finisher<E, O, TURNS, false>(a.finish, set, c, a.nC - c));
 }
 
-// Tiles: rows, columns, wavefronts along rows, columns and the contraction.  The first two are those of large results, the third of small
+// Tiles: rows, columns, wavefronts along rows and columns.  The first two are those of large results, the third of small
 // ones, the others of results that are narrow one way.
-#define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4, 1) TILE(1, 128, 128, 2, 2, 1) TILE(2, 64, 64, 2, 2, 1) TILE(3, 128, 32, 4, 1, 1) TILE(4, 32, 128, 1, 4, 1)
+#define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4) TILE(1, 128, 128, 2, 2) TILE(2, 64, 64, 2, 2) TILE(3, 128, 32, 4, 1) TILE(4, 32, 128, 1, 4)
 enum { TILE_LARGE = 0, TILE_MIDDLE = 1, TILE_SMALL = 2, TILE_TALL = 3, TILE_WIDE = 4, TILE_KINDS = 5 };
 
 // DIRECT wants operands whose chunks are aligned and whole; the largest tile is for such operands only
-template <class E, int TR, int TC, int WR, int WC, int WK, bool RT, bool CT, bool DIRECT>
+template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT>
 hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
-    typedef ProductTile<E, TR, TC, WR, WC, WK, RT, CT, DIRECT> P;
-    const auto kernel = product_kernel<E, TR, TC, WR, WC, WK, RT, CT, DIRECT>;
+    typedef ProductTile<E, TR, TC, WR, WC, RT, CT, DIRECT> P;
+    const auto kernel = product_kernel<E, TR, TC, WR, WC, RT, CT, DIRECT>;
     if (P::LDS > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
         if (e != hipSuccess) return e;
@@ -358,10 +387,10 @@ hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
 }
 
 template <class E, bool RT, bool CT> hipError_t start_kind(int tile, bool direct, const ProductArgs& a, hipStream_t st) {
-#define TILE(NUMBER, TR, TC, WR, WC, WK) \
+#define TILE(NUMBER, TR, TC, WR, WC) \
     case NUMBER: \
-        if (direct) return start_tile<E, TR, TC, WR, WC, WK, RT, CT, true>(a, st); \
-        if constexpr (TR * TC < 256 * 256) return start_tile<E, TR, TC, WR, WC, WK, RT, CT, false>(a, st); \
+        if (direct) return start_tile<E, TR, TC, WR, WC, RT, CT, true>(a, st); \
+        if constexpr (TR * TC < 256 * 256) return start_tile<E, TR, TC, WR, WC, RT, CT, false>(a, st); \
         break;
     switch (tile) { KAVG_TILES(TILE) }
 #undef TILE
