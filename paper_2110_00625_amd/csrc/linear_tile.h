@@ -233,12 +233,13 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
     // The order for the scheduler (which would fold the two sets into one): an LDS read or two behind every product, and loads of a slice as many.
     auto interleave = [&](auto loads) {
         constexpr int READS = MC * (!CT ? 1 : sizeof(E) == 2 ? 2 : 4) + MR * (!RT ? 1 : sizeof(E) == 2 ? 2 : 4), PRODUCTS = MR * MC * (sizeof(E) == 2 ? 1 : 4);
-        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+        constexpr int LOADS_EACH = 2;
+        constexpr int EACH = READS <= 2 * PRODUCTS ? 2 : (READS + PRODUCTS - 1) / PRODUCTS;
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             if (i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
-            if (loads.value && i < loads.value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            else if (loads.value) __builtin_amdgcn_sched_group_barrier(0x020, LOADS_EACH, 0);
         }
     };
 
@@ -281,10 +282,14 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         int s = 0;
         for (const int full = min(left / BK, slices); s + 2 < full; ++s, left -= BK) {   // the slices that this loop loads are whole ones
             first_slabs();
-            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0): this wavefront's part of the next slice has landed
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            load(whole, now, left);
+            __builtin_amdgcn_sched_barrier(0);               // (no product of theirs behind the barrier, where it would wait for the others)
+            // this wavefront's part of the next slice has landed, its reads of this one are done (waits that the compiler counts: it would add its own)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0070);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
             take(0, next, 0);
+            load(whole, now, left);
             multiply_slab((SLABS - 1) & 1);
             interleave(std::integral_constant<int, LOADS>());
             turn();
