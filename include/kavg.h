@@ -413,7 +413,7 @@ int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t d
  * z, so that dx is the gradient of that z, which that layer's backward call wants (KAVG_ACT_NONE: dx is the gradient of x; pre NULL).  ReLU's
  * slope at 0 is 0; for ReLU, pre may also be x itself.
  * Order of a call's sums, and so its bits, depend on the sizes, strides and alignment alone.
- * Limits: sizes at most 2^31 - 2^16, fewer than 2^42 elements in any matrix, strides at most 2^46 over the size of their dimension
+ * Limits: at most 2^31 - 2^16 rows, 2^27 inputs and outputs, fewer than 2^42 elements in any matrix, strides at most 2^46 over the size of their dimension
  * (the stride of a dimension of one says nothing); inputs, outputs >= 1; sets or rows may be 0 (dW, db are zeros then). */
 typedef struct {
     int dtype, activation;

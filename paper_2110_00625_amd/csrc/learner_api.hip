@@ -9,7 +9,8 @@ namespace {
 
 using namespace kavg;
 
-constexpr int64_t MOST_SIZE = INT32_MAX - 65535;             // of rows, inputs, outputs (tiles reach past them in 32 bits)
+constexpr int64_t MOST_ROWS = INT32_MAX - 65535;             // (tiles reach past them in 32 bits)
+constexpr int64_t MOST_COLUMNS = 1 << 27;                    // inputs, outputs: 2^22 tiles of 32, those of a launch
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 42, MOST_SPAN = (int64_t)1 << 46;
 
 int64_t at_least_one(int64_t n) { return n > 1 ? n : 1; }
@@ -22,7 +23,7 @@ bool stride_ok(int64_t stride, int64_t n, int64_t least) { return n < 2 || (stri
 
 bool product_ok(const kavg_product* p) {
     if (!p || (p->dtype != KAVG_FP32 && p->dtype != KAVG_BF16) || p->activation < KAVG_ACT_NONE || p->activation > KAVG_ACT_SILU) return false;
-    if (p->sets < 0 || p->rows < 0 || p->inputs < 1 || p->outputs < 1 || p->rows > MOST_SIZE || p->inputs > MOST_SIZE || p->outputs > MOST_SIZE) return false;
+    if (p->sets < 0 || p->rows < 0 || p->inputs < 1 || p->outputs < 1 || p->rows > MOST_ROWS || p->inputs > MOST_COLUMNS || p->outputs > MOST_COLUMNS) return false;
     return p->sets < (int64_t)1 << 31 && product_below(p->sets, p->rows, std::max(p->inputs, p->outputs), MOST_ELEMENTS) && product_below(p->sets, p->inputs, p->outputs, MOST_ELEMENTS);
 }
 bool empty(const kavg_product* p) { return !p->sets || !p->rows; }

@@ -25,6 +25,9 @@ constexpr Size tile_size(int tile) {
     return {0, 0};
 }
 
+// elements of a slice of the contraction
+int slice_of(int dtype) { return dtype == KAVG_BF16 ? Kind<__bf16>::BK : Kind<float>::BK; }
+
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int64_t tiles_of(int tile, int64_t sets, int nR, int nC) {
@@ -32,42 +35,52 @@ int64_t tiles_of(int tile, int64_t sets, int nR, int nC) {
     return sets * up(nR, s.r) * std::max<int64_t>(1, up(nC, s.c));
 }
 
-// A lane adds up the parts of eight columns of a row, in order, and finishes them; the sums follow after the last row.
-template <class E>
-__global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, uint32_t per_row, Divisor by_row) {
-    const uint64_t first = (uint64_t)blockIdx.x * T;
-    if (first < packs) {
-        // (a row has fewer than 2^28 packs, so that what is divided stays below 2^30)
-        const uint64_t row0 = first / per_row;
-        const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, down = divide(at, by_row);
-        if (first + threadIdx.x >= packs) return;
-        const uint64_t row = row0 + down;
-        const int c = (int)(at - down * per_row) * 8;
-        const float* p = a.partial + row * a.pitch + c;
-        float v[8] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            float t[8];
-            load_some<float, 8>(p + s * a.partial_split, 8, t);
+// the sum of n parts, in order, eight of them asked for at a time
+template <int V> __device__ __forceinline__ void add_parts(const float* p, int64_t apart, int n, float (&v)[V]) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += t[k];
-        }
-        const int64_t set = (int64_t)(row / (uint64_t)a.nR), r = (int64_t)(row - (uint64_t)set * a.nR);
-        const Finisher<E, E, 1, false> finish(a.finish, set, c, a.nC - c);
-        finish(r, 1, a.nR, [&](int, float (&to)[8]) {
+    for (int k = 0; k < V; ++k) v[k] = 0.f;
+    for (int s = 0; s < n; s += 8) {
+        float t[8][V];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) to[k] = v[k];
-        });
+        for (int u = 0; u < 8; ++u) load_some<float, V>(p + min(s + u, n - 1) * apart, V, t[u]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s + u < n) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] += t[u][k];
+            }
     }
 }
 
-struct SumsArgs { const float* parts; float* sums; int64_t split, from_set, to_set; int n, splits; int64_t sets; };
+// Sums of an operand of a weight gradient: [split][set][x] and where they go.
+struct SumsArgs { const float* parts; float* sums; int64_t split, from_set, to_set, n, sets; };
 
-__global__ void __launch_bounds__(T) join_sums_kernel(SumsArgs a) {
-    const int64_t i = (int64_t)blockIdx.x * T + threadIdx.x, set = i / a.n, x = i - set * a.n;
-    if (set >= a.sets) return;
-    float v = 0.f;
-    for (int s = 0; s < a.splits; ++s) v += a.parts[s * a.split + set * a.from_set + x];
-    a.sums[set * a.to_set + x] = v;
+// A lane adds up the parts of eight columns of a row, in order, and finishes them; the workgroups behind the last row's add up the operand's sums.
+template <class E>
+__global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, uint32_t groups, uint32_t per_row, Divisor by_row, SumsArgs sums) {
+    if (blockIdx.x >= groups) {
+        const int64_t i = (int64_t)(blockIdx.x - groups) * T + threadIdx.x, set = i / sums.n, x = i - set * sums.n;
+        if (set >= sums.sets) return;
+        float v[1];
+        add_parts<1>(sums.parts + set * sums.from_set + x, sums.split, a.splits, v);
+        sums.sums[set * sums.to_set + x] = v[0];
+        return;
+    }
+    const uint64_t first = (uint64_t)blockIdx.x * T;
+    // (a row has fewer than 2^28 packs, so that what is divided stays below 2^30)
+    const uint64_t row0 = first / per_row;
+    const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, down = divide(at, by_row);
+    if (first + threadIdx.x >= packs) return;
+    const uint64_t row = row0 + down;
+    const int c = (int)(at - down * per_row) * 8;
+    float v[8];
+    add_parts<8>(a.partial + row * a.pitch + c, a.partial_split, a.splits, v);
+    const int64_t set = (int64_t)(row / (uint64_t)a.nR), r = (int64_t)(row - (uint64_t)set * a.nR);
+    const Finisher<E, E, 1, false> finish(a.finish, set, c, a.nC - c);
+    finish(r, 1, a.nR, [&](int, float (&to)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) to[k] = v[k];
+    });
 }
 
 bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem) {
@@ -77,24 +90,38 @@ bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem)
 
 }  // namespace
 
+// What a tile of each kind costs, in microseconds: a slice of 128 bytes where a compute unit has one tile of them, and per tile where it has more;
+// filling and emptying the pipeline.  (256 compute units; 8192x4096x4096 in bf16 by large tiles 234 us, middle 260, small 376, four products of 1000^3 by
+// large, split in two, 33, middle 16, small 20, 2048x1024x1024 by middle 12, small 9; 4096^3 in fp32 by large 1032, middle 1004, small 1106.)
+struct Cost { float alone, shared, ends; };
+static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.26f, 0.18f, 0.5f}, {0.26f, 0.18f, 0.5f}};
+static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.5f}, {0.54f, 0.54f, 0.5f}};
+
 Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient) {
-    const int bk = dtype == KAVG_BF16 ? Kind<__bf16>::BK : Kind<float>::BK;
-    const int64_t slices = up(nK, bk);
+    const int64_t slices = up(nK, slice_of(dtype));
     Plan p = {};
     p.pitch = (int)up(nC, 8) * 8;
-    if (nC <= 32) p.tile = TILE_TALL;
-    else if (nR <= 32) p.tile = TILE_WIDE;
-    else p.tile = tiles_of(TILE_LARGE, sets, nR, nC) >= CUS ? TILE_LARGE : tiles_of(TILE_MIDDLE, sets, nR, nC) >= CUS ? TILE_MIDDLE : TILE_SMALL;
-    const int64_t tiles = tiles_of(p.tile, sets, nR, nC);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slices / 8, 2 * CUS / tiles));
-    p.splits = slices ? (int)up(slices, up(slices, p.splits)) : 1;        // (none without a slice)
+    p.splits = 1;
+    float least = INFINITY;
+    for (int tile = 0; tile < TILE_KINDS; ++tile) {
+        const Cost& c = (dtype == KAVG_BF16 ? BF16_COST : F32_COST)[tile];
+        const int64_t tiles = tiles_of(tile, sets, nR, nC);
+        for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (splits > 1 && (2 * splits > slices || tiles * splits > 8 * CUS)) break;
+            const int64_t each = up(slices, splits), m = up(tiles * up(slices, std::max<int64_t>(each, 1)), CUS);
+            float cost = m * c.ends + each * std::max(c.alone, c.shared * m);
+            // the launch that joins the parts, which are written and read
+            if (splits > 1) cost += 4.f + 0.1f * splits + (float)sets * nR * p.pitch * splits * 8 / 5.5e6f;
+            if (cost < least) { least = cost; p.tile = tile; p.splits = (int)std::max<int64_t>(1, up(slices, std::max<int64_t>(each, 1))); }
+        }
+    }
     if (p.splits > 1) p.bytes = (size_t)p.splits * sets * ((size_t)nR * p.pitch + (weight_gradient ? std::max(nR, nC) : 0)) * sizeof(float);
     return p;
 }
 
 hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes, hipStream_t st) {
     const bool bf16 = call.dtype == KAVG_BF16;
-    const int elem = bf16 ? 2 : 4, bk = bf16 ? Kind<__bf16>::BK : Kind<float>::BK;
+    const int elem = bf16 ? 2 : 4;
     const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
     if (plan.splits > 1) {
         if (bytes < plan.bytes) return hipErrorOutOfMemory;
@@ -104,13 +131,12 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
                         aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
     const int tile = plan.tile == TILE_LARGE && !direct ? TILE_MIDDLE : plan.tile;
     const Size size = tile_size(tile);
-    const int64_t slices = up(call.nK, bk);
 
     ProductArgs a = {};
     a.nC = call.nC; a.nK = call.nK;
     a.tiles_c = (int)std::max<int64_t>(1, up(call.nC, size.c));
     a.splits = plan.splits;
-    a.per_split = (int)up(slices, plan.splits);
+    a.per_split = (int)up(up(call.nK, slice_of(call.dtype)), plan.splits);
     a.finish = call.finish;
     a.side = call.side;
     a.sums = call.sums; a.sums_set = call.sums_set;
@@ -142,9 +168,9 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
                 a.pitch = plan.pitch;
                 a.partial_split = sets * (int64_t)a.nR * a.pitch;
                 if (call.side) {
-                    sums = {a.partial + plan.splits * a.partial_split, a.sums, 0, call.side == 1 ? a.nR : a.nC, call.sums_set, call.side == 1 ? a.nR : a.nC, plan.splits, sets};
-                    sums.split = sets * sums.n;
-                    a.sums = (float*)sums.parts; a.sums_set = sums.from_set; a.sums_split = sums.split;
+                    const int64_t n = call.side == 1 ? a.nR : a.nC;
+                    sums = {a.partial + plan.splits * a.partial_split, a.sums, sets * n, n, call.sums_set, n, sets};
+                    a.sums = (float*)sums.parts; a.sums_set = n; a.sums_split = sums.split;
                 }
             }
             const auto start = call.r_turned ? (bf16 ? start_bf16_gradient : start_f32_gradient)
@@ -154,12 +180,10 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
             if (plan.splits > 1) {
                 const uint32_t per_row = (uint32_t)plan.pitch / 8;
                 const uint64_t packs = (uint64_t)sets * a.nR * per_row;
-                if (packs) {
-                    const dim3 grid((unsigned)up(packs, T)), lanes(T);
-                    if (bf16 && !call.r_turned) join_kernel<__bf16><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
-                    else join_kernel<float><<<grid, lanes, 0, st>>>(a, packs, per_row, divisor(per_row));
-                }
-                if (call.side) join_sums_kernel<<<dim3((unsigned)up(sets * sums.n, T)), dim3(T), 0, st>>>(sums);
+                const uint32_t groups = (uint32_t)up(packs, T), more = (uint32_t)up(sums.n * sums.sets, T);
+                const Divisor by_row = divisor(std::max<uint32_t>(per_row, 1));
+                if (bf16 && !call.r_turned) join_kernel<__bf16><<<dim3(groups + more), dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
+                else join_kernel<float><<<dim3(groups + more), dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
                 e = hipGetLastError();
                 if (e != hipSuccess) return e;
             }

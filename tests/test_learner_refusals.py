@@ -8,7 +8,7 @@ from paper_2110_00625_amd import kavg
 from tests.test_layers_refusals import AT, lib  # noqa: F401  (lib: the loaded library)
 
 E, OK = kavg.KAVG_EINVAL, kavg.KAVG_OK
-MOST = (1 << 31) - (1 << 16)
+MOST, COLUMNS = (1 << 31) - (1 << 16), 1 << 27
 AWAY = 1 << 20                               # another address that no refused call reaches
 
 
@@ -34,7 +34,7 @@ def backward(lib, p=None, dz=rows(), x=rows(3 * AT), w=weights(), pre=None, dx=r
 
 @pytest.mark.parametrize("kw", [
     dict(dtype=2), dict(dtype=-1), dict(activation=3), dict(activation=-1), dict(sets=-1), dict(rows=-1), dict(inputs=0), dict(outputs=0), dict(inputs=-8),
-    dict(rows=MOST + 1), dict(inputs=MOST + 1), dict(outputs=MOST + 1), dict(sets=1 << 31), dict(sets=1 << 62), dict(sets=1, rows=1 << 30, inputs=1 << 12),
+    dict(rows=MOST + 1), dict(inputs=COLUMNS + 1), dict(outputs=COLUMNS + 1), dict(sets=1 << 31), dict(sets=1 << 62), dict(sets=1, rows=1 << 30, inputs=1 << 12),
     dict(sets=1 << 12, rows=1, inputs=1 << 15, outputs=1 << 15), dict(sets=0, rows=1 << 30, outputs=1 << 12),
 ])
 def test_descriptions_that_say_nothing(lib, kw):  # noqa: F811
@@ -46,8 +46,8 @@ def test_descriptions_that_say_nothing(lib, kw):  # noqa: F811
 def test_workspaces(lib):  # noqa: F811
     size = ctypes.c_size_t(0)
     assert lib.kavg_linear_workspace(product(), 0, None) == E and lib.kavg_linear_workspace(None, 0, ctypes.byref(size)) == E
-    for kw in (dict(sets=0), dict(rows=0), dict(dtype=1, sets=1, rows=MOST, inputs=8, outputs=8), dict(sets=1, rows=8, inputs=MOST, outputs=8),
-               dict(sets=1, rows=1, inputs=1, outputs=MOST), dict(sets=(1 << 31) - 1, rows=1, inputs=8, outputs=1)):
+    for kw in (dict(sets=0), dict(rows=0), dict(dtype=1, sets=1, rows=MOST, inputs=8, outputs=8), dict(sets=1, rows=8, inputs=COLUMNS, outputs=8),
+               dict(sets=1, rows=1, inputs=1, outputs=COLUMNS), dict(sets=(1 << 31) - 1, rows=1, inputs=8, outputs=1)):
         for back in (0, 1):
             assert lib.kavg_linear_workspace(product(**kw), back, ctypes.byref(size)) == OK and size.value < 1 << 40, kw
     # one row of results from a long contraction: split, and refused before a launch without the block
