@@ -4,6 +4,7 @@
 
 namespace kavg {
 
+hipError_t start_rows(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st);
 hipError_t start_bf16_plain(int tile, bool direct, const ProductArgs& a, hipStream_t st);
 hipError_t start_bf16_turned(int tile, bool direct, const ProductArgs& a, hipStream_t st);
 hipError_t start_bf16_gradient(int tile, bool direct, const ProductArgs& a, hipStream_t st);
@@ -15,6 +16,7 @@ namespace {
 
 constexpr int CUS = 256;
 constexpr int T = 256;
+constexpr int MOST_ROWS = 16;                    // that the kernel of few rows takes
 constexpr int64_t MOST_TILES = 1 << 22;          // of a launch (fewer than 2^32 lanes)
 
 struct Size { int r, c; };
@@ -122,13 +124,20 @@ Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_g
 hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes, hipStream_t st) {
     const bool bf16 = call.dtype == KAVG_BF16;
     const int elem = bf16 ? 2 : 4;
+    const bool direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
+                        aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
+    if (direct && call.nR <= MOST_ROWS && !call.r_turned && !call.c_turned && call.sets * up(call.nC, 16) <= MOST_TILES) {
+        ProductArgs a = {};
+        a.R = call.R; a.C = call.C;
+        a.nR = call.nR; a.nC = call.nC; a.nK = call.nK;
+        a.finish = call.finish;
+        return start_rows(call.dtype, a, call.sets, st);
+    }
     const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
     if (plan.splits > 1) {
         if (bytes < plan.bytes) return hipErrorOutOfMemory;
         if (!workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;
     }
-    const bool direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
-                        aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
     const int tile = plan.tile == TILE_LARGE && !direct ? TILE_MIDDLE : plan.tile;
     const Size size = tile_size(tile);
 
