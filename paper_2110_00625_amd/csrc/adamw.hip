@@ -15,6 +15,7 @@ namespace kavg {
 namespace {
 
 constexpr int T = 256, BLOCK = 256, TURNS = 2, PIECE = T * 4 * TURNS;
+constexpr double CACHE = 256e6;                  // bytes behind the L2: tensors of more are gone by the next step
 constexpr int MOST_TENSORS = 32;                 // of a launch: its arguments stay below four kilobytes
 
 struct Table {
@@ -38,10 +39,12 @@ __host__ __device__ inline void at_step(AdamwRule& r, uint64_t t) {
 
 struct Four { float v[4]; };
 
-template <class E> __device__ __forceinline__ Four load_four(const E* p, int n) {
+// four values of which n are there; STREAM: of tensors that no cache holds until the next step
+template <bool STREAM, class E> __device__ __forceinline__ Four load_four(const E* p, int n) {
     Four f;
     if (n >= 4) {
-        const auto v = pack_load<E, 4>(p);
+        const auto at = (const typename Pack<E, 4>::loose*)p;
+        const typename Pack<E, 4>::type v = STREAM ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
         for (int k = 0; k < 4; ++k) f.v[k] = to_float(v[k]);
     } else {
@@ -50,26 +53,33 @@ template <class E> __device__ __forceinline__ Four load_four(const E* p, int n) 
     }
     return f;
 }
-__device__ __forceinline__ void store_four(float* p, const Four& f, int n) {
+template <bool STREAM> __device__ __forceinline__ void store_four(float* p, const Four& f, int n) {
     if (n >= 4) {
-        Pack<float, 4>::type v = {f.v[0], f.v[1], f.v[2], f.v[3]};
-        pack_store<float, 4>(p, v);
+        const Pack<float, 4>::type v = {f.v[0], f.v[1], f.v[2], f.v[3]};
+        const auto at = (Pack<float, 4>::loose*)p;
+        if (STREAM) __builtin_nontemporal_store(v, at);
+        else *at = v;
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) if (k < n) p[k] = f.v[k];
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n) {
-    typedef uint32_t loose __attribute__((aligned(1)));
-    if (n >= 4) return *(const loose*)p;
+typedef uint32_t loose_word __attribute__((aligned(1)));
+template <bool STREAM> __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n) {
+    const auto at = (const loose_word*)p;
+    if (n >= 4) return STREAM ? __builtin_nontemporal_load(at) : *at;
     uint32_t w = 0;
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) w |= (uint32_t)p[k] << (8 * k);
     return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t w, int n) {
-    typedef uint32_t loose __attribute__((aligned(1)));
-    if (n >= 4) { *(loose*)p = w; return; }
+template <bool STREAM> __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t w, int n) {
+    const auto at = (loose_word*)p;
+    if (n >= 4) {
+        if (STREAM) __builtin_nontemporal_store(w, at);
+        else *at = w;
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < 3; ++k) if (k < n) p[k] = (uint8_t)(w >> (8 * k));
 }
@@ -89,62 +99,193 @@ __device__ __forceinline__ uint32_t scale_field(uint32_t most) {
 __device__ __forceinline__ float power(uint32_t field) { return __builtin_bit_cast(float, field << 23); }
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < INFINITY; }
 
+// bits of the largest of non-negative values over the wavefront, in all 64 lanes' scalar: NaN above infinity above the others
+template <int CTRL> __device__ __forceinline__ uint32_t max_of_move(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true)); }
 __device__ __forceinline__ uint32_t largest(const Four& f) {
-    float most = 0.f;
+    uint32_t x = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) most = fmaxf(most, finite(f.v[k]) ? __builtin_fabsf(f.v[k]) : 0.f);
-    most = butterfly(most, [](float a, float b) { return fmaxf(a, b); });
-    return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, most));
+    for (int k = 0; k < 4; ++k) x = max(x, __builtin_bit_cast(uint32_t, f.v[k]) & 0x7FFFFFFFu);
+    x = max_of_move<0xB1>(x);          // quad_perm [1,0,3,2]
+    x = max_of_move<0x4E>(x);          // quad_perm [2,3,0,1]
+    x = max_of_move<0x141>(x);         // row_half_mirror
+    x = max_of_move<0x140>(x);         // row_mirror
+    x = max_of_move<0x142>(x);         // row_bcast:15, each row's last lane to the next row
+    x = max_of_move<0x143>(x);         // row_bcast:31
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+constexpr uint32_t INFINITE = 0x7F800000;
+// ... of those that are finite
+__device__ __forceinline__ uint32_t largest_finite(Four f) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f.v[k] = finite(f.v[k]) ? f.v[k] : 0.f;
+    return largest(f);
 }
 
 constexpr uint32_t CODE_NAN = 0x7F;
 
 // to nearest, by the hardware's conversion
 __device__ __forceinline__ uint32_t coded_nearest(const Four& f, float inverse) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(f.v[0] * inverse, f.v[1] * inverse, 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f.v[2] * inverse, f.v[3] * inverse, w, true);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) if (!finite(f.v[k])) w = (w & ~(0xFF << (8 * k))) | (int)(CODE_NAN << (8 * k));
-    return (uint32_t)w;
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f.v[0] * inverse, f.v[1] * inverse, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f.v[2] * inverse, f.v[3] * inverse, w, true);
 }
 
 // Down or up by a draw: with u the distance of e4m3's values around q, floor(q / u), one more where remainder + draw reaches one.  The codes
 // count those distances: eight to an octave, from 2^-6 on; below it they are what they are there.
-__device__ __forceinline__ uint32_t coded_drawn(float r, float inverse, uint32_t field16) {
-    if (!finite(r)) return CODE_NAN;
-    const float q = r * inverse;
+__device__ __forceinline__ uint32_t coded_drawn(float q, uint32_t field16) {
     const int e = max(__builtin_amdgcn_frexp_expf(q), -5);
     const float steps = __builtin_ldexpf(q, 4 - e), down = __builtin_floorf(steps);
     const float draw = (float)(2 * field16 + 1) * 0x1p-17f;
     const int code = (int)down + ((steps - down) + draw >= 1.f ? 1 : 0) + 8 * (e + 5);
     return (uint32_t)(q > 0.f ? max(code, 1) : 0);
 }
+// The same of four values from 2^-6 on: there the code is the value's bits from the third of its mantissa on, and the draw, as wide as the others and a half
+// of their last place more, is added to those.  (Moved up by four places: a code is the top byte.)
+__device__ __forceinline__ uint32_t coded_drawn_normal(const Four& q, uint32_t lo16, uint32_t hi16) {
+    constexpr uint32_t REST = (8u << 4) - (960u << 24);
+    uint32_t u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t w = k < 2 ? lo16 : hi16, field = (k & 1 ? w >> 8 : w << 8) & 0xFFFF00u;
+        u[k] = (__builtin_bit_cast(uint32_t, q.v[k]) << 4) + (field + REST);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0703), hi = __builtin_amdgcn_perm(u[3], u[2], 0x07030C0C);
+    return lo | hi;
+}
 
-// the 16-bit fields of elements e .. e+3 (two to a word), whose draws have states base + (e/4) gamma and, unless aligned, the next
-__device__ __forceinline__ void draw_four(uint64_t base, uint64_t e, bool aligned, uint32_t* lo, uint32_t* hi) {
-    const uint64_t state = base + (e >> 2) * SPLITMIX_GAMMA, word = splitmix64_mix(state);
+// the 16-bit fields of elements e .. e+3 (two to a word): of the draw with this state, or from the (e mod 4)-th field on into the next
+__device__ __forceinline__ void draw_four(uint64_t state, uint32_t phase, uint32_t* lo, uint32_t* hi) {
+    const uint64_t word = splitmix64_mix(state);
     *lo = (uint32_t)word;
     *hi = (uint32_t)(word >> 32);
-    if (!aligned) {
+    if (phase) {
         const uint64_t more = splitmix64_mix(state + SPLITMIX_GAMMA);
-        const uint32_t next = (uint32_t)more, last0 = (uint32_t)(more >> 32), quarter = 16 * ((uint32_t)e & 1);
-        const bool halves = e & 2;
+        const uint32_t next = (uint32_t)more, last0 = (uint32_t)(more >> 32), quarter = 16 * (phase & 1);
+        const bool halves = phase & 2;
         const uint32_t a = halves ? *hi : *lo, b = halves ? next : *hi, c = halves ? last0 : next;
         *lo = __builtin_amdgcn_alignbit(b, a, quarter);       // (32-bit steps: see layers.h)
         *hi = __builtin_amdgcn_alignbit(c, b, quarter);
     }
 }
 
-// new moments (every operation rounded by itself, as the interface says, so that 8-bit states are a matter of bits) and parameter
-__device__ __forceinline__ void update(const AdamwRule& r, float g, float decay, float& p, float& m, float& v, float& root) {
+// New moments (every operation rounded by itself, as the interface says, so that 8-bit states are a matter of bits).
+__device__ __forceinline__ void moments(const AdamwRule& r, float g, float& m, float& v, float& root) {
 #pragma clang fp contract(off)
     m = m * r.beta1 + g * r.rest1;
     v = v * r.beta2 + (g * g) * r.rest2;
     root = __builtin_sqrtf(v);
-    p = p * decay - r.rate * (m / (root * r.root_scale + r.eps));
+}
+// The parameter, with the hardware's reciprocal (one unit in the last place of the change; the denominator is normal, zero or infinite: a root of
+// fp32 is).
+__device__ __forceinline__ float stepped(const AdamwRule& r, float p, float decay, float m, float root) {
+    const float change = m * __builtin_amdgcn_rcpf(__builtin_fmaf(root, r.root_scale, r.eps));
+    return __builtin_fmaf(p, decay, -(r.rate * change));
 }
 
-template <int BITS, class G>
+// One wavefront's part of a piece: TURNS blocks of its row, the t-th from `first` + t T/64 BLOCK on.  WHOLE: all of them are there.
+template <int BITS, class G, bool STREAM, bool WHOLE>
+__device__ __forceinline__ void step_piece(const AdamwTensor& t, const AdamwRule& rule, uint32_t row, int64_t first, int lane, uint64_t lane_draw) {
+    const int64_t states = row * t.cols + first, blocks = (t.cols + BLOCK - 1) / BLOCK, left = t.cols - first;
+    float* param = t.param + row * t.param_stride + first;
+    const G* grad = (const G*)t.grad + row * t.grad_stride + first;
+    const float decay = (float)(1. - rule.lr * t.decay);
+    const uint64_t draw0 = rule.seed + (1 + ((uint64_t)t.site << 40) + ((uint64_t)states >> 2)) * SPLITMIX_GAMMA;      // of the first lane
+    constexpr int APART = T / 64 * BLOCK;
+    Four p[TURNS], g[TURNS], m[TURNS], v[TURNS];
+    uint32_t mc[TURNS], vc[TURNS];
+    float ms[TURNS], vs[TURNS];
+    int n[TURNS];
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const uint32_t at = i * APART + lane * 4;
+        n[i] = WHOLE ? 4 : (int)max((int64_t)0, min((int64_t)4, left - (int64_t)at));
+        p[i] = load_four<STREAM>(param + at, n[i]);
+        g[i] = load_four<STREAM>(grad + at, n[i]);
+        if constexpr (BITS == 32) {
+            m[i] = load_four<STREAM>((const float*)t.m + states + at, n[i]);
+            v[i] = load_four<STREAM>((const float*)t.v + states + at, n[i]);
+        } else {
+            mc[i] = load_codes<STREAM>((const uint8_t*)t.m + states + at, n[i]);
+            vc[i] = load_codes<STREAM>((const uint8_t*)t.v + states + at, n[i]);
+            const int64_t block = row * blocks + min((first + i * APART) / BLOCK, blocks - 1);
+            ms[i] = t.m_scale[block];
+            vs[i] = t.v_scale[block];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const uint32_t at = i * APART + lane * 4;
+        if (!WHOLE && i * APART >= left) break;             // (a whole wavefront)
+        if constexpr (BITS == 8) {
+            m[i] = decoded(mc[i], ms[i]);
+            v[i] = decoded(vc[i], vs[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i].v[k] *= v[i].v[k];
+        }
+        Four root;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            moments(rule, g[i].v[k] * rule.grad_scale, m[i].v[k], v[i].v[k], root.v[k]);
+            p[i].v[k] = stepped(rule, p[i].v[k], decay, m[i].v[k], root.v[k]);
+        }
+        store_four<STREAM>(param + at, p[i], n[i]);
+        if (t.copy) {
+            uint16_t* copy = t.copy + row * t.copy_stride + first + at;
+            Pack<uint16_t, 4>::type c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float value = p[i].v[k];
+                c[k] = (uint16_t)split_hi(__builtin_bit_cast(uint32_t, value));
+            }
+            if (n[i] >= 4) *(Pack<uint16_t, 4>::loose*)copy = c;
+            else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) if (k < n[i]) copy[k] = c[k];
+            }
+        }
+        if constexpr (BITS == 32) {
+            store_four<STREAM>((float*)t.m + states + at, m[i], n[i]);
+            store_four<STREAM>((float*)t.v + states + at, v[i], n[i]);
+        } else {
+            if (!WHOLE) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) if (k >= n[i]) m[i].v[k] = root.v[k] = 0.f;
+            }
+            uint32_t most_m = largest(m[i]), most_r = largest(root);
+            const bool bad = most_m >= INFINITE || most_r >= INFINITE;
+            if (bad) { most_m = largest_finite(m[i]); most_r = largest_finite(root); }
+            const uint32_t fm = scale_field(most_m), fv = scale_field(most_r);
+            uint32_t lo16, hi16, m_codes = coded_nearest(m[i], power(254 - fm)), v_codes = 0;
+            draw_four(draw0 + i * (APART / 4) * SPLITMIX_GAMMA + lane_draw, (uint32_t)states & 3, &lo16, &hi16);
+            Four q;
+            float least = INFINITY;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                q.v[k] = root.v[k] * power(254 - fv);
+                least = fminf(least, q.v[k]);
+            }
+            if (!bad && __builtin_amdgcn_ballot_w64(!(least >= 0x1p-6f)) == 0) v_codes = coded_drawn_normal(q, lo16, hi16);
+            else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t word = k < 2 ? lo16 : hi16;
+                    uint32_t code = coded_drawn(q.v[k], k & 1 ? word >> 16 : word & 0xFFFF);
+                    if (!finite(root.v[k])) code = CODE_NAN;
+                    if (!finite(m[i].v[k])) m_codes = (m_codes & ~(0xFFu << (8 * k))) | CODE_NAN << (8 * k);
+                    v_codes |= code << (8 * k);
+                }
+            }
+            store_codes<STREAM>((uint8_t*)t.m + states + at, m_codes, n[i]);
+            store_codes<STREAM>((uint8_t*)t.v + states + at, v_codes, n[i]);
+            if (lane == 0) {
+                const int64_t block = row * blocks + (first + i * APART) / BLOCK;
+                t.m_scale[block] = power(fm);
+                t.v_scale[block] = power(fv);
+            }
+        }
+    }
+}
+
+template <int BITS, class G, bool STREAM>
 __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (rule.lr_dev) rule.lr = *rule.lr_dev;
@@ -155,6 +296,7 @@ __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
         if (rule.step_dev) rule.seed += (uint64_t)t;
         at_step(rule, (uint64_t)t);
     }
+    const uint64_t lane_draw = (uint64_t)lane * SPLITMIX_GAMMA;
     const uint32_t total = table.first[table.count];
     for (uint32_t piece = blockIdx.x; piece < total; piece += gridDim.x) {
         int lo = 0, hi = table.count;                       // the last tensor that begins at or before it
@@ -164,93 +306,17 @@ __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
         }
         const AdamwTensor& t = table.tensor[lo];
         const uint32_t in = piece - table.first[lo], row = in / t.pieces;
-        const int64_t col0 = (int64_t)(in - row * t.pieces) * PIECE;
-        float* param = t.param + row * t.param_stride;
-        const G* grad = (const G*)t.grad + row * t.grad_stride;
-        const int64_t states = row * t.cols;
-        const float decay = (float)(1. - rule.lr * t.decay);
-        const int64_t blocks = (t.cols + BLOCK - 1) / BLOCK;
-        const bool aligned = t.cols % 4 == 0;
-        const uint64_t base = rule.seed + (1 + ((uint64_t)t.site << 40)) * SPLITMIX_GAMMA;
-
-        Four p[TURNS], g[TURNS], m[TURNS], v[TURNS];
-        uint32_t mc[TURNS], vc[TURNS];
-        float ms[TURNS], vs[TURNS];
-        int n[TURNS];
-#pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            const int64_t block = col0 + (i * (T / 64) + wave) * BLOCK, col = block + lane * 4;
-            n[i] = (int)max((int64_t)0, min((int64_t)4, t.cols - col));
-            p[i] = load_four(param + col, n[i]);
-            g[i] = load_four(grad + col, n[i]);
-            if constexpr (BITS == 32) {
-                m[i] = load_four((const float*)t.m + states + col, n[i]);
-                v[i] = load_four((const float*)t.v + states + col, n[i]);
-            } else {
-                mc[i] = load_codes((const uint8_t*)t.m + states + col, n[i]);
-                vc[i] = load_codes((const uint8_t*)t.v + states + col, n[i]);
-                const int64_t at = row * blocks + min(block / BLOCK, blocks - 1);
-                ms[i] = t.m_scale[at];
-                vs[i] = t.v_scale[at];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            const int64_t block = col0 + (i * (T / 64) + wave) * BLOCK, col = block + lane * 4;
-            if (block >= t.cols) break;                     // (a whole wavefront)
-            if constexpr (BITS == 8) {
-                m[i] = decoded(mc[i], ms[i]);
-                v[i] = decoded(vc[i], vs[i]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[i].v[k] *= v[i].v[k];
-            }
-            Four root;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) update(rule, g[i].v[k] * rule.grad_scale, decay, p[i].v[k], m[i].v[k], v[i].v[k], root.v[k]);
-            store_four(param + col, p[i], n[i]);
-            if (t.copy) {
-                uint16_t* copy = t.copy + row * t.copy_stride + col;
-                typedef uint16_t four __attribute__((ext_vector_type(4)));
-                typedef four loose __attribute__((aligned(2)));
-                four c;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) c[k] = (uint16_t)split_hi(__builtin_bit_cast(uint32_t, p[i].v[k]));
-                if (n[i] >= 4) *(loose*)copy = c;
-                else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) if (k < n[i]) copy[k] = c[k];
-                }
-            }
-            if constexpr (BITS == 32) {
-                store_four((float*)t.m + states + col, m[i], n[i]);
-                store_four((float*)t.v + states + col, v[i], n[i]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) if (k >= n[i]) m[i].v[k] = root.v[k] = 0.f;
-                const uint32_t fm = scale_field(largest(m[i])), fv = scale_field(largest(root));
-                uint32_t lo16, hi16, codes = 0;
-                draw_four(base, (uint64_t)(states + col), aligned, &lo16, &hi16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t word = k < 2 ? lo16 : hi16;
-                    codes |= coded_drawn(root.v[k], power(254 - fv), k & 1 ? word >> 16 : word & 0xFFFF) << (8 * k);
-                }
-                store_codes((uint8_t*)t.m + states + col, coded_nearest(m[i], power(254 - fm)), n[i]);
-                store_codes((uint8_t*)t.v + states + col, codes, n[i]);
-                if (lane == 0) {
-                    const int64_t at = row * blocks + block / BLOCK;
-                    t.m_scale[at] = power(fm);
-                    t.v_scale[at] = power(fv);
-                }
-            }
-        }
+        const int64_t begin = (int64_t)(in - row * t.pieces) * PIECE, first = begin + wave * BLOCK;
+        if (begin + PIECE <= t.cols) step_piece<BITS, G, STREAM, true>(t, rule, row, first, lane, lane_draw);
+        else if (first < t.cols) step_piece<BITS, G, STREAM, false>(t, rule, row, first, lane, lane_draw);
     }
 }
 
 template <int BITS, class G>
-hipError_t start(const Table& table, const AdamwRule& rule, hipStream_t st) {
-    const uint32_t total = table.first[table.count];
-    adamw_kernel<BITS, G><<<dim3(std::min<uint32_t>(total, 1u << 22)), dim3(T), 0, st>>>(table, rule);
+hipError_t start(const Table& table, const AdamwRule& rule, bool stream, hipStream_t st) {
+    const dim3 grid(std::min<uint32_t>(table.first[table.count], 1u << 22));
+    if (stream) adamw_kernel<BITS, G, true><<<grid, dim3(T), 0, st>>>(table, rule);
+    else adamw_kernel<BITS, G, false><<<grid, dim3(T), 0, st>>>(table, rule);
     return hipGetLastError();
 }
 
@@ -259,14 +325,17 @@ hipError_t start(const Table& table, const AdamwRule& rule, hipStream_t st) {
 hipError_t launch_adamw(int bits, int grad_dtype, const AdamwRule& given, const kavg_adamw_tensor* tensors, int count, hipStream_t st) {
     AdamwRule rule = given;
     if (!rule.step_dev) { at_step(rule, rule.step); rule.seed += rule.step; }
+    double bytes = 0.;
+    for (int i = 0; i < count; ++i) bytes += (double)tensors[i].rows * tensors[i].cols * (4 + (grad_dtype == KAVG_BF16 ? 2 : 4) + bits / 4);
+    const bool stream = bytes > CACHE;
     Table table;
     table.count = 0;
     table.first[0] = 0;
     hipError_t e = hipSuccess;
     auto flush = [&] {
         if (table.count && e == hipSuccess)
-            e = bits == 32 ? (grad_dtype == KAVG_BF16 ? start<32, __bf16>(table, rule, st) : start<32, float>(table, rule, st))
-                           : (grad_dtype == KAVG_BF16 ? start<8, __bf16>(table, rule, st) : start<8, float>(table, rule, st));
+            e = bits == 32 ? (grad_dtype == KAVG_BF16 ? start<32, __bf16>(table, rule, stream, st) : start<32, float>(table, rule, stream, st))
+                           : (grad_dtype == KAVG_BF16 ? start<8, __bf16>(table, rule, stream, st) : start<8, float>(table, rule, stream, st));
         table.count = 0;
     };
     for (int i = 0; i < count; ++i) {

@@ -246,3 +246,24 @@ def test_rows_of_states_are_a_matter_of_their_scales():
         codes, scales = state[0], state[2]
         assert torch.equal(codes.float().view(rows, -1).abs().amax(1) > 220, torch.ones(rows, dtype=torch.bool, device="cuda")) and (scales > 2.0 ** -126).all()
     assert first.isfinite().all()
+
+
+@pytest.mark.parametrize("bits", (32, 8))
+def test_tensors_past_the_cache(bits):
+    """A step of more bytes than the caches hold gives, for its first elements, the bits of a step of those alone."""
+    n, some = 27_000_003, 100_000
+    p, g = normal(1, n), normal(2, n, scale=1e-2).bfloat16()
+    whole, part = kavg.AdamW([p.clone()], bits=bits), kavg.AdamW([p[:some].clone()], bits=bits)
+    for step in (1, 2):
+        whole.step([g], step, seed=3)
+        part.step([g[:some].clone()], step, seed=3)
+    ends = some if bits == 32 else some // L.BLOCK * L.BLOCK
+    assert torch.equal(whole.params[0][:ends], part.params[0][:ends])
+    for a, b in zip(whole.states[0], part.states[0]):
+        k = ends if a.dim() == 1 else ends // L.BLOCK
+        assert torch.equal(a.view(torch.uint8 if a.element_size() == 1 else a.dtype).reshape(-1)[:k], b.view(torch.uint8 if b.element_size() == 1 else b.dtype).reshape(-1)[:k])
+    last = kavg.AdamW([p[-5:].clone()])
+    last.step([g[-5:].clone()], 1)
+    first = kavg.AdamW([p.clone()])
+    first.step([g], 1)
+    assert torch.equal(first.params[0][-5:], last.params[0])
