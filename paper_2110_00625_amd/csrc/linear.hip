@@ -5,6 +5,7 @@
 namespace kavg {
 
 hipError_t start_rows(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st);
+hipError_t start_columns(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st);
 hipError_t start_bf16_plain(int tile, bool direct, const ProductArgs& a, hipStream_t st);
 hipError_t start_bf16_turned(int tile, bool direct, const ProductArgs& a, hipStream_t st);
 hipError_t start_bf16_gradient(int tile, bool direct, const ProductArgs& a, hipStream_t st);
@@ -21,7 +22,7 @@ constexpr int64_t MOST_TILES = 1 << 22;          // of a launch (fewer than 2^32
 
 struct Size { int r, c; };
 constexpr Size tile_size(int tile) {
-#define TILE(NUMBER, TR, TC, WR, WC) if (tile == NUMBER) return {TR, TC};
+#define TILE(NUMBER, TR, TC, WR, WC, BUFFERS) if (tile == NUMBER) return {TR, TC};
     KAVG_TILES(TILE)
 #undef TILE
     return {0, 0};
@@ -96,8 +97,8 @@ bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem)
 // filling and emptying the pipeline.  (256 compute units; 8192x4096x4096 in bf16 by large tiles 234 us, middle 260, small 376, four products of 1000^3 by
 // large, split in two, 33, middle 16, small 20, 2048x1024x1024 by middle 12, small 9; 4096^3 in fp32 by large 1032, middle 1004, small 1106.)
 struct Cost { float alone, shared, ends; };
-static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.26f, 0.18f, 0.5f}, {0.26f, 0.18f, 0.5f}};
-static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.5f}, {0.54f, 0.54f, 0.5f}};
+static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.21f, 0.15f, 0.8f}};
+static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.8f}};
 
 Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient) {
     const int64_t slices = up(nK, slice_of(dtype));
@@ -111,6 +112,7 @@ Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_g
         for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (splits > 1 && (2 * splits > slices || tiles * splits > 8 * CUS)) break;
             const int64_t each = up(slices, splits), m = up(tiles * up(slices, std::max<int64_t>(each, 1)), CUS);
+            if (tile == TILE_DEEP && m > 2) continue;
             float cost = m * c.ends + each * std::max(c.alone, c.shared * m);
             // the launch that joins the parts, which are written and read
             if (splits > 1) cost += 4.f + 0.1f * splits + (float)sets * nR * p.pitch * splits * 8 / 5.5e6f;
@@ -126,19 +128,21 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
     const int elem = bf16 ? 2 : 4;
     const bool direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
                         aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
-    if (direct && call.nR <= MOST_ROWS && !call.r_turned && !call.c_turned && call.sets * up(call.nC, 16) <= MOST_TILES) {
+    if (direct && !call.r_turned && !call.c_turned) {
         ProductArgs a = {};
         a.R = call.R; a.C = call.C;
         a.nR = call.nR; a.nC = call.nC; a.nK = call.nK;
         a.finish = call.finish;
-        return start_rows(call.dtype, a, call.sets, st);
+        if (call.nR <= MOST_ROWS && call.sets * up(call.nC, 16) <= MOST_TILES) return start_rows(call.dtype, a, call.sets, st);
+        // (half of the wavefronts have a part of the contraction)
+        if (call.nC <= MOST_ROWS && call.nK >= 4 * slice_of(call.dtype) && call.sets * up(call.nR, 16) <= MOST_TILES) return start_columns(call.dtype, a, call.sets, st);
     }
     const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
     if (plan.splits > 1) {
         if (bytes < plan.bytes) return hipErrorOutOfMemory;
         if (!workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;
     }
-    const int tile = plan.tile == TILE_LARGE && !direct ? TILE_MIDDLE : plan.tile;
+    const int tile = direct ? plan.tile : plan.tile == TILE_LARGE ? TILE_MIDDLE : plan.tile == TILE_DEEP ? TILE_SMALL : plan.tile;
     const Size size = tile_size(tile);
 
     ProductArgs a = {};

@@ -1,4 +1,4 @@
-// Products of few rows (up to 16) with weights whose inputs lie together: answers for single samples.  The weights are read once, the sums of a row are
+// Products of few rows, or few outputs (up to 16), with weights whose inputs lie together: answers for single samples.  The weights are read once, the sums of a row are
 // 2 bytes' worth of work for two flops a row: bound by memory.  A workgroup owns 16 or 32 outputs of a learner; its eight wavefronts go through the
 // contraction in turns of 128 bytes of every weight row, straight from memory into the operands of matrix instructions of 16 x 16 (a lane's
 // two chunks are its share of the turn: any order of the contraction will do, as long as both operands have it), and their sums meet in LDS, in
@@ -23,8 +23,9 @@ __device__ __forceinline__ f32x4 multiply16(const f32x4& c, const f32x4& r, f32x
     return acc;
 }
 
-// CB: blocks of 16 outputs.  Rows and outputs past the last are read as the last and not stored.
-template <class E, int CB>
+// CB: blocks of 16 outputs.  Rows and outputs past the last are read as the last and not stored.  TURNED: a product of few outputs instead, a last layer's;
+// rows and outputs change places until the results are stored.
+template <class E, int CB, bool TURNED>
 __global__ void __launch_bounds__(64 * WAVES) rows_kernel(ProductArgs a) {
     typedef typename Kind<E>::chunk chunk;
     constexpr int V = Kind<E>::V, TURN = 8 * V, ROUND = AT_ONCE * WAVES * TURN, PITCH = CB * 16 + 4;
@@ -32,10 +33,12 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(ProductArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t set = blockIdx.x / (uint32_t)a.tiles_c;
     const int c0 = (int)(blockIdx.x - set * a.tiles_c) * CB * 16, k0 = wave * TURN + (lane >> 4) * V;
+    const Matrix &C = TURNED ? a.R : a.C, &R = TURNED ? a.C : a.R;
+    const int nC = TURNED ? a.nR : a.nC, nR = TURNED ? a.nC : a.nR;
     const E* cp[CB];
 #pragma unroll
-    for (int j = 0; j < CB; ++j) cp[j] = (const E*)a.C.base + set * a.C.set_stride + min(c0 + j * 16 + (lane & 15), a.nC - 1) * a.C.stride;
-    const E* rp = (const E*)a.R.base + set * a.R.set_stride + min(lane & 15, a.nR - 1) * a.R.stride;
+    for (int j = 0; j < CB; ++j) cp[j] = (const E*)C.base + set * C.set_stride + min(c0 + j * 16 + (lane & 15), nC - 1) * C.stride;
+    const E* rp = (const E*)R.base + set * R.set_stride + min(lane & 15, nR - 1) * R.stride;
     f32x4 acc[CB];
 #pragma unroll
     for (int j = 0; j < CB; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -67,32 +70,38 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(ProductArgs a) {
 #pragma unroll
     for (int j = 0; j < CB; ++j) *(f32x4*)&parts[wave][lane & 15][j * 16 + (lane >> 4) * 4] = acc[j];
     __syncthreads();
-    const int row = threadIdx.x / (2 * CB), col = threadIdx.x % (2 * CB) * 8;
-    if (row >= a.nR) return;
-    const Finisher<E, E, 1, false> finish(a.finish, set, c0 + col, a.nC - c0 - col);
-    finish(row, 1, a.nR, [&](int, float (&v)[8]) {
+    const int lanes = TURNED ? 2 : 2 * CB, row = threadIdx.x / lanes, col = threadIdx.x % lanes * 8;        // of the tile, as it is stored
+    if (row >= (TURNED ? CB * 16 : 16)) return;
+    const int r = TURNED ? c0 + row : row, c = TURNED ? col : c0 + col;
+    const Finisher<E, E, 1, false> finish(a.finish, set, c, a.nC - c);
+    finish(r, 1, a.nR, [&](int, float (&v)[8]) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += parts[w][row][col + k];
+            for (int k = 0; k < 8; ++k) v[k] += TURNED ? parts[w][col + k][row] : parts[w][row][col + k];
     });
 }
 
-template <class E, int CB> hipError_t start(ProductArgs a, int64_t sets, hipStream_t st) {
-    a.tiles_c = (a.nC + CB * 16 - 1) / (CB * 16);
-    rows_kernel<E, CB><<<dim3((unsigned)(sets * a.tiles_c)), dim3(64 * WAVES), 0, st>>>(a);
+template <class E, int CB, bool TURNED> hipError_t start(ProductArgs a, int64_t sets, hipStream_t st) {
+    a.tiles_c = ((TURNED ? a.nR : a.nC) + CB * 16 - 1) / (CB * 16);
+    rows_kernel<E, CB, TURNED><<<dim3((unsigned)(sets * a.tiles_c)), dim3(64 * WAVES), 0, st>>>(a);
     return hipGetLastError();
 }
 
-template <class E> hipError_t start(const ProductArgs& a, int64_t sets, hipStream_t st) {
+template <class E, bool TURNED> hipError_t start(const ProductArgs& a, int64_t sets, hipStream_t st) {
     // twice as many outputs per read of x where even so every compute unit has two workgroups
-    return sets * ((a.nC + 31) / 32) >= 512 ? start<E, 2>(a, sets, st) : start<E, 1>(a, sets, st);
+    return sets * (((TURNED ? a.nR : a.nC) + 31) / 32) >= 512 ? start<E, 2, TURNED>(a, sets, st) : start<E, 1, TURNED>(a, sets, st);
 }
 
 }  // namespace
 
-hipError_t start_rows(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st) { return dtype == KAVG_BF16 ? start<__bf16>(a, sets, st) : start<float>(a, sets, st); }
+hipError_t start_rows(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st) {
+    return dtype == KAVG_BF16 ? start<__bf16, false>(a, sets, st) : start<float, false>(a, sets, st);
+}
+hipError_t start_columns(int dtype, const ProductArgs& a, int64_t sets, hipStream_t st) {
+    return dtype == KAVG_BF16 ? start<__bf16, true>(a, sets, st) : start<float, true>(a, sets, st);
+}
 
 }  // namespace kavg

@@ -9,7 +9,8 @@
 //     chunks of row k are exchanged too, by blocks of four, with k mod 4 (rows of 256 bytes and more), so that four rows of a block of 32 lie in different banks.
 // The lanes own slots of that layout in order, which is what loads from memory into LDS want; where an operand is not aligned to 16 bytes
 // or its contiguous extent is no multiple of a chunk, a slice comes through registers into the same slots.  A slice is in flight while the one
-// before it is multiplied (two LDS buffers).  Elements past the contraction are zeros; rows past an operand's extent are anything that can be read,
+// before it is multiplied (two LDS buffers), or three are, in a ring of four, where a compute unit has no more than two small tiles that could hide
+// each other's latency.  Elements past the contraction are zeros; rows past an operand's extent are anything that can be read,
 // they reach only results that are not stored.
 //
 // The matrix instruction's row index runs along c, so that a lane owns four consecutive columns of a row of the result.
@@ -103,6 +104,11 @@ template <class E, int TX, bool TURNED, int NT> struct Loader {
     // Through registers, at any alignment and length.  (A turned operand's last chunk of a row may be read into what follows, as far as the operand
     // reaches in memory.)
     __device__ __forceinline__ void fetch(u32x4 (&r)[N], int left, int nX) const {
+        if (TURNED ? left > BK && stride >= V && nX >= V : left >= BK) {             // (another row follows the slice's; all of its chunks are there)
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] = __builtin_bit_cast(u32x4, pack_load<E, V>(at[i]));
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int there = TURNED ? nX - x[i] : left - k[i];
@@ -163,16 +169,16 @@ __device__ __forceinline__ void add_up(const f32x4& f, float (&s)[4]) {
     for (int i = 0; i < 4; ++i) s[i] += f[i];
 }
 
-template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT> struct ProductTile {
+template <class E, int TR, int TC, int WR, int WC, int BUFFERS, bool RT, bool CT, bool DIRECT> struct ProductTile {
     static constexpr int NT = 64 * WR * WC, MR = TR / (32 * WR), MC = TC / (32 * WC);
     static constexpr int BUFFER = (TR + TC) * SLICE_BYTES;
     static constexpr int PITCH = MC * 32 + 4, STAGE = WR * WC * 32 * PITCH * 4;            // rows of results on their way out
-    static constexpr int LDS = 2 * BUFFER > STAGE ? 2 * BUFFER : STAGE;
+    static constexpr int RING = DIRECT ? BUFFERS : 2, LDS = RING * BUFFER > STAGE ? RING * BUFFER : STAGE;
 };
 
-template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT>
+template <class E, int TR, int TC, int WR, int WC, int BUFFERS, bool RT, bool CT, bool DIRECT>
 __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
-    typedef ProductTile<E, TR, TC, WR, WC, RT, CT, DIRECT> P;
+    typedef ProductTile<E, TR, TC, WR, WC, BUFFERS, RT, CT, DIRECT> P;
     typedef typename Kind<E>::chunk chunk;
     constexpr int NT = P::NT, MR = P::MR, MC = P::MC, BK = Kind<E>::BK, SLABS = 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -261,13 +267,21 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         };
         constexpr std::true_type whole = {};
         constexpr std::false_type cut = {};
-        load(cut, lds, left);
-        if (slices > 1) {
-            load(cut, lds + P::BUFFER, left - BK);
-            __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 0x0F70);      // vmcnt(LOADS)
-        } else __builtin_amdgcn_s_waitcnt(0x0F70);
+        // (vmcnt and lgkmcnt as the compiler counts them: it would add waits of its own behind an asm's)
+        constexpr int RING = P::RING, FLYING = LOADS * (RING - 2), LANDED = (FLYING & 15) | (FLYING >> 4) << 14 | 0x0070, FIRST = FLYING + LOADS;
+        static_assert(FIRST < 64, "the wait counter");
+        auto meet = [&] {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+#pragma unroll
+        for (int i = 0; i < RING; ++i) if (i < slices) load(cut, lds + i * P::BUFFER, left - i * BK);
+        if (slices >= RING) __builtin_amdgcn_s_waitcnt((FIRST & 15) | (FIRST >> 4) << 14 | 0x0F70);
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
         mend(lds, left);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                 // (no fence, which would wait for the second slice)
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
+        meet();
         take(0, lds, 0);
         char *now = lds, *next = lds + P::BUFFER;
         auto first_slabs = [&] {
@@ -278,16 +292,16 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
                 interleave(std::integral_constant<int, 0>());
             }
         };
-        auto turn = [&] { char* t = now; now = next; next = t; };
+        auto turn = [&] {
+            now = next;
+            next = next == lds + (RING - 1) * P::BUFFER ? lds : next + P::BUFFER;
+        };
         int s = 0;
-        for (const int full = min(left / BK, slices); s + 2 < full; ++s, left -= BK) {   // the slices that this loop loads are whole ones
+        for (const int full = min(left / BK, slices); s + RING < full; ++s, left -= BK) {   // the slices that this loop loads are whole ones
             first_slabs();
             __builtin_amdgcn_sched_barrier(0);               // (no product of theirs behind the barrier, where it would wait for the others)
-            // this wavefront's part of the next slice has landed, its reads of this one are done (waits that the compiler counts: it would add its own)
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x0070);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(LANDED);              // this wavefront's part of the next slice has landed, its reads of this one are done
+            meet();
             take(0, next, 0);
             load(whole, now, left);
             multiply_slab((SLABS - 1) & 1);
@@ -299,9 +313,10 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
             if (s + 1 < slices) {
                 __builtin_amdgcn_s_waitcnt(0x0F70);
                 mend(next, left - BK);
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                if (s + 2 < slices) load(cut, now, left - 2 * BK);
+                __builtin_amdgcn_s_waitcnt(0xC07F);
+                meet();
                 take(0, next, 0);
+                if (s + RING < slices) load(cut, now, left - RING * BK);
             }
             multiply_slab((SLABS - 1) & 1);
             turn();
@@ -373,16 +388,15 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
     else emit(Finisher<E, O, TURNS, false>(a.finish, set, c, a.nC - c));
 }
 
-// Tiles: rows, columns, wavefronts along rows and columns.  The first two are those of large results, the third of small
-// ones, the others of results that are narrow one way.
-#define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4) TILE(1, 128, 128, 2, 2) TILE(2, 64, 64, 2, 2) TILE(3, 128, 32, 4, 1) TILE(4, 32, 128, 1, 4)
-enum { TILE_LARGE = 0, TILE_MIDDLE = 1, TILE_SMALL = 2, TILE_TALL = 3, TILE_WIDE = 4, TILE_KINDS = 5 };
+// Tiles: rows, columns, wavefronts along rows and columns, buffers.  The last is that of few small tiles with a long contraction.
+#define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4, 2) TILE(1, 128, 128, 2, 2, 2) TILE(2, 64, 64, 2, 2, 2) TILE(3, 64, 64, 2, 2, 4)
+enum { TILE_LARGE = 0, TILE_MIDDLE = 1, TILE_SMALL = 2, TILE_DEEP = 3, TILE_KINDS = 4 };
 
-// DIRECT wants operands whose chunks are aligned and whole; the largest tile is for such operands only
-template <class E, int TR, int TC, int WR, int WC, bool RT, bool CT, bool DIRECT>
+// DIRECT wants operands whose chunks are aligned and whole; the first and the last tile are for such operands only
+template <class E, int TR, int TC, int WR, int WC, int BUFFERS, bool RT, bool CT, bool DIRECT>
 hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
-    typedef ProductTile<E, TR, TC, WR, WC, RT, CT, DIRECT> P;
-    const auto kernel = product_kernel<E, TR, TC, WR, WC, RT, CT, DIRECT>;
+    typedef ProductTile<E, TR, TC, WR, WC, BUFFERS, RT, CT, DIRECT> P;
+    const auto kernel = product_kernel<E, TR, TC, WR, WC, BUFFERS, RT, CT, DIRECT>;
     if (P::LDS > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
         if (e != hipSuccess) return e;
@@ -392,10 +406,10 @@ hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
 }
 
 template <class E, bool RT, bool CT> hipError_t start_kind(int tile, bool direct, const ProductArgs& a, hipStream_t st) {
-#define TILE(NUMBER, TR, TC, WR, WC) \
+#define TILE(NUMBER, TR, TC, WR, WC, BUFFERS) \
     case NUMBER: \
-        if (direct) return start_tile<E, TR, TC, WR, WC, RT, CT, true>(a, st); \
-        if constexpr (TR * TC < 256 * 256) return start_tile<E, TR, TC, WR, WC, RT, CT, false>(a, st); \
+        if (direct) return start_tile<E, TR, TC, WR, WC, BUFFERS, RT, CT, true>(a, st); \
+        if constexpr (TR * TC < 256 * 256 && BUFFERS == 2) return start_tile<E, TR, TC, WR, WC, BUFFERS, RT, CT, false>(a, st); \
         break;
     switch (tile) { KAVG_TILES(TILE) }
 #undef TILE

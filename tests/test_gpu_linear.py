@@ -12,7 +12,8 @@ IDS = ("f32", "bf16")
 CODE = dict(zip(L.ACTS, (kavg.KAVG_ACT_NONE, kavg.KAVG_ACT_RELU, kavg.KAVG_ACT_SILU)))
 # sets, rows, inputs, outputs: single elements, tails of every kind of tile, contractions that are split
 SIZES = [(1, 1, 1, 1), (2, 1, 8, 8), (3, 3, 5, 7), (1, 33, 64, 33), (2, 64, 64, 64), (1, 65, 130, 67), (2, 128, 128, 128), (1, 130, 72, 300), (1, 257, 264, 520),
-         (1, 300, 1, 9), (2, 1, 1000, 3), (1, 17, 2000, 130), (3, 40, 4096, 24), (1, 2, 4099, 1030), (16, 1, 96, 640), (1, 5000, 24, 40), (1, 5001, 23, 41), (2, 2049, 63, 33)]
+         (1, 300, 1, 9), (2, 1, 1000, 3), (1, 17, 2000, 130), (3, 40, 4096, 24), (1, 2, 4099, 1030), (16, 1, 96, 640), (1, 5000, 24, 40), (1, 5001, 23, 41), (2, 2049, 63, 33),
+         (2, 16, 1000, 100), (1, 15, 72, 8200), (3, 9, 4104, 1030), (2, 128, 1024, 10), (1, 5000, 264, 16), (3, 17, 520, 1), (1, 16640, 512, 5)]
 # as many tiles of the largest kind as there are compute units
 LARGE = [(4, 2048, 72, 2040), (4, 2047, 136, 2048), (1, 4096, 64, 4096)]
 
