@@ -18,6 +18,7 @@ namespace {
 constexpr int CUS = 256;
 constexpr int T = 256;
 constexpr int MOST_ROWS = 16;                    // that the kernel of few rows takes
+constexpr int64_t MOST_ELEMENTS = 1 << 25;       // of weights in bf16, there
 constexpr int64_t MOST_TILES = 1 << 22;          // of a launch (fewer than 2^32 lanes)
 
 struct Size { int r, c; };
@@ -38,52 +39,68 @@ int64_t tiles_of(int tile, int64_t sets, int nR, int nC) {
     return sets * up(nR, s.r) * std::max<int64_t>(1, up(nC, s.c));
 }
 
-// the sum of n parts, in order, eight of them asked for at a time
-template <int V> __device__ __forceinline__ void add_parts(const float* p, int64_t apart, int n, float (&v)[V]) {
+// The sum of n parts by G lanes that follow each other: each adds up every G-th, eight of which are asked for at a time, then they add in a tree.
+template <int V, int G> __device__ __forceinline__ void add_parts(const float* p, int64_t apart, int n, int lane, float (&v)[V]) {
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] = 0.f;
-    for (int s = 0; s < n; s += 8) {
+    for (int s = lane % G; s < n; s += 8 * G) {
         float t[8][V];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) load_some<float, V>(p + min(s + u, n - 1) * apart, V, t[u]);
+        for (int u = 0; u < 8; ++u) load_some<float, V>(p + min(s + u * G, n - 1) * apart, V, t[u]);
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (s + u < n) {
+            if (s + u * G < n) {
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[k] += t[u][k];
             }
     }
+#pragma unroll
+    for (int d = 1; d < G; d *= 2)
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += __shfl_xor(v[k], d);
 }
 
 // Sums of an operand of a weight gradient: [split][set][x] and where they go.
 struct SumsArgs { const float* parts; float* sums; int64_t split, from_set, to_set, n, sets; };
 
-// A lane adds up the parts of eight columns of a row, in order, and finishes them; the workgroups behind the last row's add up the operand's sums.
-template <class E>
+// G lanes add up the parts of eight columns of a row and the first finishes them; the workgroups behind the last row's add up the operand's sums.
+template <class E, int G>
 __global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, uint32_t groups, uint32_t per_row, Divisor by_row, SumsArgs sums) {
+    constexpr int EACH = T / G;                             // packs of a workgroup
+    const int lane = threadIdx.x, own = lane / G;
     if (blockIdx.x >= groups) {
-        const int64_t i = (int64_t)(blockIdx.x - groups) * T + threadIdx.x, set = i / sums.n, x = i - set * sums.n;
-        if (set >= sums.sets) return;
+        const int64_t i = min((int64_t)(blockIdx.x - groups) * EACH + own, sums.sets * sums.n - 1), set = i / sums.n, x = i - set * sums.n;
         float v[1];
-        add_parts<1>(sums.parts + set * sums.from_set + x, sums.split, a.splits, v);
-        sums.sums[set * sums.to_set + x] = v[0];
+        add_parts<1, G>(sums.parts + set * sums.from_set + x, sums.split, a.splits, lane, v);
+        sums.sums[set * sums.to_set + x] = v[0];            // (lanes past the last have the last)
         return;
     }
-    const uint64_t first = (uint64_t)blockIdx.x * T;
+    const uint64_t first = (uint64_t)blockIdx.x * EACH;
     // (a row has fewer than 2^28 packs, so that what is divided stays below 2^30)
-    const uint64_t row0 = first / per_row;
-    const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, down = divide(at, by_row);
-    if (first + threadIdx.x >= packs) return;
+    const uint64_t row0 = first / per_row, last = packs - 1 - first;
+    const uint32_t at = (uint32_t)(first - row0 * per_row) + (uint32_t)min((uint64_t)own, last), down = divide(at, by_row);
     const uint64_t row = row0 + down;
     const int c = (int)(at - down * per_row) * 8;
     float v[8];
-    add_parts<8>(a.partial + row * a.pitch + c, a.partial_split, a.splits, v);
+    add_parts<8, G>(a.partial + row * a.pitch + c, a.partial_split, a.splits, lane, v);
+    if ((uint64_t)own > last || lane % G) return;
     const int64_t set = (int64_t)(row / (uint64_t)a.nR), r = (int64_t)(row - (uint64_t)set * a.nR);
     const Finisher<E, E, 1, false> finish(a.finish, set, c, a.nC - c);
     finish(r, 1, a.nR, [&](int, float (&to)[8]) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) to[k] = v[k];
     });
+}
+// (eight lanes for a pack where there are few packs and parts for each lane: 8 results of 64x64 of 32 parts 7.2 us and JOIN_US)
+template <class E> hipError_t start_join(const ProductArgs& a, uint64_t packs, const SumsArgs& sums, hipStream_t st) {
+    const uint32_t per_row = (uint32_t)a.pitch / 8;
+    const Divisor by_row = divisor(std::max<uint32_t>(per_row, 1));
+    const int lanes = a.splits >= 8 && packs <= 64 * 1024 ? 8 : 1, each = T / lanes;
+    const uint32_t groups = (uint32_t)up(packs, each);
+    const dim3 grid(groups + (uint32_t)up(sums.n * sums.sets, each));
+    if (lanes == 8) join_kernel<E, 8><<<grid, dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
+    else join_kernel<E, 1><<<grid, dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
+    return hipGetLastError();
 }
 
 bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem) {
@@ -133,9 +150,12 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
         a.R = call.R; a.C = call.C;
         a.nR = call.nR; a.nC = call.nC; a.nK = call.nK;
         a.finish = call.finish;
-        if (call.nR <= MOST_ROWS && call.sets * up(call.nC, 16) <= MOST_TILES) return start_rows(call.dtype, a, call.sets, st);
-        // (half of the wavefronts have a part of the contraction)
-        if (call.nC <= MOST_ROWS && call.nK >= 4 * slice_of(call.dtype) && call.sets * up(call.nR, 16) <= MOST_TILES) return start_columns(call.dtype, a, call.sets, st);
+        // Larger matrices in bf16 come faster through tiles, whose loads never pause (4 rows of 4096x4096 7.5 us and 9.5 through tiles, of 4096x8192 15.6 and
+        // 15.5, of 4096x16384 27.6 and 21.2; 16 rows of 4096x4096 in fp32 17 and 26, which its products take).
+        auto fits = [&](int64_t lines) { return call.sets * up(lines, 16) <= MOST_TILES && (!bf16 || call.sets * lines * call.nK <= MOST_ELEMENTS); };
+        if (call.nR <= MOST_ROWS && fits(call.nC)) return start_rows(call.dtype, a, call.sets, st);
+        // (every wavefront has a part of the contraction)
+        if (call.nC <= MOST_ROWS && call.nK >= 8 * slice_of(call.dtype) && fits(call.nR)) return start_columns(call.dtype, a, call.sets, st);
     }
     const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
     if (plan.splits > 1) {
@@ -191,13 +211,8 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
             hipError_t e = start(tile, direct, a, st);
             if (e != hipSuccess) return e;
             if (plan.splits > 1) {
-                const uint32_t per_row = (uint32_t)plan.pitch / 8;
-                const uint64_t packs = (uint64_t)sets * a.nR * per_row;
-                const uint32_t groups = (uint32_t)up(packs, T), more = (uint32_t)up(sums.n * sums.sets, T);
-                const Divisor by_row = divisor(std::max<uint32_t>(per_row, 1));
-                if (bf16 && !call.r_turned) join_kernel<__bf16><<<dim3(groups + more), dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
-                else join_kernel<float><<<dim3(groups + more), dim3(T), 0, st>>>(a, packs, groups, per_row, by_row, sums);
-                e = hipGetLastError();
+                const uint64_t packs = (uint64_t)sets * a.nR * (plan.pitch / 8);
+                e = bf16 && !call.r_turned ? start_join<__bf16>(a, packs, sums, st) : start_join<float>(a, packs, sums, st);
                 if (e != hipSuccess) return e;
             }
         }
