@@ -80,27 +80,43 @@ template <class E, int V> __device__ __forceinline__ void store_some(E* p, int n
 }
 
 // What the values of N rows want from memory, all asked for before the first is used (a store in between could not be passed by a load).
-// E: type of the operands, O: of the result.  Columns c .. c+7 of rows r, r + step, ..; n of the columns are there, all eight if WHOLE.
-template <class E, class O, int N, bool WHOLE> struct Finisher {
+// E: type of the operands, O: of the result.  Columns c .. c+3 and c+APART .. c+APART+3 of rows r, r + step, ..; `left` columns are there from c on,
+// all eight if WHOLE.  (APART 4: eight together, 16 bytes of bf16.  In fp32 the halves are as far apart as makes the lanes of a row lie together.)
+template <class E, class O, int N, bool WHOLE, int APART = 4> struct Finisher {
     const Finish& f;
     int64_t set;
-    int c, n;
+    int c, left;
     float bias[8];
 
-    __device__ __forceinline__ Finisher(const Finish& f, int64_t set, int c, int left) : f(f), set(set), c(c), n(WHOLE ? 8 : left) {
-        if (f.bias) load_some<float, 8>(f.bias + set * f.bias_set + c, n, bias);
+    template <class X> __device__ __forceinline__ void load(const X* p, float (&v)[8]) const {
+        if (APART == 4) { load_some<X, 8>(p, WHOLE ? 8 : left, v); return; }
+        float lo[4], hi[4];
+        load_some<X, 4>(p, WHOLE ? 4 : left, lo);
+        load_some<X, 4>(p + APART, WHOLE ? 4 : left - APART, hi);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[k] = lo[k]; v[4 + k] = hi[k]; }
+    }
+    template <class X> __device__ __forceinline__ void store(X* p, const float (&v)[8]) const {
+        if (APART == 4) { store_some<X, 8>(p, WHOLE ? 8 : left, v); return; }
+        const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+        store_some<X, 4>(p, WHOLE ? 4 : left, lo);
+        store_some<X, 4>(p + APART, WHOLE ? 4 : left - APART, hi);
+    }
+
+    __device__ __forceinline__ Finisher(const Finish& f, int64_t set, int c, int left) : f(f), set(set), c(c), left(left) {
+        if (f.bias) load(f.bias + set * f.bias_set + c, bias);
     }
     // value(u, v): the eight values of row r + u * step; rows from `end` on are left out
     template <class Value> __device__ __forceinline__ void operator()(int64_t r, int step, int64_t end, Value value) const {
-        if (!WHOLE && n <= 0) return;
+        if (!WHOLE && left <= 0) return;
         float before[N][8], residual[N][8];
         if (f.before) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) if (r + u * step < end) load_some<E, 8>((const E*)f.before + set * f.before_set + (r + u * step) * f.before_row + c, n, before[u]);
+            for (int u = 0; u < N; ++u) if (r + u * step < end) load((const E*)f.before + set * f.before_set + (r + u * step) * f.before_row + c, before[u]);
         }
         if (f.residual) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) if (r + u * step < end) load_some<E, 8>((const E*)f.residual + set * f.residual_set + (r + u * step) * f.residual_row + c, n, residual[u]);
+            for (int u = 0; u < N; ++u) if (r + u * step < end) load((const E*)f.residual + set * f.residual_set + (r + u * step) * f.residual_row + c, residual[u]);
         }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -111,7 +127,7 @@ template <class E, class O, int N, bool WHOLE> struct Finisher {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] += bias[k];
             }
-            if (f.kept) store_some<E, 8>((E*)f.kept + set * f.kept_set + (r + u * step) * f.kept_row + c, n, v);
+            if (f.kept) store((E*)f.kept + set * f.kept_set + (r + u * step) * f.kept_row + c, v);
             if (f.silu) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] *= sigmoid_of(v[k] * SILU_SCALE);
@@ -132,7 +148,7 @@ template <class E, class O, int N, bool WHOLE> struct Finisher {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] += residual[u][k];
             }
-            store_some<O, 8>((O*)f.out + set * f.out_set + (r + u * step) * f.out_row + c, n, v);
+            store((O*)f.out + set * f.out_set + (r + u * step) * f.out_row + c, v);
         }
     }
 };

@@ -362,8 +362,9 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
     constexpr int WTC = MC * 32, PITCH = P::PITCH, ROW_LANES = WTC / 8, ROWS = 64 / ROW_LANES, TURNS = 32 / ROWS;
     __syncthreads();
     float* stage = (float*)lds + wave * 32 * PITCH;
-    const int c = c0 + wc * WTC + (lane % ROW_LANES) * 8, down = lane / ROW_LANES;
-    auto emit = [&](const auto& finish) {
+    const int first = c0 + wc * WTC, down = lane / ROW_LANES;
+    auto emit = [&](const auto& finish, auto apart) {
+        const int col = (lane % ROW_LANES) * (apart.value == 4 ? 8 : 4);
 #pragma unroll
         for (int i = 0; i < MR; ++i) {
 #pragma unroll
@@ -371,21 +372,25 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) *(f32x4*)(stage + (lane & 31) * PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = (f32x4){acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
             finish(r0 + (wr * MR + i) * 32 + down, ROWS, a.nR, [&](int u, float (&v)[8]) {
-                const float* from = stage + (down + u * ROWS) * PITCH + (lane % ROW_LANES) * 8;
-                const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
+                const float* from = stage + (down + u * ROWS) * PITCH + col;
+                const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + apart.value);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) { v[k] = lo[k]; v[4 + k] = hi[k]; }
             });
         }
     };
     typedef typename std::conditional<RT, float, E>::type O;
+    constexpr int FAR = WTC / 2, APART = sizeof(O) == 4 ? FAR : 4;
+    const int c = first + (lane % ROW_LANES) * (APART == 4 ? 8 : 4);
+    const std::integral_constant<int, APART> apart = {};
     if (a.partial) {
         Finish parts = {};
         parts.floor = -INFINITY;
         parts.out = a.partial + split * a.partial_split; parts.out_set = (int64_t)a.nR * a.pitch; parts.out_row = a.pitch;
-        emit(Finisher<E, float, TURNS, false>(parts, set, c, a.nC > c ? 8 : 0));          // (rows are padded to whole eights)
-    } else if (c0 + TC <= a.nC) emit(Finisher<E, O, TURNS, true>(a.finish, set, c, 8));
-    else emit(Finisher<E, O, TURNS, false>(a.finish, set, c, a.nC - c));
+        const int c = first + (lane % ROW_LANES) * 4;
+        emit(Finisher<E, float, TURNS, false, FAR>(parts, set, c, a.pitch - c), std::integral_constant<int, FAR>());       // (rows are padded to whole eights)
+    } else if (c0 + TC <= a.nC) emit(Finisher<E, O, TURNS, true, APART>(a.finish, set, c, 0), apart);
+    else emit(Finisher<E, O, TURNS, false, APART>(a.finish, set, c, a.nC - c), apart);
 }
 
 // Tiles: rows, columns, wavefronts along rows and columns, buffers.  The last is that of few small tiles with a long contraction.

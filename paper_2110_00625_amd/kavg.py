@@ -4,6 +4,7 @@ of the method runs inside the library's HIP kernels.  There is no fallback:
 if the library is missing or a call fails, an exception is raised.
 """
 import ctypes
+import functools
 import os
 import struct
 
@@ -456,14 +457,21 @@ def _weights(t, name):
     return _WEIGHTS.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2], st[-1])
 
 
-def _product_workspace(product, backward, x):
+@functools.lru_cache(maxsize=1024)
+def _product_bytes(product, backward):
+    """Bytes of workspace, a function of the sizes (asked for once: the call takes as long as the marshalling of an array)."""
     n = ctypes.c_size_t(0)
     if _lib.kavg_linear_workspace(product, backward, ctypes.byref(n)) != KAVG_OK:
         _bad("kavg_linear rejected its sizes or options")
-    if not n.value:
+    return n.value
+
+
+def _product_workspace(product, backward, x):
+    n = _product_bytes(product, backward)
+    if not n:
         return None, None, 0
-    block = _torch_module.empty(n.value, dtype=_torch_module.uint8, device=x.device)
-    return block, block.data_ptr(), n.value
+    block = _torch_module.empty(n, dtype=_torch_module.uint8, device=x.device)
+    return block, block.data_ptr(), n
 
 
 def kavg_linear(x, weight, bias=None, activation=KAVG_ACT_NONE, residual=None, pre=False, out=None):
@@ -520,7 +528,7 @@ def kavg_linear_backward(dz, x, weight, activation=KAVG_ACT_NONE, pre=None, out=
     product = _product(x, activation, lead, rows, inputs, outputs)
     z = _matrix(dz, x, lead + (rows, outputs), "dz")
     block, at, nbytes = _product_workspace(product, 1, x)
-    dx = None if out is False else torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    dx = None if out is False else x.new_empty(x.shape) if out is None else out
     d = p = None
     if dx is not None:
         d = _matrix(dx, x, x.shape, "out")
