@@ -99,10 +99,14 @@ int kavg_linear_workspace(const kavg_product* product, int backward, size_t* byt
     if (empty(product)) return KAVG_OK;
     const int64_t sets = product->sets;
     const int rows = (int)product->rows, in = (int)product->inputs, out = (int)product->outputs, dtype = product->dtype;
-    if (!backward) *bytes = product_plan(dtype, sets, rows, out, in, false).bytes;
-    else
-        *bytes = std::max({product_plan(dtype, sets, rows, in, out, false).bytes, product_plan(dtype, sets, out, in, rows, true).bytes,
-                           product_plan(dtype, sets, in, out, rows, true).bytes, product_plan(dtype, sets, out, 0, rows, true).bytes});
+    auto ask = [&](int nR, int nC, int nK, Turned turned) { *bytes = std::max(*bytes, product_plan(dtype, sets, nR, nC, nK, turned).bytes); };
+    // (for weights and gradients in either order)
+    for (const Turned turned : {NONE_TURNED, C_TURNED}) ask(rows, backward ? in : out, backward ? out : in, turned);
+    if (backward) {
+        ask(out, in, rows, BOTH_TURNED);
+        ask(in, out, rows, BOTH_TURNED);
+        ask(out, 0, rows, BOTH_TURNED);
+    }
     return KAVG_OK;
 }
 

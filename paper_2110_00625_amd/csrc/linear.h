@@ -44,7 +44,8 @@ struct Plan {
     int tile, splits, pitch;
     size_t bytes;                                // of workspace
 };
-Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient);
+enum Turned { NONE_TURNED, C_TURNED, BOTH_TURNED };        // the last: a weight gradient
+Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned);
 // hipErrorOutOfMemory, hipErrorInvalidValue: a workspace too small, misaligned or not there, before anything is launched
 hipError_t launch_product(const ProductCall& c, void* workspace, size_t bytes, hipStream_t st);
 

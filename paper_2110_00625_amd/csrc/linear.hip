@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(T) join_kernel(ProductArgs a, uint64_t packs, 
         for (int k = 0; k < 8; ++k) to[k] = v[k];
     });
 }
-// (eight lanes for a pack where there are few packs and parts for each lane: 8 results of 64x64 of 32 parts 7.2 us and JOIN_US)
+// (eight lanes for a pack where there are few packs and parts for each lane: 8 results of 64x64 of 32 parts 7.2 us and 5.3)
 template <class E> hipError_t start_join(const ProductArgs& a, uint64_t packs, const SumsArgs& sums, hipStream_t st) {
     const uint32_t per_row = (uint32_t)a.pitch / 8;
     const Divisor by_row = divisor(std::max<uint32_t>(per_row, 1));
@@ -117,7 +117,7 @@ struct Cost { float alone, shared, ends; };
 static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.21f, 0.15f, 0.8f}};
 static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.8f}};
 
-Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_gradient) {
+Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned) {
     const int64_t slices = up(nK, slice_of(dtype));
     Plan p = {};
     p.pitch = (int)up(nC, 8) * 8;
@@ -129,14 +129,15 @@ Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, bool weight_g
         for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (splits > 1 && (2 * splits > slices || tiles * splits > 8 * CUS)) break;
             const int64_t each = up(slices, splits), m = up(tiles * up(slices, std::max<int64_t>(each, 1)), CUS);
-            if (tile == TILE_DEEP && m > 2) continue;
+            // (turned operands gain nothing by slices further ahead: 16 learners' 128x1024x1024 10.5 us by deep tiles and 11.7 by small ones, turned 13.6 and 13.0)
+            if (tile == TILE_DEEP && (m > 2 || turned != NONE_TURNED)) continue;
             float cost = m * c.ends + each * std::max(c.alone, c.shared * m);
             // the launch that joins the parts, which are written and read
             if (splits > 1) cost += 4.f + 0.1f * splits + (float)sets * nR * p.pitch * splits * 8 / 5.5e6f;
             if (cost < least) { least = cost; p.tile = tile; p.splits = (int)std::max<int64_t>(1, up(slices, std::max<int64_t>(each, 1))); }
         }
     }
-    if (p.splits > 1) p.bytes = (size_t)p.splits * sets * ((size_t)nR * p.pitch + (weight_gradient ? std::max(nR, nC) : 0)) * sizeof(float);
+    if (p.splits > 1) p.bytes = (size_t)p.splits * sets * ((size_t)nR * p.pitch + (turned == BOTH_TURNED ? std::max(nR, nC) : 0)) * sizeof(float);
     return p;
 }
 
@@ -157,7 +158,7 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
         // (every wavefront has a part of the contraction)
         if (call.nC <= MOST_ROWS && call.nK >= 8 * slice_of(call.dtype) && fits(call.nR)) return start_columns(call.dtype, a, call.sets, st);
     }
-    const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned);
+    const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned ? BOTH_TURNED : call.c_turned ? C_TURNED : NONE_TURNED);
     if (plan.splits > 1) {
         if (bytes < plan.bytes) return hipErrorOutOfMemory;
         if (!workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;

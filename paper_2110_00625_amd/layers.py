@@ -4,6 +4,8 @@ again from (drop, seed, site), where seed is not the index_seed of a context (it
 products their inputs, their weights and, where an activation follows, what it was given.
 A program that writes its own backward pass calls `kavg` instead, which can also write into given tensors (a learner's gradient
 vector, x itself)."""
+import math
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -62,7 +64,8 @@ def _shape(x, weight):
     """x [sets, .., inputs] or [.., inputs] as [sets, rows, inputs] or [rows, inputs]."""
     if x.dim() < weight.dim() or (weight.dim() == 3 and x.shape[0] != weight.shape[0]):
         raise kavg.KavgError(kavg.KAVG_EINVAL, "x of %s and weights of %s" % (tuple(x.shape), tuple(weight.shape)))
-    return x.reshape(x.shape[0], -1, x.shape[-1]) if weight.dim() == 3 else x.reshape(-1, x.shape[-1])
+    rows = math.prod(x.shape[weight.dim() - 2:-1])
+    return x.reshape(x.shape[0], rows, x.shape[-1]) if weight.dim() == 3 else x.reshape(rows, x.shape[-1])
 
 
 class _Products(torch.autograd.Function):
@@ -79,7 +82,7 @@ class _Products(torch.autograd.Function):
             used.append(w)
             if i == last:
                 h = kavg.kavg_linear(h, w, b, residual=residual)
-            elif wanted:
+            elif wanted and activation != kavg.KAVG_ACT_NONE:
                 h, pre = kavg.kavg_linear(h, w, b, activation=activation, pre=True)
                 kept.append(pre)
             else:
@@ -99,7 +102,7 @@ class _Products(torch.autograd.Function):
         for i in range(n - 1, lowest - 1, -1):
             inner = wanted[0] if i == 0 else i > lowest
             dx, dw, db = kavg.kavg_linear_backward(
-                dz, inputs[i], weights[i], activation=ctx.activation if i else kavg.KAVG_ACT_NONE, pre=kept[i - 1] if i else None, out=None if inner else False,
+                dz, inputs[i], weights[i], activation=ctx.activation if i else kavg.KAVG_ACT_NONE, pre=kept[i - 1] if i and kept else None, out=None if inner else False,
                 dweight=None if wanted[3 + 2 * i] else False, dbias=None if wanted[4 + 2 * i] else False)
             grads[2 * i], grads[2 * i + 1] = None if dw is None else dw.to(ctx.types[i]), db
             dz = dx

@@ -67,6 +67,8 @@ def test_a_gradient_of_a_sum_and_of_frozen_parts():
         got = torch.autograd.grad(layers.mlp(part[0], [(part[1], part[2]), (part[3], None)]).sum(), part[k])[0]
         assert torch.equal(got, full[k]) or k == 2
         assert float((got - full[k]).abs().max()) <= 1e-5 * float(full[k].abs().max())
+    none = layers.mlp(torch.empty(2, 0, 3, 16, device="cuda"), [(normal(6, 2, 24, 16), normal(7, 2, 24)), (normal(8, 2, 8, 24), None)])
+    assert none.shape == (2, 0, 3, 8)
     r = normal(5, 30, 8).requires_grad_()
     assert torch.equal(torch.autograd.grad(layers.linear(x, normal(6, 8, 16), residual=r).sum(), r)[0], torch.ones_like(r))
 
