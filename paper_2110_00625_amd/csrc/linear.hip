@@ -112,7 +112,8 @@ bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem)
 
 // What a tile of each kind costs, in microseconds: a slice of 128 bytes where a compute unit has one tile of them, and per tile where it has more;
 // filling and emptying the pipeline.  (256 compute units; 8192x4096x4096 in bf16 by large tiles 234 us, middle 260, small 376, four products of 1000^3 by
-// large, split in two, 33, middle 16, small 20, 2048x1024x1024 by middle 12, small 9; 4096^3 in fp32 by large 1032, middle 1004, small 1106.)
+// large, split in two, 33, middle 16, small 20, 2048x1024x1024 by middle 12, small 9; 1024x8192x1024 by middle 37, split in eight 32, deep 30; 4096^3 in
+// fp32 by large 1032, middle 1004, small 1106.)
 struct Cost { float alone, shared, ends; };
 static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.21f, 0.15f, 0.8f}};
 static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.8f}};

@@ -1,11 +1,12 @@
-// Products of few rows, or few outputs (up to 16), with weights whose inputs lie together: answers for single samples.  The weights are read once, the sums of a row are
-// 2 bytes' worth of work for two flops a row: bound by memory.  A workgroup owns 16 or 32 outputs of a learner; its eight wavefronts go through the
-// contraction in turns of 128 bytes of every weight row, straight from memory into the operands of matrix instructions of 16 x 16 (a lane's
-// two chunks are its share of the turn: any order of the contraction will do, as long as both operands have it), and their sums meet in LDS, in
-// order.  No LDS in the loop, no split contraction, one launch.
-// 1 row of 4096x4096 in bf16 7.4 us a call in a graph (4.5 TB/s), 11 rows 9.3, 16 rows in fp32 18.1, 4 rows of 4096x16384 26.8 (5.0 TB/s); through tiles,
-// split in eight and joined, 1 to 32 rows 12.7.  Tried: rounds in two sets of registers, one loaded while the other is multiplied (4096x16384 30.3: fewer
-// wavefronts), sixteen wavefronts (18.6 in fp32, the same in bf16), 17 to 32 rows in two blocks (13.8: x is read as often as the weights).
+// Products of few rows, or of few outputs (up to 16), whose operands' contraction lies together: answers for single samples, last layers.  The weights (or
+// the many rows) are read once, for two flops a row and 2 or 4 bytes: bound by memory.  A workgroup owns 16 or 32 outputs of a learner; its eight wavefronts
+// go through the contraction in turns of 128 bytes of every weight row, straight from memory into the operands of matrix instructions of 16 x 16 (a
+// lane's two chunks are its share of the turn: any order of the contraction will do, as long as both operands have it), and their sums meet in
+// LDS, in order.  No LDS in the loop, no split contraction, one launch.
+// A call in a graph: 1 row of 4096x4096 in bf16 7.4 us (4.5 TB/s, 2.5 of it the launch's), 11 rows 9.2, 16 rows in fp32 18.0, 16 learners' 128x1024x10 in fp32
+// 5.9; through tiles, split and joined, 9.5, 9.5, 26 and 10.8.  Tried: rounds in two sets of registers, one loaded while the other is multiplied (4 rows of
+// 4096x16384 30.3 for 26.8: fewer wavefronts), a ring of turns in registers (30.3), loads of whole lines, eight rows' turns at a time (8.2 and 32: twice
+// the products and sums), sixteen wavefronts (18.6 in fp32, the same in bf16), 17 to 32 rows in two blocks (13.8: x is read as often as the weights).
 #include "linear_tile.h"
 
 namespace kavg {

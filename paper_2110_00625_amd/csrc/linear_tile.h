@@ -14,6 +14,14 @@
 // they reach only results that are not stored.
 //
 // The matrix instruction's row index runs along c, so that a lane owns four consecutive columns of a row of the result.
+//
+// What bounds them.  Large tiles: 8192x4096x4096 in bf16 209 - 224 us by box (1.23 - 1.31 PFLOP/s; a library's product 180), its gradients 231 and 229 turned
+// either way (248, 278); 8192x4096x16384 with SiLU and the pre-activation 927 - 970 (795 without them): the matrix cores are busy for 65 % of the
+// cycles, at a clock that falls to 1.5 - 1.8 GHz under them; the rest are a pipeline's ends and results (100 us of the last) and waits for memory.  Steps on the
+// way: the barrier in front of the last slab instead of the first and pinned orders 1190 -> 1044 (the gradient of x), waits that the compiler counts 227 -> 209,
+// results through LDS 1085 -> 938.  In fp32 4096^3 takes 1010 us, 136 TFLOP/s of the 145 that a library's product reaches.  Small tiles: latency, 0.2 us a slice.
+// Tried: rings of slices of 64 bytes (half lines: 220 for 209, turned 282 for 239), four wavefronts of 128x128 (registers in scratch), tiles of 128x32,
+// 32x128 and 128x64 (in no swept case better by more than 4 %).
 #pragma once
 #include "linear.h"
 #include <type_traits>
