@@ -275,20 +275,29 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         };
         constexpr std::true_type whole = {};
         constexpr std::false_type cut = {};
-        // (vmcnt and lgkmcnt as the compiler counts them: it would add waits of its own behind an asm's)
-        constexpr int RING = P::RING, FLYING = LOADS * (RING - 2), LANDED = (FLYING & 15) | (FLYING >> 4) << 14 | 0x0070, FIRST = FLYING + LOADS;
+        // Waits as the compiler counts them (it would add its own behind an asm's), with no access to memory moved across.
+        constexpr int RING = P::RING, FLYING = LOADS * (RING - 2), FIRST = FLYING + LOADS;
         static_assert(FIRST < 64, "the wait counter");
-        auto meet = [&] {
+        auto wait = [&](auto counts) {
             asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(counts.value);
+            asm volatile("" ::: "memory");
+        };
+        auto meet = [&] {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
+        // vmcnt n, bits 3:0 and 15:14; expcnt 7; lgkmcnt, bits 11:8, 15 (any) or 0
+        constexpr std::integral_constant<int, (FIRST & 15) | (FIRST >> 4) << 14 | 0x0F70> first_landed = {};
+        constexpr std::integral_constant<int, (FLYING & 15) | (FLYING >> 4) << 14 | 0x0070> next_landed_and_read = {};
+        constexpr std::integral_constant<int, 0x0F70> all_landed = {};
+        constexpr std::integral_constant<int, 0xC07F> lds_done = {};
 #pragma unroll
         for (int i = 0; i < RING; ++i) if (i < slices) load(cut, lds + i * P::BUFFER, left - i * BK);
-        if (slices >= RING) __builtin_amdgcn_s_waitcnt((FIRST & 15) | (FIRST >> 4) << 14 | 0x0F70);
-        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        if (slices >= RING) wait(first_landed);
+        else wait(all_landed);
         mend(lds, left);
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
+        wait(lds_done);
         meet();
         take(0, lds, 0);
         char *now = lds, *next = lds + P::BUFFER;
@@ -308,7 +317,7 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         for (const int full = min(left / BK, slices); s + RING < full; ++s, left -= BK) {   // the slices that this loop loads are whole ones
             first_slabs();
             __builtin_amdgcn_sched_barrier(0);               // (no product of theirs behind the barrier, where it would wait for the others)
-            __builtin_amdgcn_s_waitcnt(LANDED);              // this wavefront's part of the next slice has landed, its reads of this one are done
+            wait(next_landed_and_read);                      // (this wavefront's part of the next slice, its reads of this one)
             meet();
             take(0, next, 0);
             load(whole, now, left);
@@ -319,9 +328,9 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         for (; s < slices; ++s, left -= BK) {
             first_slabs();
             if (s + 1 < slices) {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
+                wait(all_landed);
                 mend(next, left - BK);
-                __builtin_amdgcn_s_waitcnt(0xC07F);
+                wait(lds_done);
                 meet();
                 take(0, next, 0);
                 if (s + RING < slices) load(cut, now, left - RING * BK);

@@ -601,9 +601,12 @@ class AdamW:
 
     def __init__(self, params, states=None, copies=None, bits=32):
         torch = _torch_module or _torch()
-        self.params, self.copies = list(params), list(copies) if copies is not None else [None] * len(params)
+        self.params = list(params)
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
         if bits not in (8, 32):
             _bad("states of %r bits" % (bits,))
+        for i, p in enumerate(self.params):
+            _dtype(p, "params[%d]" % i)
         if states is None:
             states = [self.zeros(p, bits) for p in self.params]
         self.states = [tuple(s) for s in states]
@@ -615,17 +618,19 @@ class AdamW:
         self._rows, self._decay, written = [], None, set()
         for i, (p, state, copy) in enumerate(zip(self.params, self.states, self.copies)):
             name = "params[%d]" % i
-            _dtype(p, name)
             if p.dtype is not torch.float32 or p.device != self.device:
                 _bad("%s is not a float32 tensor on the device of the others" % name)
             self._check_state(torch, p, state, "states[%d]" % i)
+            # (a parameter without gaps goes by its scales' rows, or its copy's)
             rows = state[2].shape[0] if self.bits == 8 else None
+            if rows is None and p.is_contiguous() and isinstance(copy, torch.Tensor) and copy.shape == p.shape:
+                rows = _run(copy, "copies[%d]" % i)[0]
             rows, cols, stride = _run(p, name, rows)
             if self.bits == 8 and p.numel() and state[2].shape[1] != (cols + _BLOCK - 1) // _BLOCK:
                 _bad("states[%d] has scales for %s blocks of %d columns" % (i, tuple(state[2].shape), cols))
             at, cs = 0, 0
             if copy is not None:
-                if copy.dtype is not torch.bfloat16 or copy.shape != p.shape or copy.device != p.device:
+                if not isinstance(copy, torch.Tensor) or copy.dtype is not torch.bfloat16 or copy.shape != p.shape or copy.device != p.device:
                     _bad("copies[%d] is not a bfloat16 tensor like the parameter" % i)
                 at, cs = copy.data_ptr(), _run(copy, "copies[%d]" % i, rows)[2]
             pointers = [p.data_ptr(), 0, state[0].data_ptr(), state[1].data_ptr()] + ([s.data_ptr() for s in state[2:]] if self.bits == 8 else [0, 0]) + [at]
@@ -667,7 +672,8 @@ class AdamW:
         return None, value.data_ptr()
 
     def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, seed=0):
-        """Step number `step` (from 1 on) with gradients like the parameters, all float32 or all bfloat16, in whole or evenly spaced rows; in place.
+        """Step number `step` (from 1 on) with gradients like the parameters, all float32 or all bfloat16, without gaps or in rows as the parameters are;
+        in place.
         weight_decay: a number, or one per parameter.  step, lr, grad_scale may be tensors of one element on the device (int64, float32,
         float32), which are read when the kernels run: a recorded graph goes on with what they hold then.  seed: of the roundings of
         8-bit states, with the step added to it; not the index_seed of a context."""

@@ -267,3 +267,13 @@ def test_tensors_past_the_cache(bits):
     first = kavg.AdamW([p.clone()])
     first.step([g], 1)
     assert torch.equal(first.params[0][-5:], last.params[0])
+
+
+def test_replicas_without_gaps_and_a_copy_in_wider_rows():
+    """All parameters of all learners as one tensor, the copy in rows of whole eights, as the meta step's shadow."""
+    p, g = normal(1, 3, 517), normal(2, 3, 517, scale=1e-2)
+    shadow = torch.full((3, 520), 7.0, dtype=torch.bfloat16, device="cuda")
+    plan = kavg.AdamW((t for t in [p]), copies=[shadow[:, :517]])
+    for step in (1, 2):
+        check_step(plan, [g], step)
+    assert (shadow[:, 517:] == 7.0).all()

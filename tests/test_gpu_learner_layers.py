@@ -47,7 +47,7 @@ def test_chains(sets, widths, activation, dtype, near):
         plain_chain.append((next(it), next(it) if b is not None else None))
     wide = [(w if sets is None else w[:, None], b) for w, b in plain_chain]
     want = plain_mlp(double[0], wide, activation, double[1])
-    assert y.shape == want.shape and float((y.double() - want).norm()) <= near * float(want.norm())
+    assert y.shape == want.shape and float((y.double() - want).detach().norm()) <= near * float(want.detach().norm())
     dy = normal(3, *y.shape, dtype=dtype)
     got = torch.autograd.grad(y, leaves, dy)
     for g, e, leaf in zip(got, torch.autograd.grad(want, double, dy.double()), leaves):

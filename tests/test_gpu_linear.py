@@ -210,8 +210,8 @@ def test_rows_past_32_bits():
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 def test_on_a_side_stream_and_under_graphs(dtype):
-    """Two graphs, replayed in turns with eager calls between them, on inputs that change."""
-    sizes = [(2, 70, 2000, 48), (1, 200, 64, 72)]
+    """Three graphs, replayed in turns with eager calls between them, on inputs that change."""
+    sizes = [(2, 70, 2000, 48), (1, 200, 64, 72), (1, 4096, 64, 4096)]
     static = [operands(s, dtype) for s in sizes]
     graphs, outs = [], []
     side = torch.cuda.Stream()
@@ -239,7 +239,7 @@ def test_on_a_side_stream_and_under_graphs(dtype):
         for j, s in enumerate(static):
             for t, n in zip(s, operands(sizes[j], dtype, seed=20 + 7 * k + j)):
                 t.copy_(n)
-        for j in (0, 1) if k % 2 else (1, 0):
+        for j in (0, 1, 2) if k % 2 else (2, 1, 0):
             graphs[j].replay()
         torch.cuda.synchronize()
         for j, s in enumerate(static):
