@@ -424,12 +424,12 @@ _WEIGHTS = struct.Struct("=Qqqq")             # kavg_weights
 def _sides(x, weight):
     """(leading dimensions, rows, inputs, outputs) of x [sets, rows, inputs] and weight [sets, outputs, inputs], or both without sets."""
     _dtype(x, "x")
-    shape, of = x.shape, weight.shape
+    shape, of = tuple(x.shape), tuple(weight.shape)           # (slices of a torch.Size take longer)
     if len(shape) not in (2, 3) or len(of) != len(shape) or of[-1] != shape[-1] or of[:-2] != shape[:-2]:
-        _bad("x of %s and weights of %s: [sets, rows, inputs] and [sets, outputs, inputs] or [rows, inputs] and [outputs, inputs] are wanted" % (tuple(shape), tuple(of)))
+        _bad("x of %s and weights of %s: [sets, rows, inputs] and [sets, outputs, inputs] or [rows, inputs] and [outputs, inputs] are wanted" % (shape, of))
     if weight.dtype is not x.dtype or weight.device != x.device:
         _bad("weight is not of x's type and device")
-    return tuple(shape[:-2]), shape[-2], shape[-1], of[-2]
+    return shape[:-2], shape[-2], shape[-1], of[-2]
 
 
 def _product(x, activation, lead, rows, inputs, outputs):
@@ -555,9 +555,8 @@ def kavg_linear_backward(dz, x, weight, activation=KAVG_ACT_NONE, pre=None, out=
 # -- step of a learner ------------------------------------------------------------------------------------------------------
 
 _TENSOR = struct.Struct("=7Q5qfi")            # kavg_adamw_tensor
-_GRAD = struct.Struct("=Q")                   # its gradient (at 8), the gradient's stride (at 80), its weight decay (at 96)
-_STRIDE = struct.Struct("=q")
-_DECAY = struct.Struct("=f")
+_WORDS = _TENSOR.size // 8                    # of 64 bits: its gradient is number 1, the gradient's stride number 10
+_DECAY = struct.Struct("=f")                  # its weight decay, at byte 96
 _STEP = struct.Struct("=iidddddQQQQQ")        # kavg_adamw_options
 _BLOCK = 256                                  # values of an 8-bit state that share a scale
 
@@ -615,6 +614,7 @@ class AdamW:
         self.bits = bits if not self.states else 32 if len(self.states[0]) == 2 else 8
         self.device = self.params[0].device if self.params else None
         self._table = ctypes.create_string_buffer(_TENSOR.size * max(1, len(self.params)))
+        self._words = memoryview(self._table).cast("B").cast("Q")
         self._rows, self._decay, written = [], None, set()
         for i, (p, state, copy) in enumerate(zip(self.params, self.states, self.copies)):
             name = "params[%d]" % i
@@ -689,13 +689,13 @@ class AdamW:
             for i, w in enumerate(each):
                 _DECAY.pack_into(table, i * size + 96, w)
             self._decay = weight_decay if isinstance(weight_decay, (int, float)) else None
-        code, of, device, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, 8
+        code, of, device, words, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, self._words, 1
         for g, (shape, rows, cols) in zip(grads, self._rows):
             if g.dtype is not of or g.shape != shape or g.device != device:
                 _bad("gradients are not of one type, or not of the parameters' shapes and device")
-            _GRAD.pack_into(table, at, g.data_ptr())
-            _STRIDE.pack_into(table, at + 72, cols if g.is_contiguous() else _run(g, "a gradient", rows)[2])
-            at += size
+            words[at] = g.data_ptr()
+            words[at + 9] = cols if g.is_contiguous() else _run(g, "a gradient", rows)[2]
+            at += _WORDS
         number, step_at = self._device_number(step, torch.int64, "step")
         rate, lr_at = self._device_number(lr, torch.float32, "lr")
         scale, scale_at = self._device_number(grad_scale, torch.float32, "grad_scale")
