@@ -3,7 +3,7 @@
 // time, four per lane, which are the values that share the scales of an 8-bit state, so that a block's largest magnitude is six moves between lanes.  The
 // tensors of a launch come as kernel arguments (a table in memory would have to be copied there by every call, or kept).
 // 75M parameters in six tensors with a bf16 copy: 32 bits 360 us (6.3 TB/s; 412, 5.5 TB/s, where the states of three nets are stepped in turn and none of it
-// is in the cache), 8 bits and gradients in bf16 190 (210).  13 small tensors 4.9 of a call of 11, which is the host's.  Steps on the way: streaming
+// is in the cache), 8 bits and gradients in bf16 190 (210).  13 small tensors 3.6 of a call of 10, which is the host's.  Steps on the way: streaming
 // accesses past the cache 427 -> 366 (one tensor); codes and draws of 108 instructions per element, which were as long as the bytes, 240 -> 184.
 #include "adamw.h"
 #include "layers.h"
@@ -17,9 +17,10 @@ namespace kavg {
 namespace {
 
 constexpr int T = 256, BLOCK = 256;
-// Blocks that a wavefront has under way: 75M parameters with 1 / 2 / 4 of them 420 / 420 / 412 us, with states in 8 bits 210 / 217 / 221.
-constexpr int turns_of(int bits) { return bits == 8 ? 1 : 4; }
-constexpr int piece_of(int bits) { return T * 4 * turns_of(bits); }
+// Blocks that a wavefront has under way: 75M parameters with 1 / 2 / 4 of them 420 / 420 / 412 us, with states in 8 bits 210 / 217 / 221.  In the cache more
+// wavefronts do better: 13 small tensors 3.6 for 4.9 us with 1 for 4 of them, 8M parameters 53 for 54.
+constexpr int turns_of(int bits, bool stream) { return bits == 32 && stream ? 4 : 1; }
+constexpr int piece_of(int bits, bool stream) { return T * 4 * turns_of(bits, stream); }
 constexpr double CACHE = 256e6;                  // bytes behind the L2: tensors of more are gone by the next step
 constexpr int MOST_TENSORS = 32;                 // of a launch: its arguments stay below four kilobytes
 
@@ -194,7 +195,7 @@ __device__ __forceinline__ void step_piece(const AdamwTensor& t, const AdamwRule
     const G* grad = (const G*)t.grad + row * t.grad_stride + first;
     const float decay = (float)(1. - rule.lr * t.decay);
     const uint64_t draw0 = rule.seed + (1 + ((uint64_t)t.site << 40) + ((uint64_t)states >> 2)) * SPLITMIX_GAMMA;      // of the first lane
-    constexpr int APART = T / 64 * BLOCK, TURNS = turns_of(BITS);
+    constexpr int APART = T / 64 * BLOCK, TURNS = turns_of(BITS, STREAM);
     Four p[TURNS], g[TURNS], m[TURNS], v[TURNS];
     uint32_t mc[TURNS], vc[TURNS];
     float ms[TURNS], vs[TURNS];
@@ -311,8 +312,8 @@ __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
         }
         const AdamwTensor& t = table.tensor[lo];
         const uint32_t in = piece - table.first[lo], row = in / t.pieces;
-        const int64_t begin = (int64_t)(in - row * t.pieces) * piece_of(BITS), first = begin + wave * BLOCK;
-        if (begin + piece_of(BITS) <= t.cols) step_piece<BITS, G, STREAM, true>(t, rule, row, first, lane, lane_draw);
+        const int64_t begin = (int64_t)(in - row * t.pieces) * piece_of(BITS, STREAM), first = begin + wave * BLOCK;
+        if (begin + piece_of(BITS, STREAM) <= t.cols) step_piece<BITS, G, STREAM, true>(t, rule, row, first, lane, lane_draw);
         else if (first < t.cols) step_piece<BITS, G, STREAM, false>(t, rule, row, first, lane, lane_draw);
     }
 }
@@ -352,7 +353,7 @@ hipError_t launch_adamw(int bits, int grad_dtype, const AdamwRule& given, const 
             a.cols *= t.rows;
             a.rows = 1;
         }
-        a.pieces = (uint32_t)((a.cols + piece_of(bits) - 1) / piece_of(bits));
+        a.pieces = (uint32_t)((a.cols + piece_of(bits, stream) - 1) / piece_of(bits, stream));
         const uint64_t more = (uint64_t)a.rows * a.pieces;              // below 2^32, from the limits of the call
         if (table.count == MOST_TENSORS || table.first[table.count] + more >= (uint64_t)1 << 31) flush();
         table.tensor[table.count] = a;
