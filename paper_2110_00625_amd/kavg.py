@@ -682,13 +682,17 @@ class AdamW:
             _bad("%d gradients of %d parameters" % (len(grads), len(self.params)))
         if not self.params:
             return
-        if self._decay != weight_decay:
-            each = [float(weight_decay)] * len(self.params) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        single = isinstance(weight_decay, (int, float))
+        if not single or self._decay != weight_decay:
+            try:                                                  # (all of them before the table changes)
+                each = [_DECAY.pack(w) for w in ([weight_decay] * len(self.params) if single else weight_decay)]
+            except (struct.error, TypeError, OverflowError) as e:
+                _bad("weight_decay: %s" % e)
             if len(each) != len(self.params):
                 _bad("%d weight decays of %d parameters" % (len(each), len(self.params)))
             for i, w in enumerate(each):
-                _DECAY.pack_into(table, i * size + 96, w)
-            self._decay = weight_decay if isinstance(weight_decay, (int, float)) else None
+                table[i * size + 96:i * size + 100] = w
+            self._decay = weight_decay if single else None
         code, of, device, words, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, self._words, 1
         for g, (shape, rows, cols) in zip(grads, self._rows):
             if g.dtype is not of or g.shape != shape or g.device != device:

@@ -277,3 +277,16 @@ def test_replicas_without_gaps_and_a_copy_in_wider_rows():
     for step in (1, 2):
         check_step(plan, [g], step)
     assert (shadow[:, 517:] == 7.0).all()
+
+
+def test_refused_weight_decays_leave_those_of_before():
+    params = [normal(80 + i, 70) for i in range(2)]
+    before = [p.clone() for p in params]
+    plan, grads = kavg.AdamW(params), [torch.zeros_like(p) for p in params]
+    plan.step(grads, 1, weight_decay=0.0)
+    for wrong in ([0.5, 1e300], [0.5], [0.5, None], 1e300):
+        with pytest.raises(kavg.KavgError):
+            plan.step(grads, 2, weight_decay=wrong)
+        plan.step(grads, 2, weight_decay=0.0)
+        # (zero gradients and moments: the change is 0 / eps, the decay's factor 1)
+        assert all(torch.equal(p, b) for p, b in zip(params, before)), wrong
