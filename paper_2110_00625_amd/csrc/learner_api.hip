@@ -146,35 +146,33 @@ int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const
     if (!empty(p) && dx && (shares(dx, dz->data) || dx->data == weight->data)) return KAVG_EINVAL;
     if (!empty(p) && dx && slope && shares(pre, dx->data) && ((p->rows > 1 && pre->row_stride != dx->row_stride) || (p->sets > 1 && pre->set_stride != dx->set_stride))) return KAVG_EINVAL;
     if (!p->sets) return KAVG_OK;
-    hipError_t e = hipSuccess;
-    // the weight gradient first: dx may lie where x does
-    if (dweight || dbias) {
-        ProductCall c = {};
-        c.dtype = p->dtype; c.sets = p->sets;
-        c.nK = (int)p->rows;
-        c.r_turned = c.c_turned = true;
-        c.finish.floor = -INFINITY;
-        c.sums = dbias; c.sums_set = p->sets > 1 ? dbias_stride : 0;
+    const bool outer = dweight || dbias, inner = dx && p->rows;
+    ProductCall w = {}, c = {};
+    if (outer) {
+        w.dtype = p->dtype; w.sets = p->sets;
+        w.nK = (int)p->rows;
+        w.r_turned = w.c_turned = true;
+        w.finish.floor = -INFINITY;
+        w.sums = dbias; w.sums_set = p->sets > 1 ? dbias_stride : 0;
         const Matrix of_dz = matrix_of(p, dz, p->outputs);
         const bool other = dweight && turned(p, dweight);                // dW lies as [inputs][outputs]
         if (other) {
-            c.nR = (int)p->inputs; c.nC = (int)p->outputs;
-            c.R = matrix_of(p, x, p->inputs); c.C = of_dz;
-            c.side = dbias ? 2 : 0;
+            w.nR = (int)p->inputs; w.nC = (int)p->outputs;
+            w.R = matrix_of(p, x, p->inputs); w.C = of_dz;
+            w.side = dbias ? 2 : 0;
         } else {
-            c.nR = (int)p->outputs; c.nC = dweight ? (int)p->inputs : 0;
-            c.R = of_dz;
-            if (dweight) c.C = matrix_of(p, x, p->inputs);
-            c.side = dbias ? 1 : 0;
+            w.nR = (int)p->outputs; w.nC = dweight ? (int)p->inputs : 0;
+            w.R = of_dz;
+            if (dweight) w.C = matrix_of(p, x, p->inputs);
+            w.side = dbias ? 1 : 0;
         }
         if (dweight) {
             const Matrix m = matrix_of(p, dweight);
-            c.finish.out = dweight->data; c.finish.out_set = m.set_stride; c.finish.out_row = m.stride;
+            w.finish.out = dweight->data; w.finish.out_set = m.set_stride; w.finish.out_row = m.stride;
         }
-        e = launch_product(c, workspace, workspace_bytes, (hipStream_t)hip_stream);
     }
-    if (dx && p->rows && e == hipSuccess) {
-        ProductCall c = inner_of(p);
+    if (inner) {
+        c = inner_of(p);
         c.R = matrix_of(p, dz, p->outputs);
         c.C = matrix_of(p, weight);
         c.c_turned = !turned(p, weight);
@@ -182,8 +180,11 @@ int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const
         if (slope) { const Matrix m = matrix_of(p, pre, p->inputs); f.before = pre->data; f.before_set = m.set_stride; f.before_row = m.stride; }
         const Matrix m = matrix_of(p, dx, p->inputs);
         f.out = dx->data; f.out_set = m.set_stride; f.out_row = m.stride;
-        e = launch_product(c, workspace, workspace_bytes, (hipStream_t)hip_stream);
     }
+    // the weight gradient first: dx may lie where x does; but nothing if the block is too small for dx
+    hipError_t e = inner && outer ? check_product(c, workspace, workspace_bytes) : hipSuccess;
+    if (outer && e == hipSuccess) e = launch_product(w, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    if (inner && e == hipSuccess) e = launch_product(c, workspace, workspace_bytes, (hipStream_t)hip_stream);
     return status(e);
 }
 

@@ -48,6 +48,7 @@ enum Turned { NONE_TURNED, C_TURNED, BOTH_TURNED };        // the last: a weight
 Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned);
 // hipErrorOutOfMemory, hipErrorInvalidValue: a workspace too small, misaligned or not there, before anything is launched
 hipError_t launch_product(const ProductCall& c, void* workspace, size_t bytes, hipStream_t st);
+hipError_t check_product(const ProductCall& c, const void* workspace, size_t bytes);       // the same, without the launch
 
 #if defined(__HIPCC__)
 template <class E, int V> __device__ __forceinline__ void load_some(const E* p, int n, float (&v)[V]) {

@@ -142,28 +142,58 @@ Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned
     return p;
 }
 
+namespace {
+
+enum class Way { ROWS, COLUMNS, TILES };
+struct Course { Way way; bool direct; Plan plan; };
+
+// Which kernel a product takes.
+Course course_of(const ProductCall& call) {
+    const bool bf16 = call.dtype == KAVG_BF16;
+    const int elem = bf16 ? 2 : 4;
+    Course c = {Way::TILES, false, {}};
+    c.direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
+               aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
+    if (c.direct && !call.r_turned && !call.c_turned) {
+        // Larger matrices in bf16 come faster through tiles, whose loads never pause (4 rows of 4096x4096 7.5 us and 9.5 through tiles, of 4096x8192 15.6 and
+        // 15.5, of 4096x16384 27.6 and 21.2; 16 rows of 4096x4096 in fp32 17 and 26, which its products take).
+        auto fits = [&](int64_t lines) { return call.sets * up(lines, 16) <= MOST_TILES && (!bf16 || call.sets * lines * call.nK <= MOST_ELEMENTS); };
+        if (call.nR <= MOST_ROWS && fits(call.nC)) c.way = Way::ROWS;
+        // (every wavefront has a part of the contraction)
+        else if (call.nC <= MOST_ROWS && call.nK >= 8 * slice_of(call.dtype) && fits(call.nR)) c.way = Way::COLUMNS;
+    }
+    if (c.way == Way::TILES)
+        c.plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned ? BOTH_TURNED : call.c_turned ? C_TURNED : NONE_TURNED);
+    return c;
+}
+
+hipError_t workspace_ok(const Plan& plan, const void* workspace, size_t bytes) {
+    if (plan.splits < 2) return hipSuccess;
+    if (bytes < plan.bytes) return hipErrorOutOfMemory;
+    return !workspace || ((uintptr_t)workspace & 15) ? hipErrorInvalidValue : hipSuccess;
+}
+
+}  // namespace
+
+hipError_t check_product(const ProductCall& call, const void* workspace, size_t bytes) {
+    return workspace_ok(course_of(call).plan, workspace, bytes);
+}
+
 hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes, hipStream_t st) {
     const bool bf16 = call.dtype == KAVG_BF16;
     const int elem = bf16 ? 2 : 4;
-    const bool direct = call.nC && call.nK && aligned(call.R, call.sets, call.r_turned ? call.nK : call.nR, call.r_turned ? call.nR : call.nK, elem) &&
-                        aligned(call.C, call.sets, call.c_turned ? call.nK : call.nC, call.c_turned ? call.nC : call.nK, elem);
-    if (direct && !call.r_turned && !call.c_turned) {
+    const Course course = course_of(call);
+    if (course.way != Way::TILES) {
         ProductArgs a = {};
         a.R = call.R; a.C = call.C;
         a.nR = call.nR; a.nC = call.nC; a.nK = call.nK;
         a.finish = call.finish;
-        // Larger matrices in bf16 come faster through tiles, whose loads never pause (4 rows of 4096x4096 7.5 us and 9.5 through tiles, of 4096x8192 15.6 and
-        // 15.5, of 4096x16384 27.6 and 21.2; 16 rows of 4096x4096 in fp32 17 and 26, which its products take).
-        auto fits = [&](int64_t lines) { return call.sets * up(lines, 16) <= MOST_TILES && (!bf16 || call.sets * lines * call.nK <= MOST_ELEMENTS); };
-        if (call.nR <= MOST_ROWS && fits(call.nC)) return start_rows(call.dtype, a, call.sets, st);
-        // (every wavefront has a part of the contraction)
-        if (call.nC <= MOST_ROWS && call.nK >= 8 * slice_of(call.dtype) && fits(call.nR)) return start_columns(call.dtype, a, call.sets, st);
+        return course.way == Way::ROWS ? start_rows(call.dtype, a, call.sets, st) : start_columns(call.dtype, a, call.sets, st);
     }
-    const Plan plan = product_plan(call.dtype, call.sets, call.nR, call.nC, call.nK, call.r_turned ? BOTH_TURNED : call.c_turned ? C_TURNED : NONE_TURNED);
-    if (plan.splits > 1) {
-        if (bytes < plan.bytes) return hipErrorOutOfMemory;
-        if (!workspace || ((uintptr_t)workspace & 15)) return hipErrorInvalidValue;
-    }
+    const Plan& plan = course.plan;
+    const bool direct = course.direct;
+    const hipError_t fits = workspace_ok(plan, workspace, bytes);
+    if (fits != hipSuccess) return fits;
     const int tile = direct ? plan.tile : plan.tile == TILE_LARGE ? TILE_MIDDLE : plan.tile == TILE_DEEP ? TILE_SMALL : plan.tile;
     const Size size = tile_size(tile);
 

@@ -162,3 +162,13 @@ def test_binding_refuses_what_does_not_fit(lib):  # noqa: F811
         with pytest.raises(kavg.KavgError) as e:
             call()
         assert e.value.code == E, k
+
+
+def test_backward_that_has_a_block_for_its_first_product_alone(lib):  # noqa: F811
+    # dW = dz^T x over 64 rows is not split, dx = dz W over 8192 outputs is: refused before either is launched (without a GPU the launch would say so)
+    p = product(sets=1, rows=64, inputs=64, outputs=8192)
+    size = ctypes.c_size_t(0)
+    assert lib.kavg_linear_workspace(p, 1, ctypes.byref(size)) == OK and size.value > 0
+    dz, x, w, dx, dw = rows(row=8192), rows(3 * AT, row=64), weights(o=64), rows(AWAY, row=64), weights(2 * AWAY, o=64)
+    for block, nbytes, rc in ((AWAY, size.value - 1, kavg.KAVG_ENOMEM), (AWAY, 0, kavg.KAVG_ENOMEM), (None, 0, kavg.KAVG_ENOMEM), (None, size.value, E), (AWAY + 4, size.value, E)):
+        assert backward(lib, p, dz=dz, x=x, w=w, dx=dx, dw=dw, block=block, nbytes=nbytes) == rc
