@@ -375,7 +375,8 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
         }
     }
     // Results leave through LDS, by wavefront: 32 rows of its columns at a time, so that the lanes of a row write whole lines (and the code is there once
-    // for eight columns of a lane, not for every register).
+    // for eight columns of a lane, not for every register).  The hardware keeps a wavefront's accesses to LDS in order; the fences keep the compiler, to which a
+    // lane's reads are of other places than its writes, from exchanging them.
     constexpr int WTC = MC * 32, PITCH = P::PITCH, ROW_LANES = WTC / 8, ROWS = 64 / ROW_LANES, TURNS = 32 / ROWS;
     __syncthreads();
     float* stage = (float*)lds + wave * 32 * PITCH;
@@ -388,12 +389,14 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
             for (int j = 0; j < MC; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) *(f32x4*)(stage + (lane & 31) * PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = (f32x4){acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
             finish(r0 + (wr * MR + i) * 32 + down, ROWS, a.nR, [&](int u, float (&v)[8]) {
                 const float* from = stage + (down + u * ROWS) * PITCH + col;
                 const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + apart.value);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) { v[k] = lo[k]; v[4 + k] = hi[k]; }
             });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
         }
     };
     typedef typename std::conditional<RT, float, E>::type O;

@@ -37,3 +37,23 @@ def test_long_contractions(size, dtype, turned):
     pre = normal(9, *x.shape, dtype=dtype)
     for got, want in zip(kavg.kavg_linear_backward(dz, x, at, activation=CODE["relu"], pre=pre), L.linear_backward(dz, x, w, "relu", pre, dtype)):
         L.close(got, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
+@pytest.mark.parametrize("rows,n", [(40, 64), (200, 512), (8192, 256), (2048, 1024), (4096, 2048), (16384, 1024), (515, 1003)], ids=str)
+def test_results_stay_in_their_places(rows, n, dtype):
+    """Products with a permutation: every result is one value of the other operand, whole numbers that neighbours within 200 rows and columns do not share, to the
+    last bit.  A result that left from another lane's place, or from the block before, would be another number."""
+    x = ((torch.arange(rows, device="cuda")[:, None] * 17 + torch.arange(n, device="cuda") * 29) % 251).to(dtype)
+    order = torch.randperm(n, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    w = torch.eye(n, device="cuda")[order].to(dtype)
+    for at in (w, w.t().contiguous().t()):
+        y, z = kavg.kavg_linear(x, at, activation=CODE["relu"], pre=True)
+        assert torch.equal(y, x[:, order]) and torch.equal(z, y)
+        assert torch.equal(kavg.kavg_linear_backward(y, x, at, dweight=False, dbias=False)[0], x)
+    pick = torch.randperm(rows, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")[:min(rows, n)]
+    one = torch.zeros(rows, pick.numel(), dtype=dtype, device="cuda")
+    one[pick, torch.arange(pick.numel(), device="cuda")] = 1
+    for dw in (None, torch.empty(n, pick.numel(), device="cuda").t()):
+        got = kavg.kavg_linear_backward(one, x, torch.zeros(pick.numel(), n, dtype=dtype, device="cuda"), out=False, dweight=dw)
+        assert torch.equal(got[1], x[pick].float()) and (got[2] == 1).all()
