@@ -454,7 +454,8 @@ int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const
  * rows of the replicas: a tensor's rows are the learners).  With g = grad_scale * gradient, t = step,
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
- * in fp32, every operation of the first line rounded by itself; copy, where there is one, gets p as bf16 (nearest, ties
+ * in fp32 (an eps that has no normal reciprocal in fp32 counts as it is; one of 0 leaves 0 / 0 where nothing has moved), every operation of
+ * the first line rounded by itself; copy, where there is one, gets p as bf16 (nearest, ties
  * away from zero, as kavg_meta_update_flat's shadow).
  *
  * bits 32: m and v are fp32.  bits 8: m and the root r = sqrt(v) are e4m3 (no infinities, 448 the largest), one byte per

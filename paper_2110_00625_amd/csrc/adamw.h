@@ -17,7 +17,8 @@ struct AdamwRule {
     float beta1, rest1, beta2, rest2, eps;       // rest = 1 - beta
     float rate, root_scale, grad_scale;          // rate = lr / (1 - beta1^t), root_scale = 1 / sqrt(1 - beta2^t)
     uint64_t step, seed;                         // seed: the step added to it (by the kernel, where that is in device memory)
-    double lr, exact1, exact2;                   // exact: the betas, for a step in device memory
+    double lr, exact1, exact2, exact_eps;        // exact: the betas, for a step in device memory, and eps, for one outside of these limits:
+    bool wide;                                   // eps is so small or so large that one of eps and 1 / eps is no normal number of fp32
     const int64_t* step_dev; const float* lr_dev; const float* grad_scale_dev;
 };
 

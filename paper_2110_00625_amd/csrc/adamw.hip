@@ -180,15 +180,17 @@ __device__ __forceinline__ void moments(const AdamwRule& r, float g, float& m, f
     v = v * r.beta2 + (g * g) * r.rest2;
     root = __builtin_sqrtf(v);
 }
-// The parameter, with the hardware's reciprocal (one unit in the last place of the change; the denominator is normal, zero or infinite: a root of
-// fp32 is).
-__device__ __forceinline__ float stepped(const AdamwRule& r, float p, float decay, float m, float root) {
+// The parameter, with the hardware's reciprocal (one unit in the last place of the change), which takes and gives no subnormal numbers.  The denominator is
+// normal, zero or infinite where eps is: a root of fp32 is normal or zero, and its factor is 1 at least; where eps lies outside of what has a normal
+// reciprocal the quotient is taken in 64 bits.
+template <bool WIDE> __device__ __forceinline__ float stepped(const AdamwRule& r, float p, float decay, float m, float root) {
+    if (WIDE) return (float)((double)p * decay - r.rate * (m / ((double)root * r.root_scale + r.exact_eps)));
     const float change = m * __builtin_amdgcn_rcpf(__builtin_fmaf(root, r.root_scale, r.eps));
     return __builtin_fmaf(p, decay, -(r.rate * change));
 }
 
 // One wavefront's part of a piece: TURNS blocks of its row, the t-th from `first` + t T/64 BLOCK on.  WHOLE: all of them are there.
-template <int BITS, class G, bool STREAM, bool WHOLE>
+template <int BITS, class G, bool STREAM, bool WIDE, bool WHOLE>
 __device__ __forceinline__ void step_piece(const AdamwTensor& t, const AdamwRule& rule, uint32_t row, int64_t first, int lane, uint64_t lane_draw) {
     const int64_t states = row * t.cols + first, blocks = (t.cols + BLOCK - 1) / BLOCK, left = t.cols - first;
     float* param = t.param + row * t.param_stride + first;
@@ -231,7 +233,7 @@ __device__ __forceinline__ void step_piece(const AdamwTensor& t, const AdamwRule
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             moments(rule, g[i].v[k] * rule.grad_scale, m[i].v[k], v[i].v[k], root.v[k]);
-            p[i].v[k] = stepped(rule, p[i].v[k], decay, m[i].v[k], root.v[k]);
+            p[i].v[k] = stepped<WIDE>(rule, p[i].v[k], decay, m[i].v[k], root.v[k]);
         }
         store_four<STREAM>(param + at, p[i], n[i]);
         if (t.copy) {
@@ -291,7 +293,7 @@ __device__ __forceinline__ void step_piece(const AdamwTensor& t, const AdamwRule
     }
 }
 
-template <int BITS, class G, bool STREAM>
+template <int BITS, class G, bool STREAM, bool WIDE>
 __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (rule.lr_dev) rule.lr = *rule.lr_dev;
@@ -313,16 +315,17 @@ __global__ void __launch_bounds__(T) adamw_kernel(Table table, AdamwRule rule) {
         const AdamwTensor& t = table.tensor[lo];
         const uint32_t in = piece - table.first[lo], row = in / t.pieces;
         const int64_t begin = (int64_t)(in - row * t.pieces) * piece_of(BITS, STREAM), first = begin + wave * BLOCK;
-        if (begin + piece_of(BITS, STREAM) <= t.cols) step_piece<BITS, G, STREAM, true>(t, rule, row, first, lane, lane_draw);
-        else if (first < t.cols) step_piece<BITS, G, STREAM, false>(t, rule, row, first, lane, lane_draw);
+        if (begin + piece_of(BITS, STREAM) <= t.cols) step_piece<BITS, G, STREAM, WIDE, true>(t, rule, row, first, lane, lane_draw);
+        else if (first < t.cols) step_piece<BITS, G, STREAM, WIDE, false>(t, rule, row, first, lane, lane_draw);
     }
 }
 
 template <int BITS, class G>
 hipError_t start(const Table& table, const AdamwRule& rule, bool stream, hipStream_t st) {
     const dim3 grid(std::min<uint32_t>(table.first[table.count], 1u << 22));
-    if (stream) adamw_kernel<BITS, G, true><<<grid, dim3(T), 0, st>>>(table, rule);
-    else adamw_kernel<BITS, G, false><<<grid, dim3(T), 0, st>>>(table, rule);
+    if (rule.wide) adamw_kernel<BITS, G, false, true><<<grid, dim3(T), 0, st>>>(table, rule);
+    else if (stream) adamw_kernel<BITS, G, true, false><<<grid, dim3(T), 0, st>>>(table, rule);
+    else adamw_kernel<BITS, G, false, false><<<grid, dim3(T), 0, st>>>(table, rule);
     return hipGetLastError();
 }
 
@@ -333,7 +336,7 @@ hipError_t launch_adamw(int bits, int grad_dtype, const AdamwRule& given, const 
     if (!rule.step_dev) { at_step(rule, rule.step); rule.seed += rule.step; }
     double bytes = 0.;
     for (int i = 0; i < count; ++i) bytes += (double)tensors[i].rows * tensors[i].cols * (4 + (grad_dtype == KAVG_BF16 ? 2 : 4) + bits / 4);
-    const bool stream = bytes > CACHE;
+    const bool stream = bytes > CACHE && !rule.wide;
     Table table;
     table.count = 0;
     table.first[0] = 0;

@@ -211,7 +211,8 @@ int kavg_adamw(const kavg_adamw_options* options, const kavg_adamw_tensor* tenso
     rule.eps = (float)o->eps;
     rule.grad_scale = (float)o->grad_scale;
     rule.step = o->step; rule.seed = o->seed;
-    rule.lr = o->lr; rule.exact1 = o->beta1; rule.exact2 = o->beta2;
+    rule.lr = o->lr; rule.exact1 = o->beta1; rule.exact2 = o->beta2; rule.exact_eps = o->eps;
+    rule.wide = o->eps != 0. && (o->eps < 0x1p-126 || o->eps > 0x1p126);
     rule.step_dev = o->step_dev; rule.lr_dev = o->lr_dev; rule.grad_scale_dev = o->grad_scale_dev;
     return status(launch_adamw(o->bits, o->grad_dtype, rule, tensors, count, (hipStream_t)hip_stream));
 }
