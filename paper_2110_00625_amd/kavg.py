@@ -596,7 +596,10 @@ class AdamW:
 
     states: per parameter (m, v) of 32 bits, float32 and like the parameter without gaps, or (m, v, m_scale, v_scale) of 8 bits, float8_e4m3fn
     and float32 [rows, blocks of 256 of a row]; v of 8 bits holds the root of the second moment.  Made by `zeros` if not given, of
-    `bits`, with a row per learner where the parameter lies in rows.  They are `self.states`, written by every step."""
+    `bits`, with a row per learner where the parameter lies in rows.  `self.states` are the memory that every step writes; a state is loaded by copying into it.
+
+    The table holds addresses.  A step refuses parameters or copies that have got other memory since (`p.data = ..`, a module's `.to(..)`, other entries
+    of the lists): make another AdamW of them, with these states."""
 
     def __init__(self, params, states=None, copies=None, bits=32):
         torch = _torch_module or _torch()
@@ -608,15 +611,16 @@ class AdamW:
             _dtype(p, "params[%d]" % i)
         if states is None:
             states = [self.zeros(p, bits) for p in self.params]
-        self.states = [tuple(s) for s in states]
-        if len(self.states) != len(self.params) or len(self.copies) != len(self.params) or len({len(s) for s in self.states}) > 1:
-            _bad("%d parameters, %d states, %d copies" % (len(self.params), len(self.states), len(self.copies)))
-        self.bits = bits if not self.states else 32 if len(self.states[0]) == 2 else 8
+        states = [tuple(s) for s in states]
+        if len(states) != len(self.params) or len(self.copies) != len(self.params) or len({len(s) for s in states}) > 1:
+            _bad("%d parameters, %d states, %d copies" % (len(self.params), len(states), len(self.copies)))
+        self.bits = bits if not states else 32 if len(states[0]) == 2 else 8
         self.device = self.params[0].device if self.params else None
+        self._copied = any(c is not None for c in self.copies)
         self._table = ctypes.create_string_buffer(_TENSOR.size * max(1, len(self.params)))
         self._words = memoryview(self._table).cast("B").cast("Q")
         self._rows, self._decay, written = [], None, set()
-        for i, (p, state, copy) in enumerate(zip(self.params, self.states, self.copies)):
+        for i, (p, state, copy) in enumerate(zip(self.params, states, self.copies)):
             name = "params[%d]" % i
             if p.dtype is not torch.float32 or p.device != self.device:
                 _bad("%s is not a float32 tensor on the device of the others" % name)
@@ -640,6 +644,19 @@ class AdamW:
                 written.add(a)
             _TENSOR.pack_into(self._table, i * _TENSOR.size, *pointers, rows, cols, stride, cols, cs, 0.0, 0)
             self._rows.append((p.shape, rows, cols))
+        # What the table points to stays allocated, whatever becomes of the tensors given: states are written where they were, parameters and copies, which others
+        # read through those tensors, are looked at by every step.
+        self._states = [tuple(s.detach() for s in state) for state in states]
+        self._memory = [t.detach() for t in self.params + self.copies if t is not None]
+        self._at = self._addresses()
+
+    @property
+    def states(self):
+        return [tuple(s.detach() for s in state) for state in self._states]
+
+    def _addresses(self):
+        at = list(map(_torch_module.Tensor.data_ptr, self.params))
+        return at + [None if c is None else c.data_ptr() for c in self.copies] if self._copied else at
 
     @staticmethod
     def zeros(p, bits=32):
@@ -680,6 +697,12 @@ class AdamW:
         torch, table, size = _torch_module, self._table, _TENSOR.size
         if len(grads) != len(self.params):
             _bad("%d gradients of %d parameters" % (len(grads), len(self.params)))
+        try:
+            moved = self._addresses() != self._at
+        except (AttributeError, TypeError):                       # (an entry that is no tensor any more)
+            moved = True
+        if moved:
+            _bad("a parameter or a copy has got other memory since the table was made")
         if not self.params:
             return
         single = isinstance(weight_decay, (int, float))
