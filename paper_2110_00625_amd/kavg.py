@@ -649,6 +649,8 @@ class AdamW:
         self._states = [tuple(s.detach() for s in state) for state in states]
         self._memory = [t.detach() for t in self.params + self.copies if t is not None]
         self._at = self._addresses()
+        # (views of one tensor have its version)
+        self._versions = list({id(t): t for t in (t._base if t._is_view() else t for t in self.params + self.copies if t is not None)}.values())
 
     @property
     def states(self):
@@ -734,6 +736,8 @@ class AdamW:
         rc = _launch(self.params[0], _lib.kavg_adamw, options, ctypes.addressof(table), len(self.params))
         if rc != KAVG_OK:
             _failed("kavg_adamw", rc)
+        # (a backward pass that wants the values of before says so)
+        torch.autograd.graph.increment_version(self._versions)
 
 
 class MAvg:

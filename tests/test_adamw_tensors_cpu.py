@@ -86,3 +86,31 @@ def test_states_are_written_where_they_were(launched, bits):
     plan.step([torch.zeros_like(p)], 1)
     assert list(launched[-1][0][2:4 if bits == 32 else 6]) == [s.data_ptr() for s in plan.states[0]]
     assert plan.states[0][1].shape == p.shape and mine.data_ptr() != plan.states[0][0].data_ptr()
+
+
+def test_a_step_is_a_change_of_its_tensors_for_autograd(launched):
+    """A graph that saved a parameter, a view of one, what it is a view of, or a copy, refuses its backward pass after a step, as after any change in place."""
+    def of(kind):
+        whole = torch.ones(3, 40)
+        view = whole[:, 4:24].view(3, 4, 5)
+        p = {"parameter": torch.nn.Parameter(torch.ones(3, 20)), "view": view, "base": view, "view of a view": view[:, 1:3], "detached": view.detach(), "copy": torch.ones(3, 20)}[kind]
+        copy = torch.ones(3, 20, dtype=torch.bfloat16)
+        return p, copy, {"base": whole, "copy": copy}.get(kind, p)
+    for kind in ("parameter", "view", "base", "view of a view", "detached", "copy"):
+        p, copy, saved = of(kind)
+        plan = kavg.AdamW([p], copies=[copy] if kind == "copy" else None)
+        x = torch.ones(saved.shape, dtype=saved.dtype, requires_grad=True)
+        before, graph = saved._version, (x * saved.detach()).sum()
+        plan.step([torch.zeros(p.shape)], 1)
+        assert saved._version > before, kind
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            graph.backward()
+        plan.step([torch.zeros(p.shape)], 2)
+        (x * saved.detach()).sum().backward()
+    with torch.inference_mode():
+        p = torch.ones(5)
+        kavg.AdamW([p]).step([torch.zeros(5)], 1)
+    plan = kavg.AdamW([torch.ones(5)])
+    version = plan.params[0]._version
+    refused(lambda: plan.step([torch.zeros(6)], 1))
+    assert plan.params[0]._version == version
