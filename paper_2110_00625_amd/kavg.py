@@ -719,12 +719,15 @@ class AdamW:
                 table[i * size + 96:i * size + 100] = w
             self._decay = weight_decay if single else None
         code, of, device, words, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, self._words, 1
-        for g, (shape, rows, cols) in zip(grads, self._rows):
-            if g.dtype is not of or g.shape != shape or g.device != device:
-                _bad("gradients are not of one type, or not of the parameters' shapes and device")
-            words[at] = g.data_ptr()
-            words[at + 9] = cols if g.is_contiguous() else _run(g, "a gradient", rows)[2]
-            at += _WORDS
+        try:
+            for g, (shape, rows, cols) in zip(grads, self._rows):
+                if g.dtype is not of or g.shape != shape or g.device != device:
+                    _bad("gradients are not of one type, or not of the parameters' shapes and device")
+                words[at] = g.data_ptr()
+                words[at + 9] = cols if g.is_contiguous() else _run(g, "a gradient", rows)[2]
+                at += _WORDS
+        except AttributeError:
+            _bad("a gradient is no tensor")
         number, step_at = self._device_number(step, torch.int64, "step")
         rate, lr_at = self._device_number(lr, torch.float32, "lr")
         scale, scale_at = self._device_number(grad_scale, torch.float32, "grad_scale")

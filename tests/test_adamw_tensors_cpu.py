@@ -114,3 +114,12 @@ def test_a_step_is_a_change_of_its_tensors_for_autograd(launched):
     version = plan.params[0]._version
     refused(lambda: plan.step([torch.zeros(6)], 1))
     assert plan.params[0]._version == version
+
+
+@pytest.mark.parametrize("wrong", (None, 0.0, [0.0] * 7))
+def test_what_is_no_gradient_is_refused_wherever_it_stands(launched, wrong):
+    params = [torch.ones(7), torch.ones(7), torch.ones(7)]
+    plan = kavg.AdamW(params)
+    for i in (1, 2):
+        refused(lambda: plan.step([wrong if k == i else torch.zeros(7) for k in range(3)], 1))
+    assert not launched
