@@ -616,10 +616,11 @@ class AdamW:
             _bad("%d parameters, %d states, %d copies" % (len(self.params), len(states), len(self.copies)))
         self.bits = bits if not states else 32 if len(states[0]) == 2 else 8
         self.device = self.params[0].device if self.params else None
+        self._index = self.params[0].get_device() if self.params else None
         self._copied = any(c is not None for c in self.copies)
         self._table = ctypes.create_string_buffer(_TENSOR.size * max(1, len(self.params)))
         self._words = memoryview(self._table).cast("B").cast("Q")
-        self._rows, self._decay, written = [], None, set()
+        self._rows, self._decay, self._strided, written = [], None, False, set()
         for i, (p, state, copy) in enumerate(zip(self.params, states, self.copies)):
             name = "params[%d]" % i
             if p.dtype is not torch.float32 or p.device != self.device:
@@ -684,7 +685,7 @@ class AdamW:
 
     def _device_number(self, value, dtype, name):
         """(number, address) of a host's number or of a tensor of one element."""
-        if not isinstance(value, _torch_module.Tensor):
+        if type(value) in (int, float) or not isinstance(value, _torch_module.Tensor):
             return value, 0
         if value.dtype is not dtype or value.numel() != 1 or value.device != self.device:
             _bad("%s is neither a number nor one %s on the parameters' device" % (name, dtype))
@@ -718,13 +719,18 @@ class AdamW:
             for i, w in enumerate(each):
                 table[i * size + 96:i * size + 100] = w
             self._decay = weight_decay if single else None
-        code, of, device, words, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self.device, self._words, 1
+        code, of, index, words, at = _dtype(grads[0], "grads[0]"), grads[0].dtype, self._index, self._words, 1
+        strided = self._strided                                   # (once a gradient lay in rows, the table's strides are written again)
         try:
             for g, (shape, rows, cols) in zip(grads, self._rows):
-                if g.dtype is not of or g.shape != shape or g.device != device:
+                if g.dtype is not of or g.shape != shape or g.get_device() != index:
                     _bad("gradients are not of one type, or not of the parameters' shapes and device")
                 words[at] = g.data_ptr()
-                words[at + 9] = cols if g.is_contiguous() else _run(g, "a gradient", rows)[2]
+                if not g.is_contiguous():
+                    self._strided = strided = True
+                    words[at + 9] = _run(g, "a gradient", rows)[2]
+                elif strided:
+                    words[at + 9] = cols
                 at += _WORDS
         except AttributeError:
             _bad("a gradient is no tensor")

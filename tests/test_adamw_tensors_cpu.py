@@ -123,3 +123,13 @@ def test_what_is_no_gradient_is_refused_wherever_it_stands(launched, wrong):
     for i in (1, 2):
         refused(lambda: plan.step([wrong if k == i else torch.zeros(7) for k in range(3)], 1))
     assert not launched
+
+
+def test_gradients_change_between_rows_and_whole_tensors(launched):
+    """The table has the strides of this step's gradients, whatever those of the last were, also after a refused one."""
+    params, rows = [torch.ones(3, 8)[:, :7], torch.ones(5)], torch.zeros(3, 11)[:, 2:9]
+    plan = kavg.AdamW(params)
+    for given in (torch.zeros(3, 7), rows, torch.zeros(3, 7), rows, torch.zeros(3, 9)[:, :7]):
+        plan.step([given, torch.zeros(5)], 1)
+        assert [t[1] for t in launched[-1]][0] == given.data_ptr() and [t[10] for t in launched[-1]] == [given.stride(0), 5]
+        refused(lambda: plan.step([rows, None], 1))
