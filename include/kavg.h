@@ -497,7 +497,7 @@ typedef struct {
 /* The step on `count` tensors (host arrays; tensors of no elements are left out).  Asynchronous on hip_stream, may be recorded
  * into a graph, holds nothing between calls.
  * KAVG_EINVAL: bits other than 8 and 32, unknown dtype, lr, eps or weight_decay below 0, a beta outside [0, 1), numbers that are
- * not finite, step 0 (without step_dev), count < 0 or (bits 8) of 2^24 or more, rows or cols < 0, 2^40 elements or more of a tensor,
+ * not finite (lr and grad_scale: in fp32), step 0 (without step_dev), count < 0 or (bits 8) of 2^24 or more, rows or cols < 0, 2^40 elements or more of a tensor,
  * 2^31 rows or more, a stride (of more than one row) below cols or (gradients) below 0, or above 2^46 / rows, pointers that are null or not aligned to an element. */
 int kavg_adamw(const kavg_adamw_options* options, const kavg_adamw_tensor* tensors, int count, void* hip_stream);
 

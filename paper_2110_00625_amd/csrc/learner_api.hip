@@ -88,6 +88,7 @@ ProductCall inner_of(const kavg_product* p) {
 }
 
 bool number_ok(double v) { return v >= 0. && std::isfinite(v); }
+bool fp32_ok(double v) { return std::isfinite((float)v); }
 
 }  // namespace
 
@@ -191,7 +192,7 @@ int kavg_linear_backward(const kavg_product* product, const kavg_rows* dz, const
 int kavg_adamw(const kavg_adamw_options* options, const kavg_adamw_tensor* tensors, int count, void* hip_stream) {
     const kavg_adamw_options* o = options;
     if (!o || (o->bits != 8 && o->bits != 32) || (o->grad_dtype != KAVG_FP32 && o->grad_dtype != KAVG_BF16)) return KAVG_EINVAL;
-    if (!number_ok(o->lr) || !number_ok(o->eps) || !(o->beta1 >= 0. && o->beta1 < 1.) || !(o->beta2 >= 0. && o->beta2 < 1.) || !std::isfinite(o->grad_scale)) return KAVG_EINVAL;
+    if (!number_ok(o->lr) || !number_ok(o->eps) || !(o->beta1 >= 0. && o->beta1 < 1.) || !(o->beta2 >= 0. && o->beta2 < 1.) || !fp32_ok(o->lr) || !fp32_ok(o->grad_scale)) return KAVG_EINVAL;
     if ((!o->step && !o->step_dev) || count < 0 || (o->bits == 8 && count >= 1 << 24) || (count && !tensors)) return KAVG_EINVAL;
     if (((uintptr_t)o->step_dev & 7) || ((uintptr_t)o->lr_dev & 3) || ((uintptr_t)o->grad_scale_dev & 3)) return KAVG_EINVAL;
     const int grad_size = o->grad_dtype == KAVG_BF16 ? 2 : 4, state_size = o->bits / 8;
