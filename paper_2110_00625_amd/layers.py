@@ -72,9 +72,10 @@ class _Products(torch.autograd.Function):
     """residual + (.. act(act(x W_1^T + b_1) W_2^T + b_2) ..) W_n^T + b_n.  parameters: W_1, b_1, .., W_n, b_n."""
 
     @staticmethod
-    def forward(ctx, x, residual, activation, *parameters):
+    def forward(ctx, x, residual, activation, recorded, *parameters):
         weights, biases = parameters[::2], parameters[1::2]
-        last, wanted, kept, inputs, used = len(weights) - 1, any(ctx.needs_input_grad), [], [], []
+        # (recorded: whether gradients are recorded around the call; in here they never are)
+        last, wanted, kept, inputs, used = len(weights) - 1, recorded and any(ctx.needs_input_grad), [], [], []
         h = x
         for i, (w, b) in enumerate(zip(weights, biases)):
             w = w.to(x.dtype)                                        # (float32 weights of bfloat16 activations)
@@ -98,15 +99,15 @@ class _Products(torch.autograd.Function):
         n, saved, wanted = ctx.n, ctx.saved_tensors, ctx.needs_input_grad
         inputs, weights, kept = saved[:n], saved[n:2 * n], saved[2 * n:]
         dz, grads = dy.contiguous(), [None] * (2 * n)
-        lowest = min([i for i in range(n) if wanted[3 + 2 * i] or wanted[4 + 2 * i]] + [0 if wanted[0] else n])
+        lowest = min([i for i in range(n) if wanted[4 + 2 * i] or wanted[5 + 2 * i]] + [0 if wanted[0] else n])
         for i in range(n - 1, lowest - 1, -1):
             inner = wanted[0] if i == 0 else i > lowest
             dx, dw, db = kavg.kavg_linear_backward(
                 dz, inputs[i], weights[i], activation=ctx.activation if i else kavg.KAVG_ACT_NONE, pre=kept[i - 1] if i and kept else None, out=None if inner else False,
-                dweight=None if wanted[3 + 2 * i] else False, dbias=None if wanted[4 + 2 * i] else False)
+                dweight=None if wanted[4 + 2 * i] else False, dbias=None if wanted[5 + 2 * i] else False)
             grads[2 * i], grads[2 * i + 1] = None if dw is None else dw.to(ctx.types[i]), db
             dz = dx
-        return dz if wanted[0] else None, dy if wanted[1] else None, None, *grads
+        return dz if wanted[0] else None, dy if wanted[1] else None, None, None, *grads
 
 
 def mlp(x, layers, activation="silu", residual=None):
@@ -126,7 +127,7 @@ def mlp(x, layers, activation="silu", residual=None):
         if residual.shape != shape:
             raise kavg.KavgError(kavg.KAVG_EINVAL, "a residual of %s for %s" % (tuple(residual.shape), shape))
         residual = residual.reshape(*flat.shape[:-1], outputs)
-    return _Products.apply(flat, residual, ACTIVATIONS[activation], *[p for layer in layers for p in layer]).view(shape)
+    return _Products.apply(flat, residual, ACTIVATIONS[activation], torch.is_grad_enabled(), *[p for layer in layers for p in layer]).view(shape)
 
 
 def linear(x, weight, bias=None, residual=None):
