@@ -62,10 +62,17 @@ def dropout(x, drop, seed, site=0, residual=None):
 
 def _shape(x, weight):
     """x [sets, .., inputs] or [.., inputs] as [sets, rows, inputs] or [rows, inputs]."""
-    if x.dim() < weight.dim() or (weight.dim() == 3 and x.shape[0] != weight.shape[0]):
+    if x.dim() < weight.dim() - 1 or (weight.dim() == 3 and x.shape[0] != weight.shape[0]):
         raise kavg.KavgError(kavg.KAVG_EINVAL, "x of %s and weights of %s" % (tuple(x.shape), tuple(weight.shape)))
     rows = math.prod(x.shape[weight.dim() - 2:-1])
     return x.reshape(x.shape[0], rows, x.shape[-1]) if weight.dim() == 3 else x.reshape(rows, x.shape[-1])
+
+
+def _together(t, either=False):
+    """t, or a copy of it where its last dimension (either: one of its last two) does not lie together."""
+    if t is None or t.shape[-1] < 2 or t.stride(-1) == 1 or (either and (t.shape[-2] < 2 or t.stride(-2) == 1)):
+        return t
+    return t.contiguous()
 
 
 class _Products(torch.autograd.Function):
@@ -112,21 +119,23 @@ class _Products(torch.autograd.Function):
 
 def mlp(x, layers, activation="silu", residual=None):
     """residual + the last of n products, with the activation ("relu", "silu" or None) between them: x [sets, .., inputs] with layers
-    [(weight, bias), ..], weight [sets, outputs, inputs], bias [sets, outputs] (float32) or None; or all of them without sets.  Weights are of
-    x's type, or float32 with bfloat16 activations (rounded in the call).  The activations' derivatives are taken in the epilogues of the
+    [(weight, bias), ..], weight [sets, outputs, inputs], bias [sets, outputs] (float32) or None; or all of them without sets.  Any strides will do (what
+    lies in no order that kavg.kavg_linear takes is copied).  Weights are of x's type, or float32 with bfloat16 activations (rounded in the call).  The activations' derivatives are taken in the epilogues of the
     products of the backward pass; gradients of float32 weights are float32."""
     if activation not in ACTIVATIONS:
         raise kavg.KavgError(kavg.KAVG_EINVAL, "activation %r is none of %s" % (activation, list(ACTIVATIONS)))
     layers = [tuple(layer) for layer in layers]
-    if not layers or any(len(layer) != 2 for layer in layers):
-        raise kavg.KavgError(kavg.KAVG_EINVAL, "%d layers of a weight and a bias" % len(layers))
-    flat = _shape(x, layers[0][0])
+    if not layers or not all(len(layer) == 2 and isinstance(layer[0], torch.Tensor) and layer[0].dim() in (2, 3) and
+                             (layer[1] is None or (isinstance(layer[1], torch.Tensor) and layer[1].dim())) for layer in layers):
+        raise kavg.KavgError(kavg.KAVG_EINVAL, "%d layers of a weight (of two or three dimensions) and a bias" % len(layers))
+    layers = [(_together(weight, either=True), _together(bias)) for weight, bias in layers]
+    flat = _together(_shape(x, layers[0][0]))
     outputs = layers[-1][0].shape[-2]
     shape = (*x.shape[:-1], outputs)
     if residual is not None:
         if residual.shape != shape:
             raise kavg.KavgError(kavg.KAVG_EINVAL, "a residual of %s for %s" % (tuple(residual.shape), shape))
-        residual = residual.reshape(*flat.shape[:-1], outputs)
+        residual = _together(residual.reshape(*flat.shape[:-1], outputs))
     return _Products.apply(flat, residual, ACTIVATIONS[activation], torch.is_grad_enabled(), *[p for layer in layers for p in layer]).view(shape)
 
 
