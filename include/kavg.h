@@ -406,7 +406,7 @@ int kavg_dropout_backward(const void* dy, int64_t dy_stride, void* dx, int64_t d
  * Matrix products with bias, activation and residual in their epilogue, for all learners at once, and their gradients; caller
  * arrays, conventions and errors as for the layers above.  dtype is that of x, the weights, y and their like (KAVG_FP32 or
  * KAVG_BF16; a learner's bf16 weights are the copy that kavg_adamw or the shadow that kavg_meta_update_flat writes); biases and
- * gradients of weights and biases are fp32.  Sums are fp32, a result is rounded once.
+ * gradients of weights and biases are fp32.  Sums are fp32 (db's in runs of some 2048 rows, which are added in 64 bits), a result is rounded once.
  *   z = x W^T + b,   y = residual + activation(z)                                             (kavg_linear)
  *   from dz, the gradient of z:  dx = (dz W) * slope(pre),  dW = dz^T x,  db = sum of dz's rows   (kavg_linear_backward)
  * In a net of several layers x is the activation of the layer below: `activation` of the backward call is that layer's and `pre` its

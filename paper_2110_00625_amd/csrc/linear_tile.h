@@ -219,7 +219,19 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     constexpr int MS = MR > MC ? MR : MC;
     float sums[RT ? MS : 1][4] = {};
+    double totals[RT ? MS : 1] = {};
     const bool sum_r = RT && a.side == 1 && tile_c == 0 && wc == 0, sum_c = RT && a.side == 2 && tile_r == 0 && wr == 0;
+
+    // Sums of dz: a run of 2048 rows in fp32 (256 terms to each of a lane's four), runs in 64 bits, so that any number of rows will do.
+    constexpr int RUN = 2048 / BK;
+    auto end_run = [&](int slices_done) {
+        if (!RT || slices_done % RUN || !(sum_r || sum_c)) return;
+#pragma unroll
+        for (int i = 0; i < (RT ? MS : 1); ++i) {
+            totals[i] += (double)((sums[i][0] + sums[i][1]) + (sums[i][2] + sums[i][3]));
+            sums[i][0] = sums[i][1] = sums[i][2] = sums[i][3] = 0.f;
+        }
+    };
 
     // Fragments of a slab are asked for while the one before it is multiplied: two sets of registers.
     chunk rf[2][MR], cf[2][MC];
@@ -323,6 +335,7 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
             load(whole, now, left);
             multiply_slab((SLABS - 1) & 1);
             interleave(std::integral_constant<int, LOADS>());
+            end_run(s + 1);
             turn();
         }
         for (; s < slices; ++s, left -= BK) {
@@ -359,6 +372,7 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
                 if (slab + 1 < SLABS) take(~slab & 1, now, slab + 1);
                 multiply_slab(slab & 1);
             }
+            end_run(s + 1);
         }
     }
 
@@ -368,8 +382,8 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
 #pragma unroll
         for (int i = 0; i < MS; ++i) {
             if (i >= (sum_r ? MR : MC)) break;
-            const float half = (sums[RT ? i : 0][0] + sums[RT ? i : 0][1]) + (sums[RT ? i : 0][2] + sums[RT ? i : 0][3]);
-            const float sum = half + __shfl_xor(half, 32);
+            const double half = totals[RT ? i : 0] + (double)((sums[RT ? i : 0][0] + sums[RT ? i : 0][1]) + (sums[RT ? i : 0][2] + sums[RT ? i : 0][3]));
+            const float sum = (float)(half + __shfl_xor(half, 32));
             const int x = first + i * 32 + lane;
             if (lane < 32 && x < n) to[x] = sum;
         }
