@@ -116,7 +116,7 @@ bool aligned(const Matrix& m, int64_t sets, int64_t lines, int extent, int elem)
 // fp32 by large 1032, middle 1004, small 1106.)
 struct Cost { float alone, shared, ends; };
 static constexpr Cost BF16_COST[TILE_KINDS] = {{1.75f, 1.75f, 8.f}, {0.5f, 0.48f, 2.f}, {0.24f, 0.17f, 0.5f}, {0.21f, 0.15f, 0.8f}};
-static constexpr Cost F32_COST[TILE_KINDS] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}, {0.54f, 0.54f, 0.8f}};
+static constexpr Cost F32_COST[TILE_DEEP] = {{8.f, 8.f, 8.f}, {1.95f, 1.95f, 2.f}, {0.52f, 0.52f, 0.5f}};
 
 Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned) {
     const int64_t slices = up(nK, slice_of(dtype));
@@ -125,13 +125,15 @@ Plan product_plan(int dtype, int64_t sets, int nR, int nC, int nK, Turned turned
     p.splits = 1;
     float least = INFINITY;
     for (int tile = 0; tile < TILE_KINDS; ++tile) {
+        // (turned operands gain nothing by slices further ahead: 16 learners' 128x1024x1024 10.5 us by deep tiles and 11.7 by small ones, turned 13.6 and 13.0; fp32
+        // ones neither, whose products take longer than the loads)
+        if (tile == TILE_DEEP && (dtype != KAVG_BF16 || turned != NONE_TURNED)) break;
         const Cost& c = (dtype == KAVG_BF16 ? BF16_COST : F32_COST)[tile];
         const int64_t tiles = tiles_of(tile, sets, nR, nC);
         for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (splits > 1 && (2 * splits > slices || tiles * splits > 8 * CUS)) break;
             const int64_t each = up(slices, splits), m = up(tiles * up(slices, std::max<int64_t>(each, 1)), CUS);
-            // (turned operands gain nothing by slices further ahead: 16 learners' 128x1024x1024 10.5 us by deep tiles and 11.7 by small ones, turned 13.6 and 13.0)
-            if (tile == TILE_DEEP && (m > 2 || turned != NONE_TURNED)) continue;
+            if (tile == TILE_DEEP && m > 2) continue;
             float cost = m * c.ends + each * std::max(c.alone, c.shared * m);
             // the launch that joins the parts, which are written and read
             if (splits > 1) cost += 4.f + 0.1f * splits + (float)sets * nR * p.pitch * splits * 8 / 5.5e6f;

@@ -427,12 +427,12 @@ __global__ void __launch_bounds__(64 * WR * WC) product_kernel(ProductArgs a) {
     else emit(Finisher<E, O, TURNS, false, APART>(a.finish, set, c, a.nC - c), apart);
 }
 
-// Tiles: rows, columns, wavefronts along rows and columns, buffers.  The last is that of few small tiles with a long contraction.
+// Tiles: rows, columns, wavefronts along rows and columns, buffers.  The last is that of few small tiles with a long contraction, in bf16.
 #define KAVG_TILES(TILE) TILE(0, 256, 256, 2, 4, 2) TILE(1, 128, 128, 2, 2, 2) TILE(2, 64, 64, 2, 2, 2) TILE(3, 64, 64, 2, 2, 4)
 enum { TILE_LARGE = 0, TILE_MIDDLE = 1, TILE_SMALL = 2, TILE_DEEP = 3, TILE_KINDS = 4 };
 
 // DIRECT wants operands whose chunks are aligned and whole; the first and the last tile are for such operands only, the last
-// for operands that are not turned
+// for bf16 operands that are not turned
 template <class E, int TR, int TC, int WR, int WC, int BUFFERS, bool RT, bool CT, bool DIRECT>
 hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
     typedef ProductTile<E, TR, TC, WR, WC, BUFFERS, RT, CT, DIRECT> P;
@@ -448,7 +448,7 @@ hipError_t start_tile(const ProductArgs& a, hipStream_t st) {
 template <class E, bool RT, bool CT> hipError_t start_kind(int tile, bool direct, const ProductArgs& a, hipStream_t st) {
 #define TILE(NUMBER, TR, TC, WR, WC, BUFFERS) \
     case NUMBER: \
-        if constexpr (BUFFERS == 2 || !CT) { if (direct) return start_tile<E, TR, TC, WR, WC, BUFFERS, RT, CT, true>(a, st); } \
+        if constexpr (BUFFERS == 2 || (!CT && sizeof(E) == 2)) { if (direct) return start_tile<E, TR, TC, WR, WC, BUFFERS, RT, CT, true>(a, st); } \
         if constexpr (TR * TC < 256 * 256 && BUFFERS == 2) return start_tile<E, TR, TC, WR, WC, BUFFERS, RT, CT, false>(a, st); \
         break;
     switch (tile) { KAVG_TILES(TILE) }
