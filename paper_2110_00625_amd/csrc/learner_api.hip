@@ -10,7 +10,7 @@ namespace {
 using namespace kavg;
 
 constexpr int64_t MOST_ROWS = INT32_MAX - 65535;             // (tiles reach past them in 32 bits)
-constexpr int64_t MOST_COLUMNS = 1 << 27;                    // inputs, outputs: 2^22 tiles of 32, those of a launch
+constexpr int64_t MOST_COLUMNS = 1 << 27;                    // inputs, outputs: 2^21 tiles of 64; a launch takes 2^22
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 42, MOST_SPAN = (int64_t)1 << 46;
 
 int64_t at_least_one(int64_t n) { return n > 1 ? n : 1; }

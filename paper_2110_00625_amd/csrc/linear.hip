@@ -207,7 +207,7 @@ hipError_t launch_product(const ProductCall& call, void* workspace, size_t bytes
     a.finish = call.finish;
     a.side = call.side;
     a.sums = call.sums; a.sums_set = call.sums_set;
-    // as many learners and rows at once as a launch takes (all of them, but for results of some hundred gigabytes)
+    // as many learners and rows at once as a launch takes (all of them, but for more than four million learners of small layers or hundreds of millions of rows)
     const int64_t of_row = (int64_t)a.tiles_c * a.splits, rows_at_once = std::min<int64_t>(call.nR, std::max<int64_t>(1, MOST_TILES / of_row) * size.r);
     const int64_t sets_at_once = rows_at_once < call.nR ? 1 : std::max<int64_t>(1, MOST_TILES / (of_row * up(call.nR, size.r)));
     if (of_row > MOST_TILES || (plan.splits > 1 && (rows_at_once < call.nR || sets_at_once < call.sets))) return hipErrorInvalidValue;
