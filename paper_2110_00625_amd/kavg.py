@@ -648,7 +648,7 @@ class AdamW:
         # What the table points to stays allocated, whatever becomes of the tensors given: states are written where they were, parameters and copies, which others
         # read through those tensors, are looked at by every step.
         self._states = [tuple(s.detach() for s in state) for state in states]
-        self._memory = [t.detach() for t in self.params + self.copies if t is not None]
+        self._memory = [t.untyped_storage() for t in self.params + self.copies if t is not None]
         self._at = self._addresses()
         # (views of one tensor have its version)
         self._versions = list({id(t): t for t in (t._base if t._is_view() else t for t in self.params + self.copies if t is not None)}.values())
