@@ -20,6 +20,8 @@
 // cycles, at a clock that falls to 1.5 - 1.8 GHz under them; the rest are a pipeline's ends and results (100 us of the last) and waits for memory.  Steps on the
 // way: the barrier in front of the last slab instead of the first and pinned orders 1190 -> 1044 (the gradient of x), waits that the compiler counts 227 -> 209,
 // results through LDS 1085 -> 938.  In fp32 4096^3 takes 1010 us, 136 TFLOP/s of the 145 that a library's product reaches.  Small tiles: latency, 0.2 us a slice.
+// Through registers: the wait for a whole slice in front of every barrier (four of 1001^3 in bf16 22 us, of 1000^3 straight into LDS 16; 3x1003x997x515 in fp32 43.6,
+// the matrix cores busy for 45 % of the cycles).
 // Tried: rings of slices of 64 bytes (half lines: 220 for 209, turned 282 for 239), four wavefronts of 128x128 (registers in scratch), tiles of 128x32,
 // 32x128 and 128x64 (in no swept case better by more than 4 %).
 #pragma once
